@@ -345,6 +345,139 @@ DN_API dn_status attention_decode_deferred_noalloc(const void* Q, const void* K,
                                             void* out, hipStream_t stream);
 
 /* ======================================================================= */
+/* Rotary positions                                                         */
+/* ======================================================================= */
+
+/*
+ * Rotary positions turn pairs of dimensions of a query or key head by an angle
+ * proportional to the token's position, y_p = x_p cos - x_q sin and
+ * y_q = x_q cos + x_p sin, where (p, q) = (2i, 2i + 1) (interleaved) or
+ * (i, i + rot/2) (halves), i < rot/2; dimensions from rot on stay as they are.
+ *
+ * rotary_table fills table[positions][rot/2][2] (fp32, caller-owned, 16-byte
+ * aligned) with amplitude * cos and amplitude * sin of n * inv_freq[i] for
+ * n < positions, evaluated in fp64 and rounded once; once per model, off the
+ * per-token path.  inv_freq[rot/2] are fp64 device values, 8-byte aligned: plain
+ * frequencies base^(-2i/rot), or any that were scaled for long contexts.
+ * amplitude is finite (1 where the scaling asks for none).
+ *
+ * rotary_apply turns x[T][H][d] (DN_F32 or DN_BF16; x_stride elements between
+ * tokens, heads contiguous) by table row positions[t] into out (out_stride
+ * likewise).  inverse = 1 turns back: the transpose, so the gradient with respect
+ * to x from the gradient with respect to out.  out may be x itself with equal
+ * strides; other overlaps are refused.  rot is a multiple of 16 up to d, d a
+ * multiple of 16, strides multiples of 16 bytes and at least H * d.  A position
+ * outside the table gives NaN in the turned dimensions.  positions: int32, 4-byte
+ * aligned.  Arithmetic is fp32, each result rounded once.
+ */
+DN_API dn_status rotary_table(const double* inv_freq, int64_t rot, int64_t positions, double amplitude, float* table,
+                       hipStream_t stream);
+
+DN_API dn_status rotary_apply(const void* x, int64_t x_stride, const int32_t* positions, const float* table,
+                       int64_t table_rows, int64_t T, int64_t H, int64_t d, int64_t rot, int interleaved, int inverse,
+                       int dtype, void* out, int64_t out_stride, hipStream_t stream);
+
+/* ======================================================================= */
+/* Paged key/value cache                                                    */
+/* ======================================================================= */
+
+/*
+ * A cache is one caller-owned device buffer of `pages` pages of DN_KV_PAGE
+ * tokens for `heads` key/value heads of d = 64 or 128 dimensions; which pages
+ * hold which sequence is the caller's.  Slot s is token s % 64 of page s / 64.
+ * Formats: DN_KV_BF16 holds bfloat16; DN_KV_FP8 holds OCP e4m3 codes with one
+ * fp32 scale per token and head, x = code * scale, scale = max(max |x| / 448,
+ * 2^-120), the code rounded to nearest even.  Either way a row (K or V of one
+ * token and head) that holds a NaN or an infinity is held as all NaN: codes 0,
+ * scale NaN (the scale is 1 elsewhere in DN_KV_BF16).
+ * Layout (version 1) of `data`: [pages][heads][block], block = K codes, V codes,
+ * 64 K scales, 64 V scales.  With E = 8 (bf16) or 16 (fp8) elements in 16 bytes,
+ * token 4E u + E a + 8 j + 4 t + i, dimension 4E c + E g + r of K lies at byte
+ * (((((E/8 u + j) 2 + t) d/(4E) + c) 4 + g) 16 + 4 a + i) 16 + r 16/E, and token
+ * 4E u + E g + r, dimension 16 n + w of V at byte
+ * (((u d/16 + n) 4 + g) 16 + w) 16 + r 16/E.
+ * kv_cache_describe checks the sizes (pages * 64 < 2^31), the buffer's
+ * kv_cache_bytes and its 256-byte alignment and fills *out on the host; it
+ * touches no memory, and no entry point reads slots that were never written
+ * except as masked keys, so the buffer needs no clearing.
+ */
+#define DN_KV_PAGE 64
+#define DN_KV_LAYOUT_VERSION 1
+typedef enum { DN_KV_BF16 = 1, DN_KV_FP8 = 2 } dn_kv_format;
+
+typedef struct {
+    int64_t pages, heads, d;
+    int32_t format;         /* dn_kv_format                          */
+    int32_t layout_version; /* DN_KV_LAYOUT_VERSION when described   */
+    void* data;
+} kv_cache;
+
+/* Bytes of the buffer; 0 if the request is invalid. */
+DN_API size_t kv_cache_bytes(int64_t pages, int64_t heads, int64_t d, int format);
+
+DN_API dn_status kv_cache_describe(void* data, size_t bytes, int64_t pages, int64_t heads, int64_t d, int format,
+                            kv_cache* out);
+
+/*
+ * Takes the rows of a QKV projection, qkv[T][q_heads + 2 heads][d] (DN_BF16;
+ * `stride` elements between tokens, a multiple of 8): turns the query heads into
+ * q_out[T][q_heads][d] and the key heads as rotary_apply does, and puts keys and
+ * values into the cache at slots[t] (quantised from the turned fp32 values, one
+ * rounding).  q_heads is a multiple of the cache's heads, or 0 (q_out then NULL):
+ * rows of keys and values alone.  rot = 0 turns nothing (positions and table
+ * unused).  A slot outside the cache (-1 by convention) is not written: padding.
+ * A slot named twice in a call is left with either token, whole or mixed.
+ */
+DN_API dn_status kv_cache_append(const kv_cache* cache, const void* qkv, int64_t stride, const int32_t* slots,
+                          const int32_t* positions, const float* table, int64_t table_rows, int64_t rot,
+                          int interleaved, int64_t T, int64_t q_heads, int dtype, void* q_out, hipStream_t stream);
+
+/* K, V [T][heads][d] (DN_BF16): the values held at slots[t], zeros for a slot outside the cache. */
+DN_API dn_status kv_cache_read(const kv_cache* cache, const int32_t* slots, int64_t T, int dtype, void* K, void* V,
+                        hipStream_t stream);
+
+/*
+ * Deferred attention of B ragged sequences over the cache.  Sequence b's new
+ * tokens are rows q_start[b] .. q_start[b + 1] - 1 of Q[T][q_heads][d] (q_start
+ * ascending from 0 to T; a sequence may have none); its kv_len[b] cached tokens,
+ * the new ones last, lie in pages block_table[b][0], [1], .. (table_width entries
+ * a row).  Query i of n sees keys 0 .. kv_len[b] - n + i: one new token is a decode
+ * step, many are a prefill chunk, and both may meet in one call.  Query head h
+ * reads key/value head h / (q_heads / heads).  out[T][q_heads][d]; Q has q_stride
+ * elements between tokens (a multiple of 8), scale finite and > 0, dtype DN_BF16.
+ * q_start, kv_len and block_table are int32 device arrays, read on the device, so a
+ * recorded graph replays with their new contents.  A query that sees no key gives
+ * zeros; one whose scores are all -inf gives NaN.  Entries outside the cache, the
+ * table or [0, T] are kept inside (page 0, the table's width, T): memory stays
+ * safe, the rows concerned are unspecified.
+ * workspace: caller-owned, 256-byte aligned, attention_cache_workspace_bytes
+ * (with prefix_len = 0), scratch.  Where one workgroup reads a tile's keys whole
+ * one launch writes out; else partial sums go through the workspace as in
+ * attention_decode_deferred.
+ *
+ * attention_shared_prefix_deferred: the same where all B sequences share
+ * prefix_len >= 1 leading tokens in the pages prefix_table[0], [1], ..; block_table
+ * and kv_len then count each sequence's own tokens, and every query also sees the
+ * whole prefix.  The prefix is read once per key/value head for the queries of all
+ * sequences together, and its partial sums are merged with those over the
+ * sequences' own keys.
+ * attention_cache_workspace_bytes returns 0 for an invalid request.
+ */
+DN_API size_t attention_cache_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d,
+                                       int64_t table_width, int64_t prefix_len);
+
+DN_API dn_status attention_cache_deferred(const void* Q, int64_t q_stride, int64_t T, int64_t q_heads,
+                                   const kv_cache* cache, const int32_t* block_table, int64_t table_width,
+                                   const int32_t* q_start, const int32_t* kv_len, int64_t B, float scale, int dtype,
+                                   void* workspace, size_t workspace_bytes, void* out, hipStream_t stream);
+
+DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_stride, int64_t T, int64_t q_heads,
+                                           const kv_cache* cache, const int32_t* prefix_table, int64_t prefix_len,
+                                           const int32_t* block_table, int64_t table_width, const int32_t* q_start,
+                                           const int32_t* kv_len, int64_t B, float scale, int dtype, void* workspace,
+                                           size_t workspace_bytes, void* out, hipStream_t stream);
+
+/* ======================================================================= */
 /* Unfused comparators: the conventional sub-graph of Fig. 1(a)             */
 /* ======================================================================= */
 

@@ -6,6 +6,7 @@
 
 #include "dn.h"
 #include "dn_launch.hpp"
+#include "kv_layout.hpp"
 #include "launch_rules.hpp"
 
 namespace {
@@ -419,6 +420,205 @@ DN_API dn_status gemm(const void* A, const void* B, const void* bias, int64_t ba
         return DN_ERR_INVALID_ARG;
     if (((M + 31) / 32) * ((N + 63) / 64) > kMaxGridX) return DN_ERR_UNSUPPORTED;
     return from_hip(dn::launch_gemm(A, B, bias, batch, M, K, N, b_layout, a_causal, dtype, C, stream));
+}
+
+// ------------------------------------------------------------------- rotary positions, paged cache
+// What a strided [T][width] array spans, from its first to past its last element.
+static bool span_of(int64_t T, int64_t stride, int64_t width, int64_t es, size_t* out) {
+    size_t all, last;
+    if (!bytes_of(T - 1 > 0 ? T - 1 : 1, stride, es, &all) || !bytes_of(width, es, 1, &last)) return false;
+    if (T == 1) all = 0;
+    return !__builtin_add_overflow(all, last, out);
+}
+
+DN_API dn_status rotary_table(const double* inv_freq, int64_t rot, int64_t positions, double amplitude, float* table,
+                              hipStream_t stream) {
+    if (!inv_freq || !table || rot < 1 || positions < 1 || !isfinite(amplitude)) return DN_ERR_INVALID_ARG;
+    size_t tb;
+    if (!bytes_of(positions, rot, 4, &tb)) return DN_ERR_INVALID_ARG;
+    if (rot % 16) return DN_ERR_UNSUPPORTED;
+    if (!aligned(inv_freq, 8) || !aligned(table, 16)) return DN_ERR_MISALIGNED;
+    if (overlaps(table, tb, inv_freq, (size_t)rot * 4)) return DN_ERR_INVALID_ARG;
+    if (positions > INT32_MAX || (positions * (rot / 2) + 255) / 256 > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    return from_hip(dn::launch_rotary_table(inv_freq, rot, positions, amplitude, table, stream));
+}
+
+DN_API dn_status rotary_apply(const void* x, int64_t x_stride, const int32_t* positions, const float* table,
+                              int64_t table_rows, int64_t T, int64_t H, int64_t d, int64_t rot, int interleaved,
+                              int inverse, int dtype, void* out, int64_t out_stride, hipStream_t stream) {
+    if (!x || !positions || !table || !out || table_rows < 1 || T < 1 || H < 1 || d < 1 || rot < 1 || rot > d ||
+        !valid_dtype(dtype) || (interleaved != 0 && interleaved != 1) || (inverse != 0 && inverse != 1))
+        return DN_ERR_INVALID_ARG;
+    const int64_t es = (int64_t)esize(dtype);
+    size_t hd, xb, ob, tb;
+    if (!bytes_of(H, d, es, &hd) || x_stride < H * d || out_stride < H * d || !span_of(T, x_stride, H * d, es, &xb) ||
+        !span_of(T, out_stride, H * d, es, &ob) || !bytes_of(table_rows, rot, 4, &tb))
+        return DN_ERR_INVALID_ARG;
+    if (d % 16 || rot % 16 || x_stride * es % 16 || out_stride * es % 16) return DN_ERR_UNSUPPORTED;
+    if (!aligned(x, 16) || !aligned(out, 16) || !aligned(table, 16) || !aligned(positions, 4)) return DN_ERR_MISALIGNED;
+    const bool in_place = out == x && out_stride == x_stride;
+    if ((!in_place && overlaps(out, ob, x, xb)) || overlaps(out, ob, table, tb) ||
+        overlaps(out, ob, positions, (size_t)T * 4))
+        return DN_ERR_INVALID_ARG;
+    const int64_t items = H * d / (dtype == DN_F32 ? 8 : 16);
+    if (items > INT32_MAX || T > INT32_MAX || T > (kMaxGridX * 256 - 255) / items) return DN_ERR_UNSUPPORTED;
+    return from_hip(dn::launch_rotary(x, x_stride, positions, table, table_rows, T, H, d, rot, interleaved, inverse,
+                                      dtype, out, out_stride, stream));
+}
+
+static bool valid_kv(int64_t pages, int64_t heads, int64_t d, int format, size_t* bytes) {
+    int64_t blocks, all;
+    if (pages < 1 || heads < 1 || (d != 64 && d != 128) || (format != DN_KV_BF16 && format != DN_KV_FP8)) return false;
+    if (pages > INT32_MAX / DN_KV_PAGE || heads > INT32_MAX || __builtin_mul_overflow(pages, heads, &blocks) ||
+        __builtin_mul_overflow(blocks, (int64_t)dn::kv_block_bytes(d, format), &all))
+        return false;
+    *bytes = (size_t)all;
+    return true;
+}
+
+DN_API size_t kv_cache_bytes(int64_t pages, int64_t heads, int64_t d, int format) {
+    size_t b;
+    return valid_kv(pages, heads, d, format, &b) ? b : 0;
+}
+
+DN_API dn_status kv_cache_describe(void* data, size_t bytes, int64_t pages, int64_t heads, int64_t d, int format,
+                                   kv_cache* out) {
+    if (!data || !out || pages < 1 || heads < 1 || d < 1 || (format != DN_KV_BF16 && format != DN_KV_FP8))
+        return DN_ERR_INVALID_ARG;
+    size_t need;
+    if (!valid_kv(pages, heads, d, format, &need)) return DN_ERR_UNSUPPORTED;
+    if (bytes < need) return DN_ERR_INVALID_ARG;
+    if (!aligned(data, 256)) return DN_ERR_MISALIGNED;
+    out->pages = pages;
+    out->heads = heads;
+    out->d = d;
+    out->format = format;
+    out->layout_version = DN_KV_LAYOUT_VERSION;
+    out->data = data;
+    return DN_OK;
+}
+
+// A described cache; its bytes.
+static bool described(const kv_cache* c, size_t* bytes) {
+    return c && c->data && c->layout_version == DN_KV_LAYOUT_VERSION &&
+           valid_kv(c->pages, c->heads, c->d, c->format, bytes);
+}
+static dn::KvPool pool_of(const kv_cache* c) { return dn::KvPool{c->pages, c->heads, c->d, c->format, c->data}; }
+
+DN_API dn_status kv_cache_append(const kv_cache* cache, const void* qkv, int64_t stride, const int32_t* slots,
+                                 const int32_t* positions, const float* table, int64_t table_rows, int64_t rot,
+                                 int interleaved, int64_t T, int64_t q_heads, int dtype, void* q_out,
+                                 hipStream_t stream) {
+    size_t cb, xb, qb = 0, tb = 0;
+    if (!described(cache, &cb) || !qkv || !slots || T < 1 || q_heads < 0 || q_heads > INT32_MAX || !valid_dtype(dtype) ||
+        (q_heads > 0) != (q_out != nullptr) || rot < 0 || rot > cache->d || (interleaved != 0 && interleaved != 1))
+        return DN_ERR_INVALID_ARG;
+    if (q_heads % cache->heads) return DN_ERR_INVALID_ARG;
+    if (rot > 0 && (!positions || !table || table_rows < 1 || !bytes_of(table_rows, rot, 4, &tb)))
+        return DN_ERR_INVALID_ARG;
+    const int64_t width = (q_heads + 2 * cache->heads) * cache->d;
+    if (stride < width || !span_of(T, stride, width, 2, &xb) || (q_heads && !bytes_of(T, q_heads, cache->d * 2, &qb)))
+        return DN_ERR_INVALID_ARG;
+    if (dtype != DN_BF16 || rot % 16 || stride % 8) return DN_ERR_UNSUPPORTED;
+    if (!aligned(qkv, 16) || !aligned(q_out, 16) || !aligned(cache->data, 256) || !aligned(slots, 4) ||
+        (rot > 0 && (!aligned(table, 16) || !aligned(positions, 4))))
+        return DN_ERR_MISALIGNED;
+    const size_t ib = (size_t)T * 4;
+    const void* ins[4] = {qkv, slots, rot > 0 ? positions : nullptr, rot > 0 ? table : nullptr};
+    const size_t in_bytes[4] = {xb, ib, ib, tb};
+    for (int i = 0; i < 4; ++i)
+        if (overlaps(cache->data, cb, ins[i], in_bytes[i]) || overlaps(q_out, qb, ins[i], in_bytes[i]))
+            return DN_ERR_INVALID_ARG;
+    if (overlaps(cache->data, cb, q_out, qb)) return DN_ERR_INVALID_ARG;
+    // a workgroup's items and the grid fit 31 bits
+    if (width > (int64_t(1) << 24) || T > INT32_MAX / 4 || (T + 3) / 4 > kMaxGridX / cache->heads)
+        return DN_ERR_UNSUPPORTED;
+    return from_hip(dn::launch_kv_append(qkv, stride, slots, positions, table, table_rows, rot, interleaved, T, q_heads,
+                                         pool_of(cache), q_out, stream));
+}
+
+DN_API dn_status kv_cache_read(const kv_cache* cache, const int32_t* slots, int64_t T, int dtype, void* K, void* V,
+                               hipStream_t stream) {
+    size_t cb, ob;
+    if (!described(cache, &cb) || !slots || !K || !V || T < 1 || !valid_dtype(dtype) ||
+        !bytes_of(T, cache->heads, cache->d * 2, &ob))
+        return DN_ERR_INVALID_ARG;
+    if (dtype != DN_BF16) return DN_ERR_UNSUPPORTED;
+    if (!aligned(K, 16) || !aligned(V, 16) || !aligned(cache->data, 256) || !aligned(slots, 4)) return DN_ERR_MISALIGNED;
+    const size_t ib = (size_t)T * 4;
+    if (overlaps(K, ob, V, ob) || overlaps(K, ob, cache->data, cb) || overlaps(V, ob, cache->data, cb) ||
+        overlaps(K, ob, slots, ib) || overlaps(V, ob, slots, ib))
+        return DN_ERR_INVALID_ARG;
+    if (T > INT32_MAX / 4 || (T + 3) / 4 > kMaxGridX / cache->heads) return DN_ERR_UNSUPPORTED;
+    return from_hip(dn::launch_kv_read(pool_of(cache), slots, T, K, V, stream));
+}
+
+// Sizes for which every count of the attention kernels fits its type.
+static bool attention_cache_sizes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d, int64_t width,
+                                  int64_t prefix) {
+    constexpr int64_t k31 = INT32_MAX;
+    return T <= k31 / 128 && B <= (int64_t(1) << 20) && q_heads <= (int64_t(1) << 16) && T * q_heads <= k31 / 2 &&
+           width <= k31 / DN_KV_PAGE && prefix <= k31 - DN_KV_PAGE && (T + B) * heads <= k31 / 4 &&
+           B * width < (int64_t(1) << 40) && (d == 64 || d == 128);
+}
+
+DN_API size_t attention_cache_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d,
+                                              int64_t table_width, int64_t prefix_len) {
+    if (T < 1 || B < 1 || heads < 1 || q_heads < 1 || q_heads % heads || table_width < 1 || prefix_len < 0 ||
+        !attention_cache_sizes(T, B, q_heads, heads, d, table_width, prefix_len))
+        return 0;
+    return dn::cache_workspace(T, B, heads, q_heads / heads, d, table_width, (prefix_len + DN_KV_PAGE - 1) / DN_KV_PAGE)
+        .total;
+}
+
+static dn_status attention_cache(const void* Q, int64_t q_stride, int64_t T, int64_t q_heads, const kv_cache* cache,
+                                 const int32_t* prefix_table, int64_t prefix, const int32_t* table, int64_t width,
+                                 const int32_t* q_start, const int32_t* kv_len, int64_t B, float scale, int dtype,
+                                 void* workspace, size_t workspace_bytes, void* out, hipStream_t stream) {
+    size_t cb, qb, ob, tb;
+    if (!described(cache, &cb) || !Q || !table || !q_start || !kv_len || !workspace || !out || T < 1 || B < 1 ||
+        q_heads < 1 || q_heads % cache->heads || width < 1 || !valid_dtype(dtype) || !isfinite(scale) || !(scale > 0.f))
+        return DN_ERR_INVALID_ARG;
+    if (!bytes_of(B, width, 4, &tb)) return DN_ERR_INVALID_ARG;
+    if (!attention_cache_sizes(T, B, q_heads, cache->heads, cache->d, width, prefix)) return DN_ERR_UNSUPPORTED;
+    const int64_t row = q_heads * cache->d;
+    if (q_stride < row || !span_of(T, q_stride, row, 2, &qb) || !bytes_of(T, row, 2, &ob)) return DN_ERR_INVALID_ARG;
+    if (dtype != DN_BF16 || q_stride % 8) return DN_ERR_UNSUPPORTED;
+    const size_t need = attention_cache_workspace_bytes(T, B, q_heads, cache->heads, cache->d, width, prefix);
+    if (workspace_bytes < need) return DN_ERR_INVALID_ARG;
+    if (!aligned(Q, 16) || !aligned(out, 16) || !aligned(cache->data, 256) || !aligned(workspace, 256) ||
+        !aligned(table, 4) || !aligned(q_start, 4) || !aligned(kv_len, 4) || !aligned(prefix_table, 4))
+        return DN_ERR_MISALIGNED;
+    const void* ins[6] = {Q, cache->data, table, q_start, kv_len, prefix_table};
+    const size_t in_bytes[6] = {qb, cb, tb, (size_t)(B + 1) * 4, (size_t)B * 4, (size_t)((prefix + 63) / 64) * 4};
+    for (int i = 0; i < 6; ++i)
+        if (overlaps(out, ob, ins[i], in_bytes[i]) || overlaps(workspace, need, ins[i], in_bytes[i]))
+            return DN_ERR_INVALID_ARG;
+    if (overlaps(workspace, need, out, ob)) return DN_ERR_INVALID_ARG;
+    return from_hip(dn::launch_attention_cache(
+        dn::AttentionCacheCall{Q, q_stride, T, q_heads, pool_of(cache), prefix_table, prefix, table, width, q_start, kv_len,
+                               B, scale, workspace, out},
+        stream));
+}
+
+DN_API dn_status attention_cache_deferred(const void* Q, int64_t q_stride, int64_t T, int64_t q_heads,
+                                          const kv_cache* cache, const int32_t* block_table, int64_t table_width,
+                                          const int32_t* q_start, const int32_t* kv_len, int64_t B, float scale,
+                                          int dtype, void* workspace, size_t workspace_bytes, void* out,
+                                          hipStream_t stream) {
+    return attention_cache(Q, q_stride, T, q_heads, cache, nullptr, 0, block_table, table_width, q_start, kv_len, B, scale,
+                           dtype, workspace, workspace_bytes, out, stream);
+}
+
+DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_stride, int64_t T, int64_t q_heads,
+                                                  const kv_cache* cache, const int32_t* prefix_table,
+                                                  int64_t prefix_len, const int32_t* block_table, int64_t table_width,
+                                                  const int32_t* q_start, const int32_t* kv_len, int64_t B, float scale,
+                                                  int dtype, void* workspace, size_t workspace_bytes, void* out,
+                                                  hipStream_t stream) {
+    if (!prefix_table || prefix_len < 1) return DN_ERR_INVALID_ARG;
+    return attention_cache(Q, q_stride, T, q_heads, cache, prefix_table, prefix_len, block_table, table_width, q_start,
+                           kv_len, B, scale, dtype, workspace, workspace_bytes, out, stream);
 }
 
 }  // extern "C"

@@ -110,6 +110,51 @@ hipError_t launch_layernorm(const void* x, const void* gamma, const void* beta, 
 hipError_t launch_softmax(const void* S, int64_t BH, int64_t Lq, int64_t Lk, int causal, void* P,
                           hipStream_t s);
 
+// ---- the paged key/value cache (layout: kv_layout.hpp)
+struct KvPool {
+    int64_t pages, heads, d;
+    int format;
+    void* data;
+};
+
+// table[n][i] = amplitude * (cos, sin)(n inv_freq[i]), i < rot / 2, in fp64, rounded once.
+hipError_t launch_rotary_table(const double* inv_freq, int64_t rot, int64_t rows, double amplitude, float* table,
+                               hipStream_t s);
+
+// Turns the first `rot` dimensions of x[tokens][heads][d] (strides in elements between tokens) by
+// table row positions[token]; inverse: by the opposite angle.
+hipError_t launch_rotary(const void* x, int64_t x_stride, const int32_t* positions, const float* table, int64_t rows,
+                         int64_t tokens, int64_t heads, int64_t d, int64_t rot, int interleaved, int inverse, int dtype,
+                         void* out, int64_t out_stride, hipStream_t s);
+
+// Rows of Q, K, V heads: Q turned into q_out, K turned and V put into the cache at their slots (those
+// outside it: not written).  rot = 0: nothing is turned, table and positions unused.
+hipError_t launch_kv_append(const void* qkv, int64_t stride, const int32_t* slots, const int32_t* positions,
+                            const float* table, int64_t rows, int64_t rot, int interleaved, int64_t tokens,
+                            int64_t q_heads, const KvPool& c, void* q_out, hipStream_t s);
+
+// K, V [tokens][heads][d] of the slots (those outside the cache: zeros).
+hipError_t launch_kv_read(const KvPool& c, const int32_t* slots, int64_t tokens, void* K, void* V, hipStream_t s);
+
+// Attention of B ragged sequences (tokens q_start[b] .. q_start[b + 1] - 1 of Q, kv_len[b] keys in the
+// pages of row b of the table), all behind `prefix` keys of the pages of prefix_table (0: none).
+struct AttentionCacheCall {
+    const void* Q;
+    int64_t q_stride, T, q_heads;
+    KvPool pool;
+    const int32_t* prefix_table;
+    int64_t prefix;
+    const int32_t* table;
+    int64_t width;
+    const int32_t* q_start;
+    const int32_t* kv_len;
+    int64_t B;
+    float scale;
+    void* workspace;
+    void* out;
+};
+hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s);
+
 // Largest K (elements per row) the row-wise unfused kernels keep in registers.
 constexpr int64_t kMaxRowElemsBf16 = 16384;
 constexpr int64_t kMaxRowElemsF32 = 8192;

@@ -10,6 +10,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import math
 import os
 from typing import Optional
 
@@ -27,7 +28,12 @@ SYMBOLS = ("dn_status_string", "dn_version", "ln_linear_packed_bytes", "ln_linea
            "swiglu_packed_bytes", "swiglu_prepare", "rms_swiglu_deferred", "softmax_pv_deferred",
            "attention_deferred", "attention_gqa_deferred", "attention_decode_workspace_bytes",
            "attention_decode_deferred", "attention_decode_deferred_noalloc", "layernorm",
-           "rmsnorm", "silu_mul", "softmax", "gemm")
+           "rmsnorm", "silu_mul", "softmax", "gemm", "rotary_table", "rotary_apply", "kv_cache_bytes",
+           "kv_cache_describe", "kv_cache_append", "kv_cache_read", "attention_cache_workspace_bytes",
+           "attention_cache_deferred", "attention_shared_prefix_deferred")
+DN_KV_PAGE = 64
+DN_KV_LAYOUT_VERSION = 1
+KV_FORMATS = {"bf16": 1, "fp8": 2}  # DN_KV_BF16, DN_KV_FP8
 
 
 class DNError(RuntimeError):
@@ -40,6 +46,12 @@ class LnLinearWeights(ctypes.Structure):
     """Mirror of ``ln_linear_weights`` in dn.h."""
     _fields_ = [("K", ctypes.c_int64), ("N", ctypes.c_int64), ("dtype", ctypes.c_int32),
                 ("layout_version", ctypes.c_int32), ("packed", ctypes.c_void_p)]
+
+
+class KVCacheDesc(ctypes.Structure):
+    """Mirror of ``kv_cache`` in dn.h."""
+    _fields_ = [("pages", ctypes.c_int64), ("heads", ctypes.c_int64), ("d", ctypes.c_int64),
+                ("format", ctypes.c_int32), ("layout_version", ctypes.c_int32), ("data", ctypes.c_void_p)]
 
 
 def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
@@ -76,13 +88,25 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
     lib.rmsnorm.argtypes = [vp, vp, i64, i64, f32, i32, vp, vp]
     lib.softmax.argtypes = [vp, i64, i64, i64, i32, i32, vp, vp]
     lib.gemm.argtypes = [vp, vp, vp, i64, i64, i64, i64, i32, i32, i32, vp, vp]
+    kv, sz = ctypes.POINTER(KVCacheDesc), ctypes.c_size_t
+    lib.rotary_table.argtypes = [vp, i64, i64, ctypes.c_double, vp, vp]
+    lib.rotary_apply.argtypes = [vp, i64, vp, vp, i64, i64, i64, i64, i64, i32, i32, i32, vp, i64, vp]
+    lib.kv_cache_bytes.argtypes, lib.kv_cache_bytes.restype = [i64, i64, i64, i32], sz
+    lib.kv_cache_describe.argtypes = [vp, sz, i64, i64, i64, i32, kv]
+    lib.kv_cache_append.argtypes = [kv, vp, i64, vp, vp, vp, i64, i64, i32, i64, i64, i32, vp, vp]
+    lib.kv_cache_read.argtypes = [kv, vp, i64, i32, vp, vp, vp]
+    lib.attention_cache_workspace_bytes.argtypes, lib.attention_cache_workspace_bytes.restype = [i64] * 7, sz
+    lib.attention_cache_deferred.argtypes = [vp, i64, i64, i64, kv, vp, i64, vp, vp, i64, f32, i32, vp, sz, vp, vp]
+    lib.attention_shared_prefix_deferred.argtypes = [vp, i64, i64, i64, kv, vp, i64, vp, i64, vp, vp, i64, f32, i32, vp,
+                                                     sz, vp, vp]
     for f in ("ln_linear_prepare", "ln_linear_deferred", "rms_linear_deferred", "ln_linear_prepare_centered",
               "ln_linear_serial", "ln_linear_norm_on_load", "ln_linear_deferred_post",
               "rms_linear_deferred_post", "swiglu_prepare", "rms_swiglu_deferred", "softmax_pv_deferred",
               "attention_deferred", "attention_gqa_deferred", "attention_decode_deferred",
               "attention_decode_deferred_noalloc", "layernorm", "rmsnorm",
               "silu_mul", "softmax",
-              "gemm"):
+              "gemm", "rotary_table", "rotary_apply", "kv_cache_describe", "kv_cache_append", "kv_cache_read",
+              "attention_cache_deferred", "attention_shared_prefix_deferred"):
         getattr(lib, f).restype = i32
     return lib
 
@@ -523,3 +547,277 @@ def gemm(A: torch.Tensor, B, bias: Optional[torch.Tensor] = None, b_layout: int 
     _check("gemm", _lib.gemm(_dev(A3, "A"), bptr, _dev(bias, "bias"), batch, M, K, N, int(b_layout),
                              int(a_causal), _dt(A), _dev(out, "out"), _stream(stream)))
     return out[0] if squeeze else out
+
+
+# ------------------------------------------------------------------------------- rotary positions
+def rotary_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] = None, factor: float = 1.0,
+                       original: int = 8192, low: float = 1.0, high: float = 4.0, device="cuda"):
+    """(inv_freq, amplitude) for rotary_table: the rot / 2 frequencies base ** (-2 i / rot), fp64 on
+    the device, scaled for contexts ``factor`` times as long as the ``original`` tokens of training:
+
+    - None: as they are.
+    - "linear": every frequency divided by factor (positions interpolated).
+    - "base": the base raised to base * factor ** (rot / (rot - 2)), which divides the lowest
+      frequency by factor and leaves the highest.
+    - "parts": a frequency that turns fewer than ``low`` times over the original context is divided
+      by factor, one that turns more than ``high`` times is left, those between are blended linearly
+      in their number of turns.
+    - "parts_log": the same, blended linearly in the dimension (so in the logarithm of the number of
+      turns), and with the amplitude 0.1 ln(factor) + 1.
+    """
+    if rot < 2 or rot % 2 or not base > 0 or not factor > 0:
+        raise ValueError("rot must be even and positive, base and factor positive")
+    freq = float(base) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    amplitude = 1.0
+    if scaling == "linear":
+        freq = freq / factor
+    elif scaling == "base":
+        if rot < 4:
+            raise ValueError("scaling the base needs at least two frequencies")
+        freq = (float(base) * factor ** (rot / (rot - 2))) ** (-torch.arange(0, rot, 2, dtype=torch.float64) / rot)
+    elif scaling in ("parts", "parts_log"):
+        if not 0 < low < high:
+            raise ValueError("0 < low < high is needed")
+        turns = original * freq / (2.0 * math.pi)
+        if scaling == "parts":
+            keep = (turns - low) / (high - low)
+        else:
+            keep = torch.log(turns / low) / math.log(high / low)
+            amplitude = 0.1 * math.log(factor) + 1.0 if factor > 1.0 else 1.0
+        keep = keep.clamp(0.0, 1.0)
+        freq = keep * freq + (1.0 - keep) * freq / factor
+    elif scaling is not None:
+        raise ValueError(f"unknown scaling {scaling!r}")
+    return freq.to(device), amplitude
+
+
+def rotary_table(inv_freq: torch.Tensor, positions: int, amplitude: float = 1.0, stream=None) -> torch.Tensor:
+    """cos and sin of every position below ``positions``: [positions, rot / 2, 2] fp32."""
+    if inv_freq.dim() != 1:
+        raise ValueError(f"inv_freq has shape {list(inv_freq.shape)}, expected [rot / 2]")
+    _expect(inv_freq, "inv_freq", None, torch.float64)
+    half = inv_freq.shape[0]
+    table = torch.empty((max(int(positions), 0), half, 2), dtype=torch.float32, device=inv_freq.device)
+    _check("rotary_table", _lib.rotary_table(_dev(inv_freq, "inv_freq"), 2 * half, int(positions), float(amplitude),
+                                             _dev(table, "table") or None, _stream(stream)))
+    return table
+
+
+def _rows(t: torch.Tensor, name: str):
+    """Pointer and token stride of t[T, H, d] (or [T, width]) whose tokens' values lie together."""
+    if not t.is_cuda:
+        raise ValueError(f"{name} must be a GPU tensor")
+    st, n = t.stride(), 1
+    for k in range(t.dim() - 1, 0, -1):
+        if st[k] != n and t.shape[k] != 1:
+            raise ValueError(f"{name} must be contiguous within a token")
+        n *= t.shape[k]
+    return t.data_ptr(), (max(st[0], n) if t.shape[0] != 1 else n)
+
+
+def _int32(t: torch.Tensor, name: str, shape, x: torch.Tensor):
+    """Pointer of an int32 index tensor of this shape on x's device."""
+    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype == torch.int32 and t.is_contiguous()
+            and t.get_device() == x.get_device()):
+        _expect(t, name, shape, torch.int32, x.device)
+        if not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+    return t.data_ptr()
+
+
+def _table_of(table: torch.Tensor, x: torch.Tensor):
+    """Pointer, positions and turned dimensions of a rotary table."""
+    if not (isinstance(table, torch.Tensor) and table.dim() == 3 and table.shape[2] == 2 and
+            table.dtype == torch.float32 and table.get_device() == x.get_device()):
+        _expect(table, "table", (None, None, 2), torch.float32, x.device)
+    return _dev(table, "table"), table.shape[0], 2 * table.shape[1]
+
+
+def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False,
+                 inverse: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """x[T, H, d] turned by each token's position (tokens may be strided, as the query heads of QKV
+    rows are; out may be x).  inverse turns back: the gradient with respect to x of the turned x."""
+    if x.dim() != 3:
+        raise ValueError(f"x has shape {list(x.shape)}, expected [T, H, d]")
+    T, H, d = x.shape
+    xp, xs = _rows(x, "x")
+    tp, rows, rot = _table_of(table, x)
+    if out is None:
+        out = x.new_empty((T, H, d))
+    elif not _like(out, x.shape, x):
+        _expect(out, "out", (T, H, d), x.dtype, x.device)
+    op, os_ = _rows(out, "out")
+    _check("rotary_apply", _lib.rotary_apply(xp, xs, _int32(positions, "positions", (T,), x), tp, rows, T, H, d, rot,
+                                             int(interleaved), int(inverse), _dt(x), op, os_, _stream(stream)))
+    return out
+
+
+# ------------------------------------------------------------------------------- paged key/value cache
+@dataclasses.dataclass
+class KVCache:
+    """A paged key/value cache: the device buffer and its descriptor.  Slot s is token s % 64 of
+    page s // 64; which pages hold which sequence is the caller's."""
+    data: torch.Tensor
+    desc: KVCacheDesc
+
+    @property
+    def pages(self):
+        return self.desc.pages
+
+    @property
+    def heads(self):
+        return self.desc.heads
+
+    @property
+    def d(self):
+        return self.desc.d
+
+    @property
+    def format(self):
+        return {v: k for k, v in KV_FORMATS.items()}[self.desc.format]
+
+
+def kv_cache_bytes(pages: int, heads: int, d: int, fmt: str = "bf16") -> int:
+    return int(_lib.kv_cache_bytes(pages, heads, d, KV_FORMATS.get(fmt, 0)))
+
+
+def kv_cache_create(pages: int, heads: int, d: int, fmt: str = "bf16", device="cuda") -> KVCache:
+    """A cache of ``pages`` pages of 64 tokens; its memory needs no clearing."""
+    n = kv_cache_bytes(pages, heads, d, fmt)
+    if n == 0:
+        raise DNError("kv_cache_bytes", 1)
+    return kv_cache_wrap(torch.empty((pages, heads, n // (pages * heads)), dtype=torch.uint8, device=device), d, fmt)
+
+
+def kv_cache_wrap(data: torch.Tensor, d: int, fmt: str = "bf16") -> KVCache:
+    """The cache held by data[pages, heads, block bytes] (uint8)."""
+    if data.dim() != 3:
+        raise ValueError(f"data has shape {list(data.shape)}, expected [pages, heads, block bytes]")
+    pages, heads = data.shape[:2]
+    n = kv_cache_bytes(pages, heads, d, fmt)
+    if n == 0:
+        raise DNError("kv_cache_bytes", 1)
+    _expect(data, "data", (pages, heads, n // (pages * heads)), torch.uint8)
+    desc = KVCacheDesc()
+    _check("kv_cache_describe", _lib.kv_cache_describe(_dev(data, "data"), data.numel(), pages, heads, d,
+                                                       KV_FORMATS[fmt], ctypes.byref(desc)))
+    return KVCache(data, desc)
+
+
+def _check_cache(cache, x: torch.Tensor):
+    if not isinstance(cache, KVCache):
+        raise TypeError("cache must come from kv_cache_create / kv_cache_wrap")
+    if cache.data.get_device() != x.get_device():
+        raise ValueError(f"the cache is on {cache.data.device}, expected {x.device} (all tensors of a call share one device)")
+    return cache.desc
+
+
+def kv_cache_append(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, positions: Optional[torch.Tensor] = None,
+                    table: Optional[torch.Tensor] = None, interleaved: bool = False,
+                    q_out: Optional[torch.Tensor] = None, stream=None) -> Optional[torch.Tensor]:
+    """Puts the keys and values of qkv[T, (q_heads + 2 heads) d] into the cache at slots[T] (-1: not
+    written) and returns the queries [T, q_heads, d] (None where the rows hold none).  With a rotary
+    table the queries and keys are turned by positions[T]."""
+    desc = _check_cache(cache, qkv)
+    if qkv.dim() != 2:
+        raise ValueError(f"qkv has shape {list(qkv.shape)}, expected [T, (q_heads + 2 heads) d]")
+    T, width = qkv.shape
+    heads, d = desc.heads, desc.d
+    q_heads = width // d - 2 * heads
+    if width % d or q_heads < 0 or q_heads % heads:
+        raise ValueError(f"rows of {width} values do not hold a multiple of {heads} query heads and 2 x {heads} key and "
+                         f"value heads of {d}")
+    qp, qs = _rows(qkv, "qkv")
+    if q_heads == 0:
+        if q_out is not None:
+            raise ValueError("the rows hold no queries")
+    elif q_out is None:
+        q_out = qkv.new_empty((T, q_heads, d))
+    elif not _like(q_out, (T, q_heads, d), qkv):
+        _expect(q_out, "q_out", (T, q_heads, d), qkv.dtype, qkv.device)
+    tp, rows, rot, pp = None, 0, 0, None
+    if table is not None:
+        tp, rows, rot = _table_of(table, qkv)
+        pp = _int32(positions, "positions", (T,), qkv)
+    _check("kv_cache_append", _lib.kv_cache_append(
+        ctypes.byref(desc), qp, qs, _int32(slots, "slots", (T,), qkv), pp, tp, rows, rot, int(interleaved), T, q_heads,
+        _dt(qkv), _dev(q_out, "q_out"), _stream(stream)))
+    return q_out
+
+
+def kv_cache_read(cache: KVCache, slots: torch.Tensor, K: Optional[torch.Tensor] = None,
+                  V: Optional[torch.Tensor] = None, stream=None):
+    """(K, V) [T, heads, d] bf16 held at slots[T]; zeros for a slot outside the cache."""
+    desc = _check_cache(cache, slots)
+    if slots.dim() != 1:
+        raise ValueError(f"slots has shape {list(slots.shape)}, expected [T]")
+    shape = (slots.shape[0], desc.heads, desc.d)
+    for name, t in (("K", K), ("V", V)):
+        _expect(t, name, shape, torch.bfloat16, slots.device)
+    if K is None:
+        K = torch.empty(shape, dtype=torch.bfloat16, device=slots.device)
+    if V is None:
+        V = torch.empty(shape, dtype=torch.bfloat16, device=slots.device)
+    _check("kv_cache_read", _lib.kv_cache_read(
+        ctypes.byref(desc), _int32(slots, "slots", (shape[0],), slots), shape[0], DN_BF16, _dev(K, "K"), _dev(V, "V"),
+        _stream(stream)))
+    return K, V
+
+
+def attention_cache_workspace_bytes(T: int, B: int, q_heads: int, heads: int, d: int, table_width: int,
+                                    prefix_len: int = 0) -> int:
+    return int(_lib.attention_cache_workspace_bytes(T, B, q_heads, heads, d, table_width, prefix_len))
+
+
+def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out):
+    desc = _check_cache(cache, Q)
+    if Q.dim() != 3 or Q.shape[2] != desc.d or Q.shape[1] % desc.heads:
+        raise ValueError(f"Q has shape {list(Q.shape)}, expected [T, a multiple of {desc.heads}, {desc.d}]")
+    if block_table.dim() != 2:
+        raise ValueError(f"block_table has shape {list(block_table.shape)}, expected [B, pages]")
+    T, q_heads, d = Q.shape
+    B, width = block_table.shape
+    qp, qs = _rows(Q, "Q")
+    if out is None:
+        out = Q.new_empty((T, q_heads, d))
+    elif not _like(out, Q.shape, Q):
+        _expect(out, "out", (T, q_heads, d), Q.dtype, Q.device)
+    if workspace is None:
+        n = attention_cache_workspace_bytes(T, B, q_heads, desc.heads, d, width, prefix_len)
+        workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=Q.device)
+    elif workspace.dtype != torch.uint8 or workspace.get_device() != Q.get_device():
+        _expect(workspace, "workspace", None, torch.uint8, Q.device)
+    head = (qp, qs, T, q_heads, ctypes.byref(desc))
+    tail = (_int32(block_table, "block_table", (B, width), Q), width, _int32(q_start, "q_start", (B + 1,), Q),
+            _int32(kv_len, "kv_len", (B,), Q), B, d ** -0.5 if scale is None else float(scale), _dt(Q),
+            _dev(workspace, "workspace"), workspace.numel(), _dev(out, "out"))
+    return head, tail, out
+
+
+def attention_cache_deferred(Q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, q_start: torch.Tensor,
+                             kv_len: torch.Tensor, scale: Optional[float] = None,
+                             workspace: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                             stream=None) -> torch.Tensor:
+    """Attention of ragged sequences over the cache: rows q_start[b] .. q_start[b + 1] - 1 of
+    Q[T, q_heads, d] are sequence b's new tokens, the last of its kv_len[b] cached ones, which lie in
+    pages block_table[b]; each sees the keys up to its own.  scale defaults to 1/sqrt(d)."""
+    head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out)
+    _check("attention_cache_deferred", _lib.attention_cache_deferred(*head, *tail, _stream(stream)))
+    return out
+
+
+def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_table: torch.Tensor, prefix_len: int,
+                                     block_table: torch.Tensor, q_start: torch.Tensor, kv_len: torch.Tensor,
+                                     scale: Optional[float] = None, workspace: Optional[torch.Tensor] = None,
+                                     out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """attention_cache_deferred of sequences that share their first prefix_len tokens, in pages
+    prefix_table: read once for all of them.  kv_len counts each sequence's own tokens."""
+    prefix_len = int(prefix_len)
+    pages = (prefix_len + DN_KV_PAGE - 1) // DN_KV_PAGE
+    if prefix_table.dim() != 1 or prefix_table.shape[0] < pages:
+        raise ValueError(f"prefix_table has shape {list(prefix_table.shape)}, expected [at least {pages}]")
+    head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out)
+    pp = _int32(prefix_table, "prefix_table", tuple(prefix_table.shape), Q)
+    _check("attention_shared_prefix_deferred",
+           _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream(stream)))
+    return out
