@@ -60,85 +60,83 @@ __device__ __forceinline__ Seq sequence(const Args& a, int64_t b) {
 struct Item {
     int b, tile, chunk, head;
     int per;       // pages per chunk
-    int64_t slot;  // of this item, where its tile has several chunks
+    int slot;  // of this item, where its tile has several chunks
     Seq s;
 };
 
-// exclusive scan over the 256 threads of a workgroup; total in every thread
-__device__ __forceinline__ int64_t scan256(int64_t v, int64_t* lds, int64_t& total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    int64_t x = v;
-#pragma unroll
-    for (int o = 1; o < 64; o <<= 1) {
-        const int64_t y = __shfl_up(x, o);
-        if (lane >= o) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) lds[wave] = x;
-    __syncthreads();
-    int64_t before = 0;
-    total = 0;
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        const int64_t t = lds[w];
-        before += w < wave ? t : 0;
-        total += t;
-    }
-    return before + x - v;
+// inclusive scan over the wave, on the data-parallel lane moves (no LDS)
+template <int CTRL, int ROWS>
+__device__ __forceinline__ int lane_move(int v) {
+    return __builtin_amdgcn_update_dpp(0, v, CTRL, ROWS, 0xf, false);
+}
+__device__ __forceinline__ int wave_scan(int v) {
+    v += lane_move<0x111, 0xf>(v);  // row_shr:1
+    v += lane_move<0x112, 0xf>(v);  // row_shr:2
+    v += lane_move<0x114, 0xf>(v);  // row_shr:4
+    v += lane_move<0x118, 0xf>(v);  // row_shr:8
+    v += lane_move<0x142, 0xa>(v);  // row_bcast:15 into rows 1 and 3
+    v += lane_move<0x143, 0xc>(v);  // row_bcast:31 into rows 2 and 3
+    return v;
 }
 
 // Which item this workgroup takes: false where there is none left.  Sequences in order, of each its
 // tiles from the last (which sees the most keys) to the first, of each its chunks, of each the heads
-// (consecutive workgroups go to different XCDs: with 8 heads one XCD reads one head's keys).
+// (consecutive workgroups go to different XCDs: with 8 heads one XCD reads one head's keys).  Every
+// wave works it out for itself, 64 sequences at a time, one to a lane.
 __device__ __forceinline__ bool find_item(const Args& a, int rows, Item& it) {
-    __shared__ int64_t lds[4];
-    __shared__ Item found;
-    const int64_t id = blockIdx.x;
-    const int tid = threadIdx.x;
-    int64_t cost = 0, total;
+    const int id = blockIdx.x, lane = threadIdx.x & 63;
     Seq mine{};
-    for (int64_t b = tid; b < a.B; b += 256) {
+    int tiles = 0;
+    int64_t cost = 0;
+    for (int64_t b = lane; b < a.B; b += 64) {
         mine = sequence(a, b);
-        const int64_t tiles = ((int64_t)mine.n * a.group + rows - 1) / rows;
-        cost += tiles * mine.pages * a.heads;
+        tiles = (int)(((int64_t)mine.n * a.group + rows - 1) / rows);
+        cost += (int64_t)tiles * mine.pages;
     }
-    scan256(cost, lds, total);
-    const int64_t per = max(a.least, (total + a.target - 1) / a.target);
-    int64_t items_before = 0, slots_before = 0;
-    if (tid == 0) found.b = -1;
-    for (int64_t b0 = 0; b0 < a.B; b0 += 256) {
-        const int64_t b = b0 + tid;
-        int64_t items = 0, parts = 0, chunks = 1;
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) cost += __shfl_xor(cost, o);
+    const int per = (int)max(a.least, (cost * a.heads + a.target - 1) / a.target);
+    int items_before = 0, slots_before = 0;
+    for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
+        const int64_t b = b0 + lane;
+        int items = 0, parts = 0, chunks = 1;
         if (b < a.B) {
-            if (a.B > 256) mine = sequence(a, b);
-            const int64_t tiles = ((int64_t)mine.n * a.group + rows - 1) / rows;
-            chunks = max((int64_t)1, (mine.pages + per - 1) / per);
+            if (a.B > 64) {
+                mine = sequence(a, b);
+                tiles = (int)(((int64_t)mine.n * a.group + rows - 1) / rows);
+            }
+            chunks = max(1, (mine.pages + per - 1) / per);
             items = tiles * chunks * a.heads;
             parts = a.always_partial || chunks > 1 ? items : 0;
         }
-        int64_t items_total, parts_total;
-        const int64_t ib = items_before + scan256(items, lds, items_total);
-        const int64_t pb = slots_before + scan256(parts, lds, parts_total);
-        if (items > 0 && id >= ib && id < ib + items) {
-            const int64_t at = id - ib, rest = at / a.heads;
-            const int64_t tiles = items / (chunks * a.heads);
-            found.b = (int)b;
-            found.head = (int)(at - rest * a.heads);
-            found.chunk = (int)(rest % chunks);
-            found.tile = (int)(tiles - 1 - rest / chunks);
-            found.per = (int)per;
+        const int to = items_before + wave_scan(items), from = to - items;
+        const int slots_to = slots_before + wave_scan(parts);
+        const uint64_t here = __ballot(id >= from && id < to);
+        if (here) {
+            const int l = __builtin_ctzll(here);
+            const int at = id - __builtin_amdgcn_readlane(from, l), first = __builtin_amdgcn_readlane(slots_to - parts, l);
+            chunks = __builtin_amdgcn_readlane(chunks, l);
+            tiles = __builtin_amdgcn_readlane(tiles, l);
+            it.b = (int)b0 + l;
+            const int rest = at / a.heads;
+            it.head = at - rest * a.heads;
+            it.chunk = rest % chunks;
+            it.tile = tiles - 1 - rest / chunks;
+            it.per = per;
             // slots go by tile, chunk and head, whatever order the items have
-            found.slot = pb + ((int64_t)found.tile * chunks + found.chunk) * a.heads + found.head;
-            found.s = mine;
-            if (at == 0 && a.info) a.info[b] = int4{(int)pb, (int)per, (int)chunks, 0};
+            it.slot = first + (it.tile * chunks + it.chunk) * a.heads + it.head;
+            it.s.first = __builtin_amdgcn_readlane(mine.first, l);
+            it.s.n = __builtin_amdgcn_readlane(mine.n, l);
+            it.s.len = __builtin_amdgcn_readlane(mine.len, l);
+            it.s.pages = __builtin_amdgcn_readlane(mine.pages, l);
+            if (at == 0 && threadIdx.x == 0) a.info[it.b] = int4{first, per, chunks, 0};
+            return true;
         }
-        items_before += items_total;
-        slots_before += parts_total;
-        if (id < items_before) break;
+        items_before = __builtin_amdgcn_readlane(to, 63);
+        slots_before = __builtin_amdgcn_readlane(slots_to, 63);
+        if (id < items_before) return false;  // counts past 31 bits (q_start out of order)
     }
-    __syncthreads();
-    it = found;
-    return it.b >= 0;
+    return false;
 }
 
 // Keys that some query of the tile sees.
@@ -149,6 +147,13 @@ __device__ __forceinline__ int tile_keys(const Args& a, const Seq& s, int tile, 
 }
 __device__ __forceinline__ int tile_chunks(int keys, int per) {
     return max(1, ((keys + kKvPage - 1) / kKvPage + per - 1) / per);
+}
+
+// The pages of one of a tile's chunks, which are as equal as they can be.
+__device__ __forceinline__ void chunk_pages(int keys, int chunks, int chunk, int& lo, int& hi) {
+    const int pages = (keys + kKvPage - 1) / kKvPage, each = pages / chunks, more = pages - each * chunks;
+    lo = chunk * each + min(chunk, more);
+    hi = lo + each + (chunk < more ? 1 : 0);
 }
 
 // The table's page, kept inside the pool whatever the table holds.
@@ -186,57 +191,67 @@ __device__ __forceinline__ u32x4 keep_tokens(u32x4 c, int keep) {
     return u32x4{w[0], w[1], w[2], w[3]};
 }
 
-__device__ __forceinline__ float weight(float m, float mn) {
-    return m != -__builtin_inff() ? __builtin_amdgcn_exp2f(m - mn) : 0.f;
-}
+// Partial sums relative to m, brought to a larger reference.  A reference is never -inf (kLowest, no
+// key yet), so no difference of two infinities arises but where a score is +inf: NaN, as it should be.
+constexpr float kLowest = -3.402823466e38f;
+__device__ __forceinline__ float weight(float m, float mn) { return __builtin_amdgcn_exp2f(m - mn); }
 
-// Softmax state of one 16-query block: the reference maximum, raised only when a unit exceeds it by
-// more than 2^8 (numerators stay below 256), and the lane's share of the sum.
+// Softmax state of one 16-query block: the reference maximum, raised only when a score exceeds it by
+// more than 8 (numerators stay below 2^8), and the lane's share of the sum.
 struct State {
     float m, l;
 };
 
-// Scores of TILES key tiles (16 each, of one unit) -> numerators as operands.  s holds q . K; ks, vs
-// the lane's scales of each tile's four keys; lim: the last unit key that this lane's query sees.
+// Scores of TILES key tiles (16 each, of one unit) -> numerators as operands.  s holds q . K; kk the
+// lane's K scales (of each tile's four keys) times scale log2(e), vs its V scales; lim: the last key
+// that this lane's query sees.
 template <int TILES, int D, bool MASK>
-__device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const float4 (&ks)[TILES], const float4 (&vs)[TILES],
-                                             const int (&key0)[TILES], int lim, float sl2, State& st, f32x4 (&acc)[D / 16],
+__device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x4 (&kk)[TILES], const f32x4 (&vs)[TILES],
+                                             const int (&key0)[TILES], int lim, State& st, f32x4 (&acc)[D / 16],
                                              u32x4 (&pf)[TILES / 2]) {
-    float x[TILES][4];
+    f32x4 x[TILES];
     float top = -__builtin_inff();
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-        const float k4[4] = {ks[t].x, ks[t].y, ks[t].z, ks[t].w};
+    for (int t = 0; t < TILES; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            x[t][i] = s[t][i] * (k4[i] * sl2);
+            x[t][i] = __builtin_fmaf(s[t][i], kk[t][i], -st.m);
             if (MASK) x[t][i] = key0[t] + i <= lim ? x[t][i] : -__builtin_inff();
             top = fmaxf(top, x[t][i]);
         }
-    }
-    top = max_lane_groups(top);
-    if (__any(top > st.m + 8.f)) {
-        const float mn = fmaxf(top, st.m), w = weight(st.m, mn);
+    if (__any(top > 8.f)) {
+        float high = kLowest;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                x[t][i] = s[t][i] * kk[t][i];
+                if (MASK) x[t][i] = key0[t] + i <= lim ? x[t][i] : -__builtin_inff();
+                high = fmaxf(high, x[t][i]);
+            }
+        const float mn = fmaxf(max_lane_groups(high), st.m), w = weight(st.m, mn);
         st.m = mn;
         st.l *= w;
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) acc[n] *= w;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[t][i] -= mn;
     }
-    const float m = st.m == -__builtin_inff() ? 0.f : st.m;
 #pragma unroll
     for (int t = 0; t < TILES; t += 2) {
         float p[8];
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const float v4[4] = {vs[t + h].x, vs[t + h].y, vs[t + h].z, vs[t + h].w};
+        for (int h = 0; h < 2; ++h)
 #pragma unroll
             for (int i = 0; i < 4; ++i) {
-                const float e = __builtin_amdgcn_exp2f(x[t + h][i] - m);
+                const float e = __builtin_amdgcn_exp2f(x[t + h][i]);
+                // a masked key's scale may be anything: its numerator is 0 whatever it holds
                 const bool on = !MASK || key0[t + h] + i <= lim;
                 st.l += on ? e : 0.f;
-                p[4 * h + i] = on ? e * v4[i] : 0.f;
+                p[4 * h + i] = on ? e * vs[t + h][i] : 0.f;
             }
-        }
         pf[t / 2] = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
     }
 }
@@ -262,7 +277,7 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
     const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
     if (it.chunk >= chunks) return;
     const bool partial = a.always_partial || chunks > 1;
-    if (partial && it.slot >= a.slots) return;
+    if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
 
     // this lane's query
     const int64_t row = (int64_t)it.tile * R + q;
@@ -282,9 +297,10 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
     f32x4 acc[NB];
 #pragma unroll
     for (int n = 0; n < NB; ++n) acc[n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    State st{-__builtin_inff(), 0.f};
+    State st{kLowest, 0.f};
 
-    const int page_lo = it.chunk * it.per, page_hi = min(page_lo + it.per, (keys + kKvPage - 1) / kKvPage);
+    int page_lo, page_hi;
+    chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
     const int count = page_hi - page_lo > wave ? (page_hi - page_lo - wave + 3) / 4 : 0;  // pages of this wave
     const int64_t page_bytes = (int64_t)a.heads * B::SIZE;
     const char* head_base = a.pool + (int64_t)it.head * B::SIZE;
@@ -304,13 +320,13 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
     }
     for (int un = 0; un < total; ++un) {
         const int u = un % UNITS, page = page_lo + wave + 4 * (un / UNITS);
-        float4 ks[TILES], vs[TILES];
+        f32x4 kk[TILES], vs[TILES];
         int key0[TILES];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const int o = 4 * E * u + E * G + 4 * t;
-            ks[t] = *reinterpret_cast<const float4*>(block + B::KS + 4 * o);
-            vs[t] = *reinterpret_cast<const float4*>(block + B::VS + 4 * o);
+            kk[t] = *reinterpret_cast<const f32x4*>(block + B::KS + 4 * o);
+            vs[t] = *reinterpret_cast<const f32x4*>(block + B::VS + 4 * o);
             key0[t] = page * kKvPage + o;
         }
 #pragma unroll
@@ -331,17 +347,19 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) kf[i] = ld16_stream(block + (nu * LOADS + i) * kChunkBytes + lane * 16);
         }
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) kk[t] *= a.sl2;
         u32x4 pf[TILES / 2];
         const int end = page * kKvPage + 4 * E * (u + 1);  // first key past the unit
         if (end - 1 > lim_min) {
-            softmax_unit<TILES, D, true>(s, ks, vs, key0, lim, a.sl2, st, acc, pf);
+            softmax_unit<TILES, D, true>(s, kk, vs, key0, lim, st, acc, pf);
             if (end > it.s.len) {
                 const int keep = min(max(it.s.len - (page * kKvPage + 4 * E * u + E * G), 0), E);
 #pragma unroll
                 for (int i = 0; i < LOADS; ++i) vf[i] = keep_tokens<FMT>(vf[i], keep);
             }
         } else {
-            softmax_unit<TILES, D, false>(s, ks, vs, key0, lim, a.sl2, st, acc, pf);
+            softmax_unit<TILES, D, false>(s, kk, vs, key0, lim, st, acc, pf);
         }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -361,7 +379,7 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
     constexpr int PER = 8;  // outputs of a thread at a time
     for (int i = threadIdx.x; i < rows_here * (D / PER); i += 256) {
         const int r = i / (D / PER), x = i % (D / PER) * PER;
-        float m = -__builtin_inff(), w[4], lt = 0.f, o[PER];
+        float m = kLowest, w[4], lt = 0.f, o[PER];
 #pragma unroll
         for (int v = 0; v < 4; ++v) m = fmaxf(m, ml[v][0][r]);
 #pragma unroll
@@ -375,7 +393,7 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
         }
         const int64_t ro = (int64_t)it.tile * R + r;
         if (partial) {
-            float* part = a.parts + (it.slot * R + r) * (int64_t)(D + 4);
+            float* part = a.parts + ((int64_t)it.slot * R + r) * (int64_t)(D + 4);
             *reinterpret_cast<f32x4*>(part + x) = f32x4{o[0], o[1], o[2], o[3]};
             *reinterpret_cast<f32x4*>(part + x + 4) = f32x4{o[4], o[5], o[6], o[7]};
             if (x == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{lt, m, 0.f, 0.f};
@@ -393,16 +411,19 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 }
 
 // ----------------------------------------------------------------------------- many rows
-// Tiles of 4 waves x QW x 16 rows.  Bound by the matrix cores: a page's codes go through LDS (two
-// slots, copied while the page before is worked on) and serve the tile's four waves.
+// Tiles of 4 waves x QW x 16 rows.  Bound by the matrix cores and the exponentials beside them: a
+// page goes through LDS as bf16 operands (two slots, the next one filled while a page is worked on)
+// and serves the tile's four waves.  bf16 codes are copied there directly; e4m3 codes go through
+// registers and are widened once for all waves.
 template <int FMT, int D, int QW>
 __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     using B = KvBlock<FMT, D>;
-    constexpr int E = B::E, R = 64 * QW, TILES = 4, KC = D / (4 * E), NB = D / 16;
-    constexpr int CHUNKS = 2 * B::PART / kChunkBytes;           // K and V codes
-    constexpr int SLOT = 2 * B::PART + 8 * kKvPage;             // and the scales
-    __shared__ __attribute__((aligned(1024))) char smem[2 * ((SLOT + 1023) / 1024 * 1024)];
-    constexpr int STEP = (SLOT + 1023) / 1024 * 1024;
+    constexpr int E = B::E, J = E / 8, R = 64 * QW, TILES = 4, KC = D / (4 * E), NB = D / 16;
+    constexpr int FRAGS = 2 * kKvPage * D * 2 / kChunkBytes;  // operands of a page, 1 KiB each: K's, then V's
+    constexpr int CHUNKS = FRAGS / J;                         // of 1 KiB in the cache
+    constexpr int SCALES = FRAGS * kChunkBytes;               // then K's and V's scales
+    constexpr int STEP = SCALES + 8 * kKvPage;
+    __shared__ __attribute__((aligned(1024))) char smem[2 * STEP];
 
     Item it;
     if (!find_item(a, R, it)) return;
@@ -411,7 +432,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
     if (it.chunk >= chunks) return;
     const bool partial = a.always_partial || chunks > 1;
-    if (partial && it.slot >= a.slots) return;
+    if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
 
     const int64_t rows_all = (int64_t)it.s.n * a.group;
     const int64_t row0 = (int64_t)it.tile * R + wave * QW * 16;  // the wave's first row
@@ -436,32 +457,52 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     for (int f = 0; f < QW; ++f) {
 #pragma unroll
         for (int n = 0; n < NB; ++n) acc[f][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-        st[f] = State{-__builtin_inff(), 0.f};
+        st[f] = State{kLowest, 0.f};
     }
 
-    const int page_lo = it.chunk * it.per, page_hi = min(page_lo + it.per, (keys + kKvPage - 1) / kKvPage);
+    int page_lo, page_hi;
+    chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
     const int count = page_hi - page_lo;
     const int64_t page_bytes = (int64_t)a.heads * B::SIZE;
     const char* head_base = a.pool + (int64_t)it.head * B::SIZE;
     const uint32_t lds0 = lds_addr32(smem);
     int ids = 0;
-    auto issue = [&](int k) __attribute__((always_inline)) {
+    u32x4 raw[CHUNKS / 4];
+    auto fetch = [&](int k) __attribute__((always_inline)) {
         if (k % 64 == 0) ids = k + lane < count ? page_at(a, it.b, page_lo + k + lane) : 0;
-        const uint64_t src = uniform_u64(head_base + (int64_t)__builtin_amdgcn_readlane(ids, k % 64) * page_bytes);
+        const char* block = head_base + (int64_t)__builtin_amdgcn_readlane(ids, k % 64) * page_bytes;
+        const uint64_t src = uniform_u64(block);
         const uint32_t dst = lds0 + (uint32_t)(k & 1) * STEP;
 #pragma unroll
         for (int i = 0; i < CHUNKS / 4; ++i) {
             const uint32_t at = (uint32_t)(wave + 4 * i) * kChunkBytes;
-            g2lds16_async_sb(src, at + lane * 16, dst + at);
+            if constexpr (J == 1)
+                g2lds16_async_sb(src, at + lane * 16, dst + at);
+            else
+                raw[i] = ld16(block + at + lane * 16);
         }
         // the scales: half a KiB, the first 32 lanes of one wave
-        if (wave == 0 && lane < 32) g2lds16_async_sb(src, (uint32_t)B::KS + lane * 16, dst + (uint32_t)B::KS);
+        if (wave == 0 && lane < 32) g2lds16_async_sb(src, (uint32_t)B::KS + lane * 16, dst + (uint32_t)SCALES);
     };
-    if (count > 0) issue(0);
-    for (int k = 0; k < count; ++k) {
+    auto land = [&](int k) __attribute__((always_inline)) {
+        if constexpr (J > 1) {
+            char* slot = smem + (k & 1) * STEP;
+#pragma unroll
+            for (int i = 0; i < CHUNKS / 4; ++i)
+#pragma unroll
+                for (int j = 0; j < J; ++j)
+                    *reinterpret_cast<u32x4*>(slot + ((wave + 4 * i) * J + j) * kChunkBytes + lane * 16) =
+                        frag<FMT>(raw[i], j);
+        }
         wait_vm();
-        __syncthreads();  // page k has landed, and every wave is done with page k - 1
-        if (k + 1 < count) issue(k + 1);
+        __syncthreads();
+    };
+    if (count > 0) {
+        fetch(0);
+        land(0);
+    }
+    for (int k = 0; k < count; ++k) {
+        if (k + 1 < count) fetch(k + 1);
         const char* slot = smem + (k & 1) * STEP;
         const int base = (page_lo + k) * kKvPage;
         f32x4 s[QW][TILES];
@@ -470,23 +511,19 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
 #pragma unroll
             for (int f = 0; f < QW; ++f) s[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < KC; ++c) {
-                const u32x4 kf = lds_ld16(lds_ptr((char*)slot + (t * KC + c) * kChunkBytes + lane * 16));
+            for (int c = 0; c < KC * J; ++c) {
+                const u32x4 kf = lds_ld16(lds_ptr((char*)slot + (t * KC * J + c) * kChunkBytes + lane * 16));
 #pragma unroll
-                for (int j = 0; j < E / 8; ++j) {
-                    const u32x4 b = frag<FMT>(kf, j);
-#pragma unroll
-                    for (int f = 0; f < QW; ++f) s[f][t] = mfma_chunk<__bf16>(b, qf[f][c * (E / 8) + j], s[f][t]);
-                }
+                for (int f = 0; f < QW; ++f) s[f][t] = mfma_chunk<__bf16>(kf, qf[f][c], s[f][t]);
             }
         }
-        float4 ks[TILES], vs[TILES];
+        f32x4 kk[TILES], vs[TILES];
         int key0[TILES];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const int o = t * 4 / E * 4 * E + E * G + t * 4 % E;  // tile t's first token of lane group G
-            ks[t] = *reinterpret_cast<const float4*>(slot + B::KS + 4 * o);
-            vs[t] = *reinterpret_cast<const float4*>(slot + B::VS + 4 * o);
+            kk[t] = *reinterpret_cast<const f32x4*>(slot + SCALES + 4 * o) * a.sl2;
+            vs[t] = *reinterpret_cast<const f32x4*>(slot + SCALES + 4 * kKvPage + 4 * o);
             key0[t] = base + o;
         }
         u32x4 pf[QW][TILES / 2];
@@ -494,26 +531,24 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
 #pragma unroll
         for (int f = 0; f < QW; ++f) {
             if (masked)
-                softmax_unit<TILES, D, true>(s[f], ks, vs, key0, lim[f], a.sl2, st[f], acc[f], pf[f]);
+                softmax_unit<TILES, D, true>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
             else
-                softmax_unit<TILES, D, false>(s[f], ks, vs, key0, lim[f], a.sl2, st[f], acc[f], pf[f]);
+                softmax_unit<TILES, D, false>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
         }
         const bool cut = base + kKvPage > it.s.len;
 #pragma unroll
-        for (int u = 0; u < kKvPage / (4 * E); ++u) {
-            const int keep = min(max(it.s.len - (base + 4 * E * u + E * G), 0), E);
+        for (int u = 0; u < kKvPage / (4 * E); ++u)
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                u32x4 vf = lds_ld16(lds_ptr((char*)slot + B::PART + (u * NB + n) * kChunkBytes + lane * 16));
-                if (cut) vf = keep_tokens<FMT>(vf, keep);
+            for (int n = 0; n < NB; ++n)
 #pragma unroll
-                for (int j = 0; j < E / 8; ++j) {
-                    const u32x4 b = frag<FMT>(vf, j);
+                for (int j = 0; j < J; ++j) {
+                    u32x4 vf = lds_ld16(
+                        lds_ptr((char*)slot + (FRAGS / 2 + (u * NB + n) * J + j) * kChunkBytes + lane * 16));
+                    if (cut) vf = keep_tokens<kKvBf16>(vf, it.s.len - (base + 4 * E * u + E * G + 8 * j));
 #pragma unroll
-                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(b, pf[f][u * (E / 8) + j], acc[f][n]);
+                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(vf, pf[f][u * J + j], acc[f][n]);
                 }
-            }
-        }
+        if (k + 1 < count) land(k + 1);  // page k + 1 has landed, and every wave is done with page k
     }
 
 #pragma unroll
@@ -522,7 +557,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
         const float l = sum_lane_groups(st[f].l);
         if (row >= rows_all) continue;
         if (partial) {
-            float* part = a.parts + (it.slot * R + (row - (int64_t)it.tile * R)) * (int64_t)(D + 4);
+            float* part = a.parts + ((int64_t)it.slot * R + (row - (int64_t)it.tile * R)) * (int64_t)(D + 4);
 #pragma unroll
             for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(part + 16 * n + 4 * G) = acc[f][n];
             if (G == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{l, st[f].m, 0.f, 0.f};
@@ -557,83 +592,88 @@ __device__ __forceinline__ int parts_of(const Set& set, const int4& plan, int ti
     return first >= 0 && first + (int64_t)(chunks - 1) * heads < set.slots ? chunks : 0;
 }
 
-// One output row per workgroup: D / 4 threads over its dimensions, the others over its partial sums.
-// `shared` (parts null: none) holds the partial sums over the prefix, `own` those over the
-// sequence's own keys; without a prefix rows whose tile has one chunk are already written.
-template <int D>
+// Output rows (token, query head): D / 4 threads over a row's dimensions, NS such groups over its
+// partial sums, the other threads over rows.  `shared` (parts null: none) holds the partial sums over
+// the prefix, `own` those over the sequence's own keys; without a prefix rows whose tile has one
+// chunk are already written.
+template <int D, int NS>
 __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own, const Set shared) {
-    constexpr int NX = D / 4, NS = 256 / NX;
-    __shared__ int found;
-    __shared__ __attribute__((aligned(16))) float red[NS][D + 4];
-    __shared__ float red_m[NS];
-    const int tid = threadIdx.x;
-    const int hq = blockIdx.x % (a.heads * a.group);
-    const int64_t token = blockIdx.x / (a.heads * a.group);
-    if (tid == 0) found = -1;
+    constexpr int NX = D / 4, ROWS = 256 / (NX * NS);
+    __shared__ int found[ROWS];
+    __shared__ __attribute__((aligned(16))) float red[ROWS][NS][D + 4];
+    const int tid = threadIdx.x, heads = a.heads * a.group;
+    const int in = tid / (NX * NS), g = tid / NX % NS, x = tid % NX * 4;
+    const int64_t row_id = (int64_t)blockIdx.x * ROWS + in, token = row_id / heads;
+    const bool is_row = token < a.T;
+    if (tid < ROWS) found[tid] = -1;
     __syncthreads();
-    for (int64_t b = tid; b < a.B; b += 256)
-        if (a.q_start[b] <= token && token < a.q_start[b + 1]) found = (int)b;
+    if (is_row)
+        for (int64_t b = tid % (NX * NS); b < a.B; b += NX * NS)
+            if (a.q_start[b] <= token && token < a.q_start[b + 1]) found[in] = (int)b;
     __syncthreads();
-    const int b = found;
-    if (b < 0) return;
-    const Seq s = sequence(a, b);
-    const int h = hq / a.group, r = hq % a.group;
-    int64_t first[2] = {0, 0};
-    int count[2] = {0, 0}, at[2] = {0, 0}, lim_keys;
-    const float* base[2] = {own.parts, shared.parts};
-    {
-        const int4 info = own.info[b];
-        const int64_t row = (token - s.first) * a.group + r;
-        const int tile = (int)(row / own.rows);
-        const int chunks = tile_chunks(tile_keys(a, s, tile, own.rows), max(info.y, 1));
-        lim_keys = s.len - s.n + (int)(token - s.first) + 1;
-        if (!shared.parts && chunks == 1) return;
-        at[0] = (int)(row % own.rows);
-        count[0] = parts_of(own, info, tile, chunks, a.heads, h, first[0]);
-    }
-    if (shared.parts) {
-        const int4 info = shared.info[0];
-        const int64_t row = token * a.group + r;
-        const int tile = (int)(row / shared.rows);
-        at[1] = (int)(row % shared.rows);
-        count[1] = parts_of(shared, info, tile, info.z, a.heads, h, first[1]);
-    }
-    const int x = tid % NX * 4, g = tid / NX;
-    float m = -__builtin_inff(), l = 0.f;
+    const int b = found[in];
+    bool write = is_row && b >= 0;
+    const int hq = (int)(row_id - token * heads), h = hq / a.group, r = hq % a.group;
+    const Set* sets[2] = {&own, &shared};
+    float m = kLowest, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    bool none = false;
+    if (write) {
+        const Seq s = sequence(a, b);
+        none = !shared.parts && s.len - s.n + (int)(token - s.first) < 0;  // no key at all: zero
 #pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        const int rows = w ? shared.rows : own.rows;
-        for (int c = g; c < count[w]; c += NS) {
-            const float* part = base[w] + ((first[w] + (int64_t)c * a.heads) * rows + at[w]) * (int64_t)(D + 4);
-            const f32x4 v = *reinterpret_cast<const f32x4*>(part + x), t = *reinterpret_cast<const f32x4*>(part + D);
-            const float mn = fmaxf(m, t[1]), wo = weight(m, mn), wn = weight(t[1], mn);
-            l = wo * l + wn * t[0];
-            o = o * wo + v * wn;
+        for (int w = 0; w < 2; ++w) {
+            const Set& set = *sets[w];
+            if (!set.parts) continue;
+            const int4 plan = set.info[w ? 0 : b];
+            const int64_t row = (w ? token : token - s.first) * a.group + r;
+            const int tile = (int)(row / set.rows);
+            const int chunks = w ? plan.z : tile_chunks(tile_keys(a, s, tile, set.rows), max(plan.y, 1));
+            if (!shared.parts && chunks == 1) write = false;
+            int64_t first;
+            const int count = write ? parts_of(set, plan, tile, chunks, a.heads, h, first) : 0;
+            for (int c = g; c < count; c += NS) {
+                const float* part = set.parts + ((first + (int64_t)c * a.heads) * set.rows + row % set.rows) * (D + 4);
+                const f32x4 v = *reinterpret_cast<const f32x4*>(part + x), t = *reinterpret_cast<const f32x4*>(part + D);
+                const float mn = fmaxf(m, t[1]), wo = weight(m, mn), wn = weight(t[1], mn);
+                l = wo * l + wn * t[0];
+                o = o * wo + v * wn;
+                m = mn;
+            }
+        }
+    }
+    if constexpr (NS > 1) {
+        *reinterpret_cast<f32x4*>(&red[in][g][x]) = o;
+        if (x == 0) {
+            red[in][g][D] = l;
+            red[in][g][D + 1] = m;
+        }
+        __syncthreads();
+        if (g) return;
+#pragma unroll
+        for (int v = 1; v < NS; ++v) {
+            const float mv = red[in][v][D + 1], mn = fmaxf(m, mv), wo = weight(m, mn), wn = weight(mv, mn);
+            l = wo * l + wn * red[in][v][D];
+            o = o * wo + *reinterpret_cast<const f32x4*>(&red[in][v][x]) * wn;
             m = mn;
         }
     }
-    *reinterpret_cast<f32x4*>(&red[g][x]) = o;
-    if (x == 0) {
-        red[g][D] = l;
-        red_m[g] = m;
-    }
-    __syncthreads();
-    if (g) return;
-    float mt = -__builtin_inff(), lt = 0.f;
-#pragma unroll
-    for (int v = 0; v < NS; ++v) mt = fmaxf(mt, red_m[v]);
-    f32x4 ot = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-    for (int v = 0; v < NS; ++v) {
-        const float w = weight(red_m[v], mt);
-        lt += w * red[v][D];
-        ot += *reinterpret_cast<const f32x4*>(&red[v][x]) * w;
-    }
-    const bool none = !shared.parts && lim_keys <= 0;
-    const float inv = 1.0f / lt;
-    const uint2 v = {pack_bf16(ot[0] * inv, ot[1] * inv), pack_bf16(ot[2] * inv, ot[3] * inv)};
-    *reinterpret_cast<uint2*>(a.out + (token * a.heads * a.group + hq) * D + x) = none ? uint2{0, 0} : v;
+    if (!write) return;
+    const float inv = 1.0f / l;
+    const uint2 v = {pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
+    *reinterpret_cast<uint2*>(a.out + row_id * D + x) = none ? uint2{0, 0} : v;
+}
+
+template <int D>
+hipError_t launch_merge(const Args& a, const Set& own, const Set& shared, hipStream_t s) {
+    // a workgroup to each row until the rows fill the chip
+    const int64_t rows = a.T * a.heads * a.group;
+    constexpr int MOST = 256 / (D / 4);
+    if (rows <= 2048)
+        merge_kernel<D, MOST><<<dim3((unsigned)rows), 256, 0, s>>>(a, own, shared);
+    else
+        merge_kernel<D, 1><<<dim3((unsigned)((rows + MOST - 1) / MOST)), 256, 0, s>>>(a, own, shared);
+    return hipGetLastError();
 }
 
 template <int FMT, int D>
@@ -700,12 +740,7 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
     const hipError_t e = ca::launch_any(c.pool, own, w.own.rows, w.own.grid, s);
     if (e != hipSuccess || (w.own.slots == 0 && prefix_pages == 0)) return e;
     const ca::Set set{own.info, own.parts, own.slots, w.own.rows};
-    const dim3 g((unsigned)(c.T * c.q_heads));
-    if (c.pool.d == 64)
-        ca::merge_kernel<64><<<g, 256, 0, s>>>(own, set, shared);
-    else
-        ca::merge_kernel<128><<<g, 256, 0, s>>>(own, set, shared);
-    return hipGetLastError();
+    return c.pool.d == 64 ? ca::launch_merge<64>(own, set, shared, s) : ca::launch_merge<128>(own, set, shared, s);
 }
 
 }  // namespace dn
