@@ -12,6 +12,8 @@
 // their own: query i of n sees keys 0 .. kv_len - n + i.  A masked key weighs exactly 0 whatever
 // its slot holds: its numerator is selected away, and V codes past kv_len are zeroed before the
 // product (codes below are finite: rows with NaN or infinities are held as a NaN scale).
+#include <type_traits>
+
 #include "dn_device.hpp"
 #include "dn_launch.hpp"
 #include "kv_layout.hpp"
@@ -318,7 +320,8 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 #pragma unroll
         for (int i = 0; i < LOADS; ++i) kf[i] = ld16_stream(block + i * kChunkBytes + lane * 16);
     }
-    for (int un = 0; un < total; ++un) {
+    auto step = [&](int un, auto tag) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(tag)::value;
         const int u = un % UNITS, page = page_lo + wave + 4 * (un / UNITS);
         f32x4 kk[TILES], vs[TILES];
         int key0[TILES];
@@ -350,22 +353,22 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 #pragma unroll
         for (int t = 0; t < TILES; ++t) kk[t] *= a.sl2;
         u32x4 pf[TILES / 2];
-        const int end = page * kKvPage + 4 * E * (u + 1);  // first key past the unit
-        if (end - 1 > lim_min) {
-            softmax_unit<TILES, D, true>(s, kk, vs, key0, lim, st, acc, pf);
-            if (end > it.s.len) {
-                const int keep = min(max(it.s.len - (page * kKvPage + 4 * E * u + E * G), 0), E);
+        softmax_unit<TILES, D, MASK>(s, kk, vs, key0, lim, st, acc, pf);
+        if (MASK) {
+            const int keep = it.s.len - (page * kKvPage + 4 * E * u + E * G);
 #pragma unroll
-                for (int i = 0; i < LOADS; ++i) vf[i] = keep_tokens<FMT>(vf[i], keep);
-            }
-        } else {
-            softmax_unit<TILES, D, false>(s, kk, vs, key0, lim, st, acc, pf);
+            for (int i = 0; i < LOADS; ++i) vf[i] = keep_tokens<FMT>(vf[i], keep);
         }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
             for (int j = 0; j < E / 8; ++j) acc[n] = mfma_chunk<__bf16>(frag<FMT>(vf[n], j), pf[j], acc[n]);
-    }
+    };
+    // pages that every query of the tile sees whole, then those that a mask cuts
+    const int whole_pages = (lim_min + 1) / kKvPage - page_lo;
+    const int whole = min(whole_pages > wave ? (whole_pages - wave + 3) / 4 : 0, count) * UNITS;
+    for (int un = 0; un < whole; ++un) step(un, std::false_type{});
+    for (int un = whole; un < total; ++un) step(un, std::true_type{});
 
     // the four waves' sums
     const float l = sum_lane_groups(st.l);
@@ -437,7 +440,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     const int64_t rows_all = (int64_t)it.s.n * a.group;
     const int64_t row0 = (int64_t)it.tile * R + wave * QW * 16;  // the wave's first row
     u32x4 qf[QW][D / 32];
-    int lim[QW], lim_min;
+    int lim[QW];
 #pragma unroll
     for (int f = 0; f < QW; ++f) {
         const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
@@ -449,7 +452,6 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
             for (int j = 0; j < E / 8; ++j) qf[f][c * (E / 8) + j] = ld16(qp + 4 * E * c + E * G + 8 * j);
         lim[f] = a.kv_len ? it.s.len - it.s.n + qi : it.s.len - 1;
     }
-    lim_min = a.kv_len ? it.s.len - it.s.n + (int)(min(row0, rows_all - 1) / a.group) : it.s.len - 1;
 
     f32x4 acc[QW][NB];
     State st[QW];
@@ -501,24 +503,31 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
         fetch(0);
         land(0);
     }
-    for (int k = 0; k < count; ++k) {
-        if (k + 1 < count) fetch(k + 1);
+    // Operands are read from LDS one group of products ahead, in an order fixed by scheduling groups.
+    auto read = [&](const char* slot, int first, u32x4(&fr)[KC * J]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < KC * J; ++c) fr[c] = lds_ld16(lds_ptr((char*)slot + (first + c) * kChunkBytes + lane * 16));
+    };
+    constexpr int G4 = KC * J, VG = FRAGS / 2 / G4;  // operands of a group; groups of V
+    auto step = [&](int k, auto tag) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(tag)::value;
         const char* slot = smem + (k & 1) * STEP;
         const int base = (page_lo + k) * kKvPage;
-        f32x4 s[QW][TILES];
+        f32x4 s[QW][TILES], kk[TILES], vs[TILES];
+        int key0[TILES];
+        u32x4 fr[2][G4];
+        read(slot, 0, fr[0]);
+        if (k + 1 < count) fetch(k + 1);
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
+            read(slot, (t + 1) * G4, fr[(t + 1) & 1]);  // after the last tile of K: V's first group
 #pragma unroll
             for (int f = 0; f < QW; ++f) s[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < KC * J; ++c) {
-                const u32x4 kf = lds_ld16(lds_ptr((char*)slot + (t * KC * J + c) * kChunkBytes + lane * 16));
+            for (int c = 0; c < G4; ++c)
 #pragma unroll
-                for (int f = 0; f < QW; ++f) s[f][t] = mfma_chunk<__bf16>(kf, qf[f][c], s[f][t]);
-            }
+                for (int f = 0; f < QW; ++f) s[f][t] = mfma_chunk<__bf16>(fr[t & 1][c], qf[f][c], s[f][t]);
         }
-        f32x4 kk[TILES], vs[TILES];
-        int key0[TILES];
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             const int o = t * 4 / E * 4 * E + E * G + t * 4 % E;  // tile t's first token of lane group G
@@ -527,29 +536,27 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
             key0[t] = base + o;
         }
         u32x4 pf[QW][TILES / 2];
-        const bool masked = base + kKvPage - 1 > lim_min;
 #pragma unroll
-        for (int f = 0; f < QW; ++f) {
-            if (masked)
-                softmax_unit<TILES, D, true>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
-            else
-                softmax_unit<TILES, D, false>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
+        for (int f = 0; f < QW; ++f) softmax_unit<TILES, D, MASK>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
+#pragma unroll
+        for (int v = 0; v < VG; ++v) {
+            if (v + 1 < VG) read(slot, (TILES + v + 1) * G4, fr[(v + 1) & 1]);
+#pragma unroll
+            for (int c = 0; c < G4; ++c) {
+                const int at = v * G4 + c, n = at / J % NB, u = at / J / NB, j = at % J;
+                if (MASK) fr[v & 1][c] = keep_tokens<kKvBf16>(fr[v & 1][c], it.s.len - (base + 4 * E * u + E * G + 8 * j));
+#pragma unroll
+                for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[v & 1][c], pf[f][u * J + j], acc[f][n]);
+            }
         }
-        const bool cut = base + kKvPage > it.s.len;
-#pragma unroll
-        for (int u = 0; u < kKvPage / (4 * E); ++u)
-#pragma unroll
-            for (int n = 0; n < NB; ++n)
-#pragma unroll
-                for (int j = 0; j < J; ++j) {
-                    u32x4 vf = lds_ld16(
-                        lds_ptr((char*)slot + (FRAGS / 2 + (u * NB + n) * J + j) * kChunkBytes + lane * 16));
-                    if (cut) vf = keep_tokens<kKvBf16>(vf, it.s.len - (base + 4 * E * u + E * G + 8 * j));
-#pragma unroll
-                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(vf, pf[f][u * J + j], acc[f][n]);
-                }
         if (k + 1 < count) land(k + 1);  // page k + 1 has landed, and every wave is done with page k
-    }
+    };
+    // pages that every query of the tile sees whole, then those that a mask cuts
+    const int64_t tile_row = (int64_t)it.tile * R;
+    const int lim_min = a.kv_len ? it.s.len - it.s.n + (int)(tile_row / a.group) : it.s.len - 1;
+    const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
+    for (int k = 0; k < whole; ++k) step(k, std::false_type{});
+    for (int k = whole; k < count; ++k) step(k, std::true_type{});
 
 #pragma unroll
     for (int f = 0; f < QW; ++f) {
