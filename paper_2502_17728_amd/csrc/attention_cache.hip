@@ -21,6 +21,8 @@
 namespace dn {
 namespace ca {
 
+constexpr int kSgDsWrite = 0x200;  // with dn_device.hpp's instruction classes of the scheduling groups
+
 struct Args {
     const __bf16* Q;
     int64_t q_stride;
@@ -414,6 +416,31 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 }
 
 // ----------------------------------------------------------------------------- many rows
+// The lane's row: its sums into the tile's slot, or divided into the output.
+template <int D>
+__device__ __forceinline__ void store_rows(const Args& a, const Item& it, int rows, int64_t row, int64_t rows_all,
+                                           bool partial, int lim, const State& st, const f32x4 (&acc)[D / 16]) {
+    const int G = (threadIdx.x & 63) >> 4;
+    const float l = sum_lane_groups(st.l);
+    if (row >= rows_all) return;
+    if (partial) {
+        float* part = a.parts + ((int64_t)it.slot * rows + (row - (int64_t)it.tile * rows)) * (int64_t)(D + 4);
+#pragma unroll
+        for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(part + 16 * n + 4 * G) = acc[n];
+        if (G == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{l, st.m, 0.f, 0.f};
+        return;
+    }
+    const int qi = (int)(row / a.group);
+    const bool none = lim < 0;  // no key at all: zero
+    const float inv = 1.0f / l;
+    const int64_t oh = (int64_t)(it.s.first + qi) * a.heads * a.group + it.head * a.group + row % a.group;
+#pragma unroll
+    for (int n = 0; n < D / 16; ++n) {
+        const uint2 v = {pack_bf16(acc[n][0] * inv, acc[n][1] * inv), pack_bf16(acc[n][2] * inv, acc[n][3] * inv)};
+        *reinterpret_cast<uint2*>(a.out + oh * D + 16 * n + 4 * G) = none ? uint2{0, 0} : v;
+    }
+}
+
 // Tiles of 4 waves x QW x 16 rows.  Bound by the matrix cores and the exponentials beside them: a
 // page goes through LDS as bf16 operands (two slots, the next one filled while a page is worked on)
 // and serves the tile's four waves.  bf16 codes are copied there directly; e4m3 codes go through
@@ -559,28 +586,246 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     for (int k = whole; k < count; ++k) step(k, std::true_type{});
 
 #pragma unroll
+    for (int f = 0; f < QW; ++f)
+        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial, lim[f], st[f], acc[f]);
+}
+
+// Tiles of 8 waves x 32 rows, two waves to a SIMD.  A page is an exponential phase (mask, maximum,
+// numerators: VALU) and a matrix phase (its product with V, the scores of the next page); the two
+// halves of the workgroup run one phase apart, separated by barriers, so that on every SIMD one
+// wave's exponentials run beside the other's products: left alone the two fall into step.  The half
+// that runs behind (late) fills the rings, one page ahead: stage k is K of page k + 1 and V of page k.
+// With phases counted from the first scores of the early half (-1), early waves work on page k in 2k
+// and 2k + 1, late ones in 2k + 1 and 2k + 2; stage k lands by the end of 2k in slots last read in 2k - 2.
+template <int FMT, int D>
+__global__ __launch_bounds__(512) void wide_kernel(const Args a) {
+    using B = KvBlock<FMT, D>;
+    constexpr int E = B::E, J = E / 8, QW = 2, R = 256, TILES = 4, NB = D / 16, DC = D / 32;
+    constexpr int PAGE_K = kKvPage * D * 2;                // bf16 operands of a page's K, and of its V
+    constexpr int FRAGS = PAGE_K / kChunkBytes;
+    constexpr int CHUNKS = FRAGS / J;                      // of 1 KiB in the cache
+    constexpr int PER = CHUNKS / 4;                        // of a late wave
+    constexpr int VRING = 2 * PAGE_K, SRING = 4 * PAGE_K;  // K, V: two slots each; scales: four
+    constexpr int SCALES = 8 * kKvPage;
+    __shared__ __attribute__((aligned(1024))) char smem[SRING + 4 * SCALES];
+
+    Item it;
+    if (!find_item(a, R, it)) return;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int q = lane & 15, G = lane >> 4;
+    const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
+    if (it.chunk >= chunks) return;
+    const bool partial = a.always_partial || chunks > 1;
+    if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
+
+    const int64_t rows_all = (int64_t)it.s.n * a.group;
+    const int64_t tile_row = (int64_t)it.tile * R, row0 = tile_row + wave * QW * 16;  // the wave's first row
+    u32x4 qf[QW][DC];
+    int lim[QW];
+#pragma unroll
     for (int f = 0; f < QW; ++f) {
-        const int64_t row = row0 + f * 16 + q;
-        const float l = sum_lane_groups(st[f].l);
-        if (row >= rows_all) continue;
-        if (partial) {
-            float* part = a.parts + ((int64_t)it.slot * R + (row - (int64_t)it.tile * R)) * (int64_t)(D + 4);
+        const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
+        const int qi = (int)(row / a.group), qh = it.head * a.group + (int)(row % a.group);
+        const __bf16* qp = a.Q + (int64_t)(it.s.first + qi) * a.q_stride + (int64_t)qh * D;
 #pragma unroll
-            for (int n = 0; n < NB; ++n) *reinterpret_cast<f32x4*>(part + 16 * n + 4 * G) = acc[f][n];
-            if (G == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{l, st[f].m, 0.f, 0.f};
-        } else {
-            const int qi = (int)(row / a.group);
-            const bool none = lim[f] < 0;
-            const float inv = 1.0f / l;
-            const int64_t oh = (int64_t)(it.s.first + qi) * a.heads * a.group + it.head * a.group + row % a.group;
+        for (int c = 0; c < DC; ++c) qf[f][c] = ld16(qp + 4 * E * (c / J) + E * G + 8 * (c % J));
+        lim[f] = a.kv_len ? it.s.len - it.s.n + qi : it.s.len - 1;
+    }
+    f32x4 acc[QW][NB], s[QW][TILES];
+    State st[QW];
 #pragma unroll
-            for (int n = 0; n < NB; ++n) {
-                const uint2 v = {pack_bf16(acc[f][n][0] * inv, acc[f][n][1] * inv),
-                                 pack_bf16(acc[f][n][2] * inv, acc[f][n][3] * inv)};
-                *reinterpret_cast<uint2*>(a.out + oh * D + 16 * n + 4 * G) = none ? uint2{0, 0} : v;
+    for (int f = 0; f < QW; ++f) {
+#pragma unroll
+        for (int n = 0; n < NB; ++n) acc[f][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+        st[f] = State{kLowest, 0.f};
+    }
+
+    int page_lo, page_hi;
+    chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
+    const int count = page_hi - page_lo;
+    const int64_t page_bytes = (int64_t)a.heads * B::SIZE;
+    const char* head_base = a.pool + (int64_t)it.head * B::SIZE;
+    const uint32_t lds0 = lds_addr32(smem);
+    const bool late = wave >= 4;
+    const int w4 = wave & 3;
+    int ids = 0;
+    u32x4 raw[2][PER];
+    auto block_of = [&](int k) __attribute__((always_inline)) {
+        return head_base + (int64_t)__builtin_amdgcn_readlane(ids, k % 64) * page_bytes;
+    };
+    // One page's K (which = 0) or V: bf16 codes on their way into the ring, e4m3 codes into registers.
+    auto fetch = [&](int which, int k) __attribute__((always_inline)) {
+        const char* block = block_of(k) + which * B::PART;
+        const uint64_t src = uniform_u64(block);
+        const uint32_t dst = lds0 + which * VRING + (uint32_t)(k & 1) * PAGE_K;
+#pragma unroll
+        for (int i = 0; i < PER; ++i) {
+            const uint32_t at = (uint32_t)(w4 + 4 * i) * kChunkBytes;
+            if constexpr (J == 1)
+                g2lds16_async_sb(src, at + lane * 16, dst + at);
+            else
+                raw[which][i] = ld16(block + at + lane * 16);
+        }
+        if (which == 0 && w4 == 0 && lane < 32)
+            g2lds16_async_sb(src, (uint32_t)B::KS + lane * 16, lds0 + SRING + (uint32_t)(k & 3) * SCALES);
+    };
+    // operand i of those that a late wave's codes make: V of page k + 1, then K of page k + 2 (where
+    // there is none, what lies in the registers goes into a slot that is not read again)
+    auto put_one = [&](int i, int k) __attribute__((always_inline)) {
+        const int which = i / (PER * J) ? 0 : 1, c = i / J % PER, j = i % J;
+        char* dst = smem + which * VRING + ((which ? k + 1 : k + 2) & 1) * PAGE_K;
+        *reinterpret_cast<u32x4*>(dst + ((w4 + 4 * c) * J + j) * kChunkBytes + lane * 16) = frag<FMT>(raw[which][c], j);
+    };
+    // the page table's next 64 entries from the 64-page boundary that page k crosses
+    auto table = [&](int k) __attribute__((always_inline)) {
+        if (k % 64 == 0) ids = k + lane < count ? page_at(a, it.b, page_lo + k + lane) : 0;
+    };
+    auto stage = [&](int k) __attribute__((always_inline)) {  // V of page k before the table moves on to page k + 1's
+        fetch(1, k);
+        if (k + 1 < count) {
+            table(k + 1);
+            fetch(0, k + 1);
+        }
+    };
+    auto meet = [&]() __attribute__((always_inline)) {
+        wait_lgkm0();
+        block_barrier();
+    };
+    auto read = [&](const char* slot, int first, u32x4(&fr)[DC]) __attribute__((always_inline)) {
+#pragma unroll
+        for (int c = 0; c < DC; ++c) fr[c] = lds_ld16(lds_ptr((char*)slot + (first + c) * kChunkBytes + lane * 16));
+    };
+    constexpr int VG = FRAGS / DC;  // groups of V operands
+    u32x4 pf[QW][TILES / 2];
+    // The product of page k's numerators with V, then the scores of page k + 1.  Operands are read
+    // from LDS one group of DC ahead of their products, in an order fixed by scheduling groups: left
+    // to itself the compiler reads each beside its use and waits for it.
+    // A late wave's e4m3 codes are widened and put into the rings among the products.
+    constexpr int PUTS = J > 1 ? 2 * PER * J : 0;
+    auto matrix = [&](int k, auto pv_tag, auto qk_tag, auto mask_tag, auto put_tag) __attribute__((always_inline)) {
+        constexpr bool PV = decltype(pv_tag)::value, QK = decltype(qk_tag)::value, MASK = decltype(mask_tag)::value;
+        constexpr bool PUT = decltype(put_tag)::value && PUTS > 0;
+        constexpr int V0 = PV ? VG : 0, GROUPS = V0 + (QK ? TILES : 0);
+        const char* vb = smem + VRING + (k & 1) * PAGE_K;
+        const char* kb = smem + ((k + 1) & 1) * PAGE_K;
+        u32x4 fr[2][DC];
+        auto group = [&](int i) __attribute__((always_inline)) {
+            if (i < V0)
+                read(vb, i * DC, fr[i & 1]);
+            else
+                read(kb, (i - V0) * DC, fr[i & 1]);
+        };
+        if constexpr (QK) {
+#pragma unroll
+            for (int f = 0; f < QW; ++f)
+#pragma unroll
+                for (int t = 0; t < TILES; ++t) s[f][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        group(0);
+#pragma unroll
+        for (int i = 0; i < GROUPS; ++i) {
+            if (i + 1 < GROUPS) group(i + 1);
+            if (PUT && i < PUTS) put_one(i, k);
+#pragma unroll
+            for (int c = 0; c < DC; ++c) {
+                if (i < V0) {
+                    const int at = i * DC + c, n = at / J % NB, u = at / J / NB, j = at % J;
+                    if (MASK)
+                        fr[i & 1][c] = keep_tokens<kKvBf16>(
+                            fr[i & 1][c], it.s.len - ((page_lo + k) * kKvPage + 4 * E * u + E * G + 8 * j));
+#pragma unroll
+                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[i & 1][c], pf[f][u * J + j], acc[f][n]);
+                } else {
+                    const int t = i - V0;
+#pragma unroll
+                    for (int f = 0; f < QW; ++f) s[f][t] = mfma_chunk<__bf16>(fr[i & 1][c], qf[f][c], s[f][t]);
+                }
             }
         }
+        if constexpr (!MASK) {
+            __builtin_amdgcn_sched_group_barrier(kSgDsRead, DC, 0);
+#pragma unroll
+            for (int i = 0; i < GROUPS; ++i) {
+                if (i + 1 < GROUPS) __builtin_amdgcn_sched_group_barrier(kSgDsRead, DC, 0);
+                if (PUT && i < PUTS) {
+#pragma unroll
+                    for (int v = 0; v < 4; ++v) {
+                        __builtin_amdgcn_sched_group_barrier(kSgMfma, DC * QW / 4, 0);
+                        __builtin_amdgcn_sched_group_barrier(kSgValu, 1, 0);
+                    }
+                    __builtin_amdgcn_sched_group_barrier(kSgDsWrite, 1, 0);
+                } else {
+                    __builtin_amdgcn_sched_group_barrier(kSgMfma, DC * QW, 0);
+                }
+            }
+        }
+    };
+    auto exponentials = [&](int k, auto mask_tag) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(mask_tag)::value;
+        const char* scales = smem + SRING + (k & 3) * SCALES;
+        f32x4 kk[TILES], vs[TILES];
+        int key0[TILES];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            const int o = t * 4 / E * 4 * E + E * G + t * 4 % E;  // tile t's first token of lane group G
+            kk[t] = *reinterpret_cast<const f32x4*>(scales + 4 * o) * a.sl2;
+            vs[t] = *reinterpret_cast<const f32x4*>(scales + 4 * kKvPage + 4 * o);
+            key0[t] = (page_lo + k) * kKvPage + o;
+        }
+#pragma unroll
+        for (int f = 0; f < QW; ++f) softmax_unit<TILES, D, MASK>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
+    };
+    const std::true_type yes{};
+    const std::false_type no{};
+    auto page = [&](int k, auto mask_tag, auto late_tag) __attribute__((always_inline)) {
+        constexpr bool LATE = decltype(late_tag)::value;
+        const bool more = k + 1 < count;
+        if (LATE && J == 1 && more) stage(k + 1);
+        exponentials(k, mask_tag);
+        meet();
+        if (more)
+            matrix(k, yes, yes, mask_tag, late_tag);
+        else
+            matrix(k, yes, no, mask_tag, no);
+        if (LATE && more) {
+            wait_vm();  // stage k + 1
+            if (J > 1 && k + 2 < count) stage(k + 2);
+        }
+        if (!LATE || more) meet();
+    };
+    // pages that every query of the tile sees whole, then those that a mask cuts
+    const int lim_min = a.kv_len ? it.s.len - it.s.n + (int)(tile_row / a.group) : it.s.len - 1;
+    const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
+    if (count > 0) {
+        if (late) {
+            table(0);
+            fetch(0, 0);
+#pragma unroll
+            for (int i = PER * J; i < PUTS; ++i) put_one(i, -2);
+            wait_vm();
+            meet();
+            stage(0);  // phase -1
+            meet();
+            matrix(-1, no, yes, no, no);
+#pragma unroll
+            for (int i = 0; i < PUTS; ++i) put_one(i, -1);
+            wait_vm();
+            if (J > 1 && count > 1) stage(1);
+            meet();
+            for (int k = 0; k < whole; ++k) page(k, no, yes);
+            for (int k = whole; k < count; ++k) page(k, yes, yes);
+        } else {
+            meet();
+            matrix(-1, no, yes, no, no);
+            meet();
+            for (int k = 0; k < whole; ++k) page(k, no, no);
+            for (int k = whole; k < count; ++k) page(k, yes, no);
+        }
     }
+
+#pragma unroll
+    for (int f = 0; f < QW; ++f)
+        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial, lim[f], st[f], acc[f]);
 }
 
 // ----------------------------------------------------------------------------- merge
@@ -690,8 +935,10 @@ hipError_t launch(const Args& a, int rows, int64_t grid, hipStream_t s) {
         decode_kernel<FMT, D><<<g, 256, 0, s>>>(a);
     else if (rows == 64)
         tile_kernel<FMT, D, 1><<<g, 256, 0, s>>>(a);
-    else
+    else if (rows == 128)
         tile_kernel<FMT, D, 2><<<g, 256, 0, s>>>(a);
+    else
+        wide_kernel<FMT, D><<<g, 512, 0, s>>>(a);
     return hipGetLastError();
 }
 hipError_t launch_any(const KvPool& c, const Args& a, int rows, int64_t grid, hipStream_t s) {

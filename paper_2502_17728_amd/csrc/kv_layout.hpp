@@ -68,7 +68,7 @@ inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, 
                             bool always_partial) {
     CachePlan p;
     p.rows = rows;
-    p.target = rows == 16 ? 768 : 512;
+    p.target = rows == 16 ? 768 : rows == 256 ? 256 : 512;
     p.least = rows == 16 ? 8 : 4;
     const int64_t tiles = std::min(T * group, T * group / rows + std::min(B, T));
     const int64_t most = (table_width + p.least - 1) / p.least;  // chunks of one tile
@@ -83,7 +83,7 @@ inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, 
 // once and go straight to registers.
 inline int cache_rows(int64_t T, int64_t B, int64_t group) {
     if (T * group <= 16 * B) return 16;
-    return T * group <= 64 * B ? 64 : 128;
+    return T * group <= 64 * B ? 64 : T * group <= 128 * B ? 128 : 256;
 }
 
 inline size_t cache_slot_bytes(int rows, int64_t d) { return (size_t)rows * (size_t)(d + 4) * sizeof(float); }
