@@ -21,7 +21,12 @@
 namespace dn {
 namespace ca {
 
-constexpr int kSgDsWrite = 0x200;  // with dn_device.hpp's instruction classes of the scheduling groups
+// A run's share of a tile: pages [lo, hi), and where its partial sums go (kWhole: it has all pages and
+// writes the output; kNone: no pages).
+struct Piece {
+    int b, head, tile, lo, hi, slot;
+};
+constexpr int kWhole = -1, kNone = -2;
 
 struct Args {
     const __bf16* Q;
@@ -38,7 +43,12 @@ struct Args {
     int64_t target, least, slots;
     int always_partial;
     float sl2;  // scale * log2(e)
-    int4* info;    // [B]: first slot, pages per chunk, chunks of the longest tile, 0
+    int4* info;    // [B]: first slot, pages per chunk, chunks of the longest tile, first tile
+    // dealt in runs (else null, 0): of each run and of each tile its first piece and their number
+    int2* run_pieces;
+    int2* tile_pieces;
+    Piece* pieces;
+    int64_t tiles_most;
     float* parts;  // [slots][rows][d + 4]: sums, l, m
     __bf16* out;   // [T][heads * group][d]
 };
@@ -63,7 +73,7 @@ __device__ __forceinline__ Seq sequence(const Args& a, int64_t b) {
 
 struct Item {
     int b, tile, chunk, head;
-    int per;       // pages per chunk
+    int per;   // pages per chunk
     int slot;  // of this item, where its tile has several chunks
     Seq s;
 };
@@ -158,6 +168,140 @@ __device__ __forceinline__ void chunk_pages(int keys, int chunks, int chunk, int
     const int pages = (keys + kKvPage - 1) / kKvPage, each = pages / chunks, more = pages - each * chunks;
     lo = chunk * each + min(chunk, more);
     hi = lo + each + (chunk < more ? 1 : 0);
+}
+
+// ----------------------------------------------------------------------------- runs
+// Long tiles are dealt in equal runs.  The work is laid on a line: sequences, of each its key/value
+// heads, of each its tiles, of each its pages.  A tile weighs the query-key pairs of its rows' largest
+// query, times `group`, and a start; a sequence's tiles then sum to a closed form.  Every run is an
+// equal stretch of the line, so all end together whatever the lengths.  A tile that several runs
+// share leaves partial sums, two slots to a run at most: its first tile's and its last's.
+struct Weights {
+    int64_t each, more;  // tile t weighs each + (t + 1) more
+    __device__ __forceinline__ int64_t before(int64_t t) const { return t * each + more * (t * (t + 1) / 2); }
+    __device__ __forceinline__ int64_t of(int64_t t) const { return each + (t + 1) * more; }
+};
+constexpr int kStart = 128;  // a tile's start and end, in keys
+__device__ __forceinline__ Weights weights(const Args& a, const Seq& s, int rows) {
+    return Weights{(int64_t)(max(s.len - s.n, 0) + kStart) * a.group, rows};
+}
+__device__ __forceinline__ int tiles_of(const Args& a, const Seq& s, int rows) {
+    return (int)(((int64_t)s.n * a.group + rows - 1) / rows);
+}
+// The page at which the line is cut `at` into a tile; nobody is left a single page.
+__device__ __forceinline__ int cut_page(int64_t at, int64_t weight, int pages) {
+    if (at <= 0) return 0;
+    if (at >= weight) return pages;
+    const int p = (int)((double)at * (double)pages / (double)weight);
+    return p < 2 ? 0 : pages - p < 2 ? pages : p;
+}
+
+// Lists every run's pieces, a run to a thread.  Piece (tile + run) of the line: both only grow.
+__global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
+    const int lane = threadIdx.x;
+    const int64_t run = (int64_t)blockIdx.x * 64 + lane;
+    int64_t total = 0;
+    for (int64_t b = lane; b < a.B; b += 64) {
+        const Seq s = sequence(a, b);
+        total += weights(a, s, rows).before(tiles_of(a, s, rows)) * a.heads;
+    }
+#pragma unroll
+    for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
+    const int64_t per = max((total + a.target - 1) / a.target, a.least * kKvPage * a.group);
+    const int64_t x0 = run * per, x1 = min(x0 + per, total);
+    // the sequence in which the run starts: 64 sequences at a time, one to a lane
+    int64_t start = 0, tile_start = 0, b = -1, b_start = 0, b_tiles = 0;
+    for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
+        int64_t sum = 0, tiles = 0;
+        if (b0 + lane < a.B) {
+            const Seq s = sequence(a, b0 + lane);
+            tiles = tiles_of(a, s, rows);
+            sum = weights(a, s, rows).before(tiles) * a.heads;
+            tiles *= a.heads;
+        }
+        int64_t to = sum, tiles_to = tiles;
+#pragma unroll
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t y = __shfl_up(to, o), z = __shfl_up(tiles_to, o);
+            to += lane >= o ? y : 0;
+            tiles_to += lane >= o ? z : 0;
+        }
+        to += start;
+        tiles_to += tile_start;
+        if (blockIdx.x == 0 && b0 + lane < a.B) a.info[b0 + lane] = int4{0, 0, 0, (int)(tiles_to - tiles)};
+        int low = 0, high = 64;  // the first lane whose sequence ends past x0
+#pragma unroll
+        for (int i = 0; i < 6; ++i) {
+            const int mid = (low + high) >> 1;
+            if (__shfl(to, mid - 1) <= x0)
+                low = mid;
+            else
+                high = mid;
+        }
+        const int64_t to_l = __shfl(to, low & 63), sum_l = __shfl(sum, low & 63);
+        const int64_t tiles_to_l = __shfl(tiles_to, low & 63), tiles_l = __shfl(tiles, low & 63);
+        if (b < 0 && to_l > x0) {
+            b = b0 + low;
+            b_start = to_l - sum_l;
+            b_tiles = tiles_to_l - tiles_l;
+        }
+        start = __shfl(to, 63);
+        tile_start = __shfl(tiles_to, 63);
+    }
+    if (run >= a.target) return;
+    int2 list = {0, 0};
+    if (b >= 0 && x0 < x1) {
+        Seq s = sequence(a, b);
+        Weights w = weights(a, s, rows);
+        int tiles = tiles_of(a, s, rows);
+        const int64_t head_weight = w.before(tiles);
+        int head = (int)((x0 - b_start) / head_weight);
+        const int64_t at = x0 - b_start - head * head_weight;
+        int tile = 0, high = tiles - 1;  // the last tile that starts at `at` or before
+        while (tile < high) {
+            const int mid = (tile + high + 1) >> 1;
+            if (w.before(mid) <= at)
+                tile = mid;
+            else
+                high = mid - 1;
+        }
+        int64_t x = x0 - at + w.before(tile);  // where the tile starts
+        int64_t ordinal = b_tiles + (int64_t)head * tiles + tile;
+        list.x = (int)(ordinal + run);
+        while (true) {
+            const int64_t weight = w.of(tile), piece = ordinal + run;
+            const int pages = (tile_keys(a, s, tile, rows) + kKvPage - 1) / kKvPage;
+            const int lo = cut_page(x0 - x, weight, pages), hi = cut_page(x1 - x, weight, pages);
+            if (ordinal >= a.tiles_most) break;  // q_start out of order
+            const int slot = (int)(2 * run) + (x > x0 ? 1 : 0);
+            a.pieces[piece] = Piece{(int)b, head, tile, lo, hi,
+                                    lo == 0 && hi == pages && (pages > 0 || x >= x0) ? kWhole : lo < hi ? slot : kNone};
+            if (x >= x0) {
+                const int64_t last = (x + weight - 1) / per;
+                // a run is longer than a start and two pages, so one of any three cuts divides the tile
+                bool whole = true;
+                for (int64_t r = run + 1; r <= min(last, run + 3); ++r) {
+                    const int cut = cut_page(r * per - x, weight, pages);
+                    whole = whole && (cut == 0 || cut == pages);
+                }
+                a.tile_pieces[ordinal] = int2{(int)piece, whole ? 0 : (int)(last - run) + 1};
+            }
+            ++list.y;
+            x += weight;
+            if (x >= x1) break;
+            ++ordinal;
+            if (++tile < tiles) continue;
+            tile = 0;
+            if (++head < a.heads) continue;
+            head = 0;
+            do
+                if (++b >= a.B) break;
+            while ((tiles = tiles_of(a, s = sequence(a, b), rows)) == 0);
+            if (b >= a.B) break;
+            w = weights(a, s, rows);
+        }
+    }
+    a.run_pieces[run] = list;
 }
 
 // The table's page, kept inside the pool whatever the table holds.
@@ -419,12 +563,12 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 // The lane's row: its sums into the tile's slot, or divided into the output.
 template <int D>
 __device__ __forceinline__ void store_rows(const Args& a, const Item& it, int rows, int64_t row, int64_t rows_all,
-                                           bool partial, int lim, const State& st, const f32x4 (&acc)[D / 16]) {
+                                           int slot, int lim, const State& st, const f32x4 (&acc)[D / 16]) {
     const int G = (threadIdx.x & 63) >> 4;
     const float l = sum_lane_groups(st.l);
     if (row >= rows_all) return;
-    if (partial) {
-        float* part = a.parts + ((int64_t)it.slot * rows + (row - (int64_t)it.tile * rows)) * (int64_t)(D + 4);
+    if (slot >= 0) {
+        float* part = a.parts + ((int64_t)slot * rows + (row - (int64_t)it.tile * rows)) * (int64_t)(D + 4);
 #pragma unroll
         for (int n = 0; n < D / 16; ++n) *reinterpret_cast<f32x4*>(part + 16 * n + 4 * G) = acc[n];
         if (G == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{l, st.m, 0.f, 0.f};
@@ -587,7 +731,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
 
 #pragma unroll
     for (int f = 0; f < QW; ++f)
-        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial, lim[f], st[f], acc[f]);
+        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial ? it.slot : kWhole, lim[f], st[f], acc[f]);
 }
 
 // Tiles of 8 waves x 32 rows, two waves to a SIMD.  A page is an exponential phase (mask, maximum,
@@ -609,14 +753,40 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     constexpr int SCALES = 8 * kKvPage;
     __shared__ __attribute__((aligned(1024))) char smem[SRING + 4 * SCALES];
 
-    Item it;
-    if (!find_item(a, R, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int q = lane & 15, G = lane >> 4;
-    const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
-    if (it.chunk >= chunks) return;
-    const bool partial = a.always_partial || chunks > 1;
-    if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
+    Item it;
+    int page_lo, count, slot;
+    int2 list = {0, 1};
+    if (a.pieces) {
+        // give each XCD a stretch of the line: its workgroups then share keys in one L2
+        list = a.run_pieces[xcd_contiguous(blockIdx.x, gridDim.x)];
+        list.x = __builtin_amdgcn_readfirstlane(list.x);
+        list.y = __builtin_amdgcn_readfirstlane(list.y);
+    }
+    for (; list.y > 0; ++list.x, --list.y) {
+    if (a.pieces) {
+        const Piece p = a.pieces[list.x];
+        it.b = __builtin_amdgcn_readfirstlane(p.b);
+        it.head = __builtin_amdgcn_readfirstlane(p.head);
+        it.tile = __builtin_amdgcn_readfirstlane(p.tile);
+        page_lo = __builtin_amdgcn_readfirstlane(p.lo);
+        count = __builtin_amdgcn_readfirstlane(p.hi) - page_lo;
+        slot = __builtin_amdgcn_readfirstlane(p.slot);
+        const Seq s = sequence(a, it.b);
+        it.s.first = __builtin_amdgcn_readfirstlane(s.first);
+        it.s.n = __builtin_amdgcn_readfirstlane(s.n);
+        it.s.len = __builtin_amdgcn_readfirstlane(s.len);
+    } else {
+        if (!find_item(a, R, it)) return;
+        const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
+        if (it.chunk >= chunks) return;
+        int page_hi;
+        chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
+        count = page_hi - page_lo;
+        slot = a.always_partial || chunks > 1 ? it.slot : kWhole;
+    }
+    if (slot == kNone || slot >= a.slots) continue;
 
     const int64_t rows_all = (int64_t)it.s.n * a.group;
     const int64_t tile_row = (int64_t)it.tile * R, row0 = tile_row + wave * QW * 16;  // the wave's first row
@@ -640,9 +810,6 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         st[f] = State{kLowest, 0.f};
     }
 
-    int page_lo, page_hi;
-    chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
-    const int count = page_hi - page_lo;
     const int64_t page_bytes = (int64_t)a.heads * B::SIZE;
     const char* head_base = a.pool + (int64_t)it.head * B::SIZE;
     const uint32_t lds0 = lds_addr32(smem);
@@ -669,12 +836,22 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         if (which == 0 && w4 == 0 && lane < 32)
             g2lds16_async_sb(src, (uint32_t)B::KS + lane * 16, lds0 + SRING + (uint32_t)(k & 3) * SCALES);
     };
-    // operand i of those that a late wave's codes make: V of page k + 1, then K of page k + 2 (where
-    // there is none, what lies in the registers goes into a slot that is not read again)
-    auto put_one = [&](int i, int k) __attribute__((always_inline)) {
-        const int which = i / (PER * J) ? 0 : 1, c = i / J % PER, j = i % J;
-        char* dst = smem + which * VRING + ((which ? k + 1 : k + 2) & 1) * PAGE_K;
-        *reinterpret_cast<u32x4*>(dst + ((w4 + 4 * c) * J + j) * kChunkBytes + lane * 16) = frag<FMT>(raw[which][c], j);
+    // A late wave's e4m3 codes into the rings: V of page k + 1 and K of page k + 2 (where there is none,
+    // what lies in the registers goes into a slot that is not read again).
+    auto put = [&](int k, bool v = true) __attribute__((always_inline)) {
+        if constexpr (J > 1) {
+#pragma unroll
+            for (int which = 1; which >= 0; --which) {
+                char* dst = smem + which * VRING + ((which ? k + 1 : k + 2) & 1) * PAGE_K;
+                if (which && !v) continue;
+#pragma unroll
+                for (int i = 0; i < PER; ++i)
+#pragma unroll
+                    for (int j = 0; j < J; ++j)
+                        *reinterpret_cast<u32x4*>(dst + ((w4 + 4 * i) * J + j) * kChunkBytes + lane * 16) =
+                            frag<FMT>(raw[which][i], j);
+            }
+        }
     };
     // the page table's next 64 entries from the 64-page boundary that page k crosses
     auto table = [&](int k) __attribute__((always_inline)) {
@@ -700,11 +877,8 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     // The product of page k's numerators with V, then the scores of page k + 1.  Operands are read
     // from LDS one group of DC ahead of their products, in an order fixed by scheduling groups: left
     // to itself the compiler reads each beside its use and waits for it.
-    // A late wave's e4m3 codes are widened and put into the rings among the products.
-    constexpr int PUTS = J > 1 ? 2 * PER * J : 0;
-    auto matrix = [&](int k, auto pv_tag, auto qk_tag, auto mask_tag, auto put_tag) __attribute__((always_inline)) {
+    auto matrix = [&](int k, auto pv_tag, auto qk_tag, auto mask_tag) __attribute__((always_inline)) {
         constexpr bool PV = decltype(pv_tag)::value, QK = decltype(qk_tag)::value, MASK = decltype(mask_tag)::value;
-        constexpr bool PUT = decltype(put_tag)::value && PUTS > 0;
         constexpr int V0 = PV ? VG : 0, GROUPS = V0 + (QK ? TILES : 0);
         const char* vb = smem + VRING + (k & 1) * PAGE_K;
         const char* kb = smem + ((k + 1) & 1) * PAGE_K;
@@ -725,7 +899,6 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
 #pragma unroll
         for (int i = 0; i < GROUPS; ++i) {
             if (i + 1 < GROUPS) group(i + 1);
-            if (PUT && i < PUTS) put_one(i, k);
 #pragma unroll
             for (int c = 0; c < DC; ++c) {
                 if (i < V0) {
@@ -747,16 +920,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
 #pragma unroll
             for (int i = 0; i < GROUPS; ++i) {
                 if (i + 1 < GROUPS) __builtin_amdgcn_sched_group_barrier(kSgDsRead, DC, 0);
-                if (PUT && i < PUTS) {
-#pragma unroll
-                    for (int v = 0; v < 4; ++v) {
-                        __builtin_amdgcn_sched_group_barrier(kSgMfma, DC * QW / 4, 0);
-                        __builtin_amdgcn_sched_group_barrier(kSgValu, 1, 0);
-                    }
-                    __builtin_amdgcn_sched_group_barrier(kSgDsWrite, 1, 0);
-                } else {
-                    __builtin_amdgcn_sched_group_barrier(kSgMfma, DC * QW, 0);
-                }
+                __builtin_amdgcn_sched_group_barrier(kSgMfma, DC * QW, 0);
             }
         }
     };
@@ -783,11 +947,14 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         if (LATE && J == 1 && more) stage(k + 1);
         exponentials(k, mask_tag);
         meet();
+        __builtin_amdgcn_s_setprio(1);  // the products first: the other wave's exponentials fill the gaps
         if (more)
-            matrix(k, yes, yes, mask_tag, late_tag);
+            matrix(k, yes, yes, mask_tag);
         else
-            matrix(k, yes, no, mask_tag, no);
+            matrix(k, yes, no, mask_tag);
+        __builtin_amdgcn_s_setprio(0);
         if (LATE && more) {
+            put(k);
             wait_vm();  // stage k + 1
             if (J > 1 && k + 2 < count) stage(k + 2);
         }
@@ -800,15 +967,13 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         if (late) {
             table(0);
             fetch(0, 0);
-#pragma unroll
-            for (int i = PER * J; i < PUTS; ++i) put_one(i, -2);
+            put(-2, false);
             wait_vm();
             meet();
             stage(0);  // phase -1
             meet();
-            matrix(-1, no, yes, no, no);
-#pragma unroll
-            for (int i = 0; i < PUTS; ++i) put_one(i, -1);
+            matrix(-1, no, yes, no);
+            put(-1);
             wait_vm();
             if (J > 1 && count > 1) stage(1);
             meet();
@@ -816,7 +981,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
             for (int k = whole; k < count; ++k) page(k, yes, yes);
         } else {
             meet();
-            matrix(-1, no, yes, no, no);
+            matrix(-1, no, yes, no);
             meet();
             for (int k = 0; k < whole; ++k) page(k, no, no);
             for (int k = whole; k < count; ++k) page(k, yes, no);
@@ -825,24 +990,19 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
 
 #pragma unroll
     for (int f = 0; f < QW; ++f)
-        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial, lim[f], st[f], acc[f]);
+        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, slot, lim[f], st[f], acc[f]);
+    __syncthreads();  // before the next piece's pages
+    }
 }
 
 // ----------------------------------------------------------------------------- merge
 struct Set {
     const int4* info;
     const float* parts;
+    const Piece* pieces;  // of runs; null: chunks
     int64_t slots;
     int rows;
 };
-
-// Partial sums of a row: the first one's slot, the next ones `heads` slots further each.  0 where the
-// plan that a sequence's workgroups left does not fit the workspace (q_start out of order).
-__device__ __forceinline__ int parts_of(const Set& set, const int4& plan, int tile, int chunks, int heads, int h,
-                                        int64_t& first) {
-    first = plan.x + (int64_t)tile * plan.z * heads + h;
-    return first >= 0 && first + (int64_t)(chunks - 1) * heads < set.slots ? chunks : 0;
-}
 
 // Output rows (token, query head): D / 4 threads over a row's dimensions, NS such groups over its
 // partial sums, the other threads over rows.  `shared` (parts null: none) holds the partial sums over
@@ -880,12 +1040,25 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
             const int4 plan = set.info[w ? 0 : b];
             const int64_t row = (w ? token : token - s.first) * a.group + r;
             const int tile = (int)(row / set.rows);
-            const int chunks = w ? plan.z : tile_chunks(tile_keys(a, s, tile, set.rows), max(plan.y, 1));
-            if (!shared.parts && chunks == 1) write = false;
-            int64_t first;
-            const int count = write ? parts_of(set, plan, tile, chunks, a.heads, h, first) : 0;
+            int count, first;
+            if (set.pieces) {
+                const int64_t ordinal = plan.w + (int64_t)h * tiles_of(a, s, set.rows) + tile;
+                int2 list = {0, 0};
+                if (ordinal >= 0 && ordinal < a.tiles_most) list = a.tile_pieces[ordinal];
+                first = list.x;
+                count = list.y;
+                if (!shared.parts && count == 0) write = false;
+            } else {
+                const int chunks = w ? plan.z : tile_chunks(tile_keys(a, s, tile, set.rows), max(plan.y, 1));
+                if (!shared.parts && chunks == 1) write = false;
+                first = plan.x + tile * plan.z * a.heads + h;
+                count = chunks;
+            }
+            if (!write) break;
             for (int c = g; c < count; c += NS) {
-                const float* part = set.parts + ((first + (int64_t)c * a.heads) * set.rows + row % set.rows) * (D + 4);
+                const int slot = set.pieces ? set.pieces[first + c].slot : first + c * a.heads;
+                if (slot < 0 || slot >= set.slots) continue;  // a run with none of its pages; q_start out of order
+                const float* part = set.parts + ((int64_t)slot * set.rows + row % set.rows) * (D + 4);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(part + x), t = *reinterpret_cast<const f32x4*>(part + D);
                 const float mn = fmaxf(m, t[1]), wo = weight(m, mn), wn = weight(t[1], mn);
                 l = wo * l + wn * t[0];
@@ -963,38 +1136,44 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
     a.T = c.T;
     a.sl2 = c.scale * 1.4426950408889634f;
     a.out = (__bf16*)c.out;
-    ca::Args own = a, pre = a;
+    auto planned = [&](const CachePlan& p, size_t info, size_t parts, size_t runs) {
+        a.target = p.target;
+        a.least = p.least;
+        a.slots = p.slots;
+        a.info = (int4*)(ws + info);
+        a.parts = (float*)(ws + parts);
+        a.run_pieces = p.in_runs ? (int2*)(ws + runs) : nullptr;
+        a.tile_pieces = p.in_runs ? a.run_pieces + p.target : nullptr;
+        a.pieces = p.in_runs ? (ca::Piece*)(a.tile_pieces + p.tiles) : nullptr;
+        a.tiles_most = p.tiles;
+        return ca::Set{a.info, a.parts, a.pieces, p.slots, p.rows};
+    };
     ca::Set shared{};
     if (prefix_pages > 0) {
-        pre.table = c.prefix_table;
-        pre.width = prefix_pages;
-        pre.prefix = c.prefix;
-        pre.B = 1;
-        pre.target = w.prefix.target;
-        pre.least = w.prefix.least;
-        pre.slots = w.prefix.slots;
-        pre.always_partial = 1;
-        pre.info = (int4*)ws + c.B;
-        pre.parts = (float*)(ws + w.prefix_slots);
-        const hipError_t e = ca::launch_any(c.pool, pre, w.prefix.rows, w.prefix.grid, s);
+        a.table = c.prefix_table;
+        a.width = prefix_pages;
+        a.prefix = c.prefix;
+        a.B = 1;
+        a.always_partial = 1;
+        shared = planned(w.prefix, w.prefix_info, w.prefix_parts, 0);
+        const hipError_t e = ca::launch_any(c.pool, a, w.prefix.rows, w.prefix.grid, s);
         if (e != hipSuccess) return e;
-        shared = ca::Set{pre.info, pre.parts, pre.slots, w.prefix.rows};
     }
-    own.table = c.table;
-    own.width = c.width;
-    own.q_start = c.q_start;
-    own.kv_len = c.kv_len;
-    own.B = c.B;
-    own.target = w.own.target;
-    own.least = w.own.least;
-    own.slots = w.own.slots;
-    own.always_partial = prefix_pages > 0;
-    own.info = (int4*)ws;
-    own.parts = (float*)(ws + w.own_slots);
-    const hipError_t e = ca::launch_any(c.pool, own, w.own.rows, w.own.grid, s);
-    if (e != hipSuccess || (w.own.slots == 0 && prefix_pages == 0)) return e;
-    const ca::Set set{own.info, own.parts, own.slots, w.own.rows};
-    return c.pool.d == 64 ? ca::launch_merge<64>(own, set, shared, s) : ca::launch_merge<128>(own, set, shared, s);
+    a.table = c.table;
+    a.width = c.width;
+    a.q_start = c.q_start;
+    a.kv_len = c.kv_len;
+    a.B = c.B;
+    const ca::Set own = planned(w.own, w.own_info, w.own_parts, w.own_runs);
+    hipError_t e;
+    if (a.pieces) {
+        ca::plan_kernel<<<dim3((unsigned)((w.own.target + 63) / 64)), 64, 0, s>>>(a, w.own.rows);
+        e = hipGetLastError();
+        if (e != hipSuccess) return e;
+    }
+    e = ca::launch_any(c.pool, a, w.own.rows, w.own.grid, s);
+    if (e != hipSuccess || w.own.slots == 0) return e;
+    return c.pool.d == 64 ? ca::launch_merge<64>(a, own, shared, s) : ca::launch_merge<128>(a, own, shared, s);
 }
 
 }  // namespace dn

@@ -51,63 +51,71 @@ inline size_t kv_block_bytes(int64_t d, int format) {
 
 // ------------------------------------------------------------------- attention over the cache
 // Work is dealt on the device, where the lengths are.  Of sequence b the n g query rows of one
-// key/value head (n new tokens, g query heads) make tiles of `rows`; a tile's keys are cut into
-// chunks of `chunk` pages, chunk = ceil(pages of all tiles and heads / target), at least `least`.
-// Each (tile, chunk, head) is one workgroup, so all have about the same work whatever the lengths.
-// Chunks of a tile that has several leave partial sums, which a second kernel merges.
+// key/value head (n new tokens, g query heads) make tiles of `rows`.  Two deals:
+// - chunks: a tile's keys are cut into equal chunks of at most `per` pages, per = ceil(pages of all
+//   tiles and heads / target), at least `least`; each (tile, chunk, head) is a workgroup, which finds
+//   itself by a scan of the lengths.  For work whose chunks are short.
+// - runs: a kernel before lists, for each of `target` workgroups, an equal stretch of all tiles' keys.
+//   It costs a launch; chunks of uneven tiles leave more of the chip idle once they are long.
+// A tile that is cut leaves partial sums, which a last kernel merges.
 struct CachePlan {
-    int rows;        // query rows per tile: 16 (keys straight to registers) or 64, 128 (through LDS)
+    int rows;        // query rows per tile: 16 (keys straight to registers), 64, 128 or 256 (through LDS)
+    bool in_runs;
     int64_t target;  // workgroups aimed at
-    int64_t least;   // pages per chunk at least
-    int64_t grid;    // workgroups at most
+    int64_t least;   // pages per chunk or run at least
+    int64_t tiles;   // at most, over all heads
+    int64_t grid;    // workgroups launched
     int64_t slots;   // partial sums at most
 };
-
-// every tile's chunks: at most one more than an even share each, and no more than the table holds
-inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, int64_t table_width, int rows,
-                            bool always_partial) {
-    CachePlan p;
-    p.rows = rows;
-    p.target = rows == 16 ? 768 : rows == 256 ? 256 : 512;
-    p.least = rows == 16 ? 8 : 4;
-    const int64_t tiles = std::min(T * group, T * group / rows + std::min(B, T));
-    const int64_t most = (table_width + p.least - 1) / p.least;  // chunks of one tile
-    p.grid = heads * tiles > INT64_MAX / most ? p.target + heads * tiles
-                                              : std::min(p.target + heads * tiles, heads * tiles * most);
-    // several chunks of a tile are at most twice its even share
-    p.slots = always_partial ? p.grid : most < 2 ? 0 : std::min(2 * p.target, p.grid);
-    return p;
-}
 
 // Tiles of 16 rows while the sequences have no more rows than that on average; keys are then used
 // once and go straight to registers.
 inline int cache_rows(int64_t T, int64_t B, int64_t group) {
-    if (T * group <= 16 * B) return 16;
-    return T * group <= 64 * B ? 64 : T * group <= 128 * B ? 128 : 256;
+    const int64_t rows = (T * group + B - 1) / B;
+    return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+}
+
+inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, int64_t table_width, int rows,
+                            bool prefix, bool always_partial) {
+    CachePlan p;
+    p.rows = rows;
+    p.target = rows == 16 ? 768 : rows == 256 ? 256 : 512;
+    p.least = rows == 16 ? 8 : 4;
+    p.tiles = heads * std::min(T * group, T * group / rows + std::min(B, T));
+    const int64_t most = (table_width + p.least - 1) / p.least;  // chunks of one tile
+    p.in_runs = rows == 256 && !prefix && !always_partial && most > 1;
+    // every tile's chunks: at most one more than an even share each, and no more than the table holds
+    p.grid = p.in_runs ? p.target : p.tiles > INT64_MAX / most ? p.target + p.tiles : std::min(p.target + p.tiles, p.tiles * most);
+    // several chunks of a tile are at most twice its even share; a run cuts two tiles
+    p.slots = always_partial ? p.grid : most < 2 ? 0 : p.in_runs ? 2 * p.target : std::min(2 * p.target, p.grid);
+    return p;
 }
 
 inline size_t cache_slot_bytes(int rows, int64_t d) { return (size_t)rows * (size_t)(d + 4) * sizeof(float); }
 
-// Workspace: what each sequence's chunks are (16 bytes each), then the partial sums; behind a
-// shared prefix (one sequence of all T tokens) the prefix's own first.
+// Workspace: 16 bytes for each sequence and for the shared prefix (one sequence of all T tokens), the
+// runs' lists (8 bytes a run and a tile, 24 a piece), then the partial sums.
 struct CacheWorkspace {
     CachePlan own, prefix;
-    size_t info, prefix_slots, own_slots, total;
+    size_t own_info, prefix_info, own_runs, own_parts, prefix_parts, total;
 };
 inline CacheWorkspace cache_workspace(int64_t T, int64_t B, int64_t heads, int64_t group, int64_t d, int64_t table_width,
                                       int64_t prefix_pages) {
     CacheWorkspace w;
-    w.own = cache_plan(T, B, heads, group, table_width, cache_rows(T, B, group), prefix_pages > 0);
-    w.info = 0;
-    w.prefix_slots = (size_t)(B + 1) * 16;
-    w.prefix_slots = (w.prefix_slots + 255) / 256 * 256;
-    w.own_slots = w.prefix_slots;
+    w.own = cache_plan(T, B, heads, group, table_width, cache_rows(T, B, group), false, prefix_pages > 0);
+    w.own_info = 0;
+    w.prefix_info = (size_t)B * 16;
+    w.own_runs = w.prefix_info + 16;
+    w.own_parts = w.own_runs;
+    if (w.own.in_runs) w.own_parts += (size_t)(w.own.target + w.own.tiles) * (8 + 24);
+    w.own_parts = (w.own_parts + 255) / 256 * 256;
+    w.prefix_parts = w.own_parts + (size_t)w.own.slots * cache_slot_bytes(w.own.rows, d);
+    w.total = w.prefix_parts;
     w.prefix = CachePlan{};
     if (prefix_pages > 0) {
-        w.prefix = cache_plan(T, 1, heads, group, prefix_pages, cache_rows(T, 1, group), true);
-        w.own_slots += (size_t)w.prefix.slots * cache_slot_bytes(w.prefix.rows, d);
+        w.prefix = cache_plan(T, 1, heads, group, prefix_pages, cache_rows(T, 1, group), true, true);
+        w.total += (size_t)w.prefix.slots * cache_slot_bytes(w.prefix.rows, d);
     }
-    w.total = w.own_slots + (size_t)w.own.slots * cache_slot_bytes(w.own.rows, d);
     return w;
 }
 
