@@ -75,7 +75,7 @@ struct Item {
     int b, tile, chunk, head;
     int per;   // pages per chunk
     int slot;  // of this item, where its tile has several chunks
-    Seq s;
+    int first, n, len;  // of its sequence
 };
 
 // inclusive scan over the wave, on the data-parallel lane moves (no LDS)
@@ -97,38 +97,31 @@ __device__ __forceinline__ int wave_scan(int v) {
 // tiles from the last (which sees the most keys) to the first, of each its chunks, of each the heads
 // (consecutive workgroups go to different XCDs: with 8 heads one XCD reads one head's keys).  Every
 // wave works it out for itself, 64 sequences at a time, one to a lane.
-__device__ __forceinline__ bool find_item(const Args& a, int rows, Item& it) {
-    const int id = blockIdx.x, lane = threadIdx.x & 63;
-    Seq mine{};
-    int tiles = 0;
+__device__ __forceinline__ bool find_item(const Args& a, int id, int rows, Item& it) {
+    const int lane = threadIdx.x & 63;
     int64_t cost = 0;
     for (int64_t b = lane; b < a.B; b += 64) {
-        mine = sequence(a, b);
-        tiles = (int)(((int64_t)mine.n * a.group + rows - 1) / rows);
-        cost += (int64_t)tiles * mine.pages;
+        const Seq s = sequence(a, b);
+        cost += (int64_t)(int)(((int64_t)s.n * a.group + rows - 1) / rows) * s.pages;
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) cost += __shfl_xor(cost, o);
-    const int per = (int)max(a.least, (cost * a.heads + a.target - 1) / a.target);
+    cost = cost * a.heads + a.target - 1;
+    const int even = cost >> 32 ? (int)(cost / a.target) : (int)((uint32_t)cost / (uint32_t)a.target);
+    const int per = max((int)a.least, even);
     int items_before = 0, slots_before = 0;
     for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
         const int64_t b = b0 + lane;
-        int items = 0, parts = 0, chunks = 1;
-        if (b < a.B) {
-            if (a.B > 64) {
-                mine = sequence(a, b);
-                tiles = (int)(((int64_t)mine.n * a.group + rows - 1) / rows);
-            }
-            chunks = max(1, (mine.pages + per - 1) / per);
-            items = tiles * chunks * a.heads;
-            parts = a.always_partial || chunks > 1 ? items : 0;
-        }
+        // lanes past the last sequence read it again, and count nothing
+        const Seq s = sequence(a, min(b, a.B - 1));
+        int tiles = (int)(((int64_t)s.n * a.group + rows - 1) / rows), chunks = max(1, (s.pages + per - 1) / per);
+        const int items = b < a.B ? tiles * chunks * a.heads : 0, parts = a.always_partial || chunks > 1 ? items : 0;
         const int to = items_before + wave_scan(items), from = to - items;
         const int slots_to = slots_before + wave_scan(parts);
         const uint64_t here = __ballot(id >= from && id < to);
         if (here) {
             const int l = __builtin_ctzll(here);
-            const int at = id - __builtin_amdgcn_readlane(from, l), first = __builtin_amdgcn_readlane(slots_to - parts, l);
+            const int at = id - __builtin_amdgcn_readlane(from, l), slot = __builtin_amdgcn_readlane(slots_to - parts, l);
             chunks = __builtin_amdgcn_readlane(chunks, l);
             tiles = __builtin_amdgcn_readlane(tiles, l);
             it.b = (int)b0 + l;
@@ -138,12 +131,14 @@ __device__ __forceinline__ bool find_item(const Args& a, int rows, Item& it) {
             it.tile = tiles - 1 - rest / chunks;
             it.per = per;
             // slots go by tile, chunk and head, whatever order the items have
-            it.slot = first + (it.tile * chunks + it.chunk) * a.heads + it.head;
-            it.s.first = __builtin_amdgcn_readlane(mine.first, l);
-            it.s.n = __builtin_amdgcn_readlane(mine.n, l);
-            it.s.len = __builtin_amdgcn_readlane(mine.len, l);
-            it.s.pages = __builtin_amdgcn_readlane(mine.pages, l);
-            if (at == 0 && threadIdx.x == 0) a.info[it.b] = int4{first, per, chunks, 0};
+            it.slot = slot + (it.tile * chunks + it.chunk) * a.heads + it.head;
+            it.first = __builtin_amdgcn_readlane(s.first, l);
+            it.n = __builtin_amdgcn_readlane(s.n, l);
+            it.len = __builtin_amdgcn_readlane(s.len, l);
+            // a store that is known to be global: a flat one would make every later wait a full one
+            if (at == 0 && threadIdx.x == 0)
+                *(__attribute__((address_space(1))) u32x4*)(uintptr_t)(a.info + it.b) =
+                    u32x4{(uint32_t)slot, (uint32_t)per, (uint32_t)chunks, 0u};
             return true;
         }
         items_before = __builtin_amdgcn_readlane(to, 63);
@@ -154,10 +149,10 @@ __device__ __forceinline__ bool find_item(const Args& a, int rows, Item& it) {
 }
 
 // Keys that some query of the tile sees.
-__device__ __forceinline__ int tile_keys(const Args& a, const Seq& s, int tile, int rows) {
-    if (!a.kv_len) return s.len;
-    const int last = (int)min((int64_t)s.n - 1, ((int64_t)tile * rows + rows - 1) / a.group);
-    return min(s.len, max(s.len - s.n + last + 1, 0));
+__device__ __forceinline__ int tile_keys(const Args& a, int n, int len, int tile, int rows) {
+    if (!a.kv_len) return len;
+    const int last = (int)min((int64_t)n - 1, ((int64_t)tile * rows + rows - 1) / a.group);
+    return min(len, max(len - n + last + 1, 0));
 }
 __device__ __forceinline__ int tile_chunks(int keys, int per) {
     return max(1, ((keys + kKvPage - 1) / kKvPage + per - 1) / per);
@@ -270,7 +265,7 @@ __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
         list.x = (int)(ordinal + run);
         while (true) {
             const int64_t weight = w.of(tile), piece = ordinal + run;
-            const int pages = (tile_keys(a, s, tile, rows) + kKvPage - 1) / kKvPage;
+            const int pages = (tile_keys(a, s.n, s.len, tile, rows) + kKvPage - 1) / kKvPage;
             const int lo = cut_page(x0 - x, weight, pages), hi = cut_page(x1 - x, weight, pages);
             if (ordinal >= a.tiles_most) break;  // q_start out of order
             const int slot = (int)(2 * run) + (x > x0 ? 1 : 0);
@@ -408,39 +403,43 @@ __device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x
 // Tiles of 16 rows.  Bound by HBM: each wave takes pages of the chunk in turn, its codes straight to
 // registers (V of a unit and K of the next in flight while the unit's scores are worked on), and
 // the four waves' sums meet in LDS at the end.
+constexpr int kDecodeRows = 16;
 template <int FMT, int D>
-__global__ __launch_bounds__(256) void decode_kernel(const Args a) {
+constexpr int decode_lds = 4 * kDecodeRows * (D + 4) * 4 + 8 * kDecodeRows * 4;
+
+template <int FMT, int D>
+__device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
     using B = KvBlock<FMT, D>;
-    constexpr int E = B::E, R = 16, UNITS = kKvPage / (4 * E), TILES = E / 4, KC = D / (4 * E), NB = D / 16;
+    constexpr int E = B::E, R = kDecodeRows, UNITS = kKvPage / (4 * E), TILES = E / 4, KC = D / (4 * E), NB = D / 16;
     constexpr int LOADS = NB;  // chunks of K, and of V, in a unit
     static_assert(TILES * KC == LOADS, "");
     constexpr int PITCH = D + 4;
-    __shared__ __attribute__((aligned(16))) float sums[4][R][PITCH];
-    __shared__ float ml[4][2][R];
+    float(*sums)[R][PITCH] = reinterpret_cast<float(*)[R][PITCH]>(lds);
+    float(*ml)[2][R] = reinterpret_cast<float(*)[2][R]>(lds + 4 * R * PITCH * 4);
 
     Item it;
-    if (!find_item(a, R, it)) return;
+    if (!find_item(a, id, R, it)) return;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int q = lane & 15, G = lane >> 4;
-    const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
+    const int keys = tile_keys(a, it.n, it.len, it.tile, R), chunks = tile_chunks(keys, it.per);
     if (it.chunk >= chunks) return;
     const bool partial = a.always_partial || chunks > 1;
     if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
 
     // this lane's query
     const int64_t row = (int64_t)it.tile * R + q;
-    const int rows_here = (int)min((int64_t)R, (int64_t)it.s.n * a.group - (int64_t)it.tile * R);
+    const int rows_here = (int)min((int64_t)R, (int64_t)it.n * a.group - (int64_t)it.tile * R);
     const int64_t rr = q < rows_here ? row : row - q;
     const int qi = (int)(rr / a.group), qh = it.head * a.group + (int)(rr % a.group);
-    const __bf16* qp = a.Q + (int64_t)(it.s.first + qi) * a.q_stride + (int64_t)qh * D;
+    const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
     u32x4 qf[D / 32];
 #pragma unroll
     for (int c = 0; c < KC; ++c)
 #pragma unroll
         for (int j = 0; j < E / 8; ++j) qf[c * (E / 8) + j] = ld16(qp + 4 * E * c + E * G + 8 * j);
-    const int lim = a.kv_len ? it.s.len - it.s.n + qi : it.s.len - 1;
+    const int lim = a.kv_len ? it.len - it.n + qi : it.len - 1;
     // the first query of the tile sees the fewest keys
-    const int lim_min = a.kv_len ? it.s.len - it.s.n + (int)((int64_t)it.tile * R / a.group) : it.s.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + (int)((int64_t)it.tile * R / a.group) : it.len - 1;
 
     f32x4 acc[NB];
 #pragma unroll
@@ -459,28 +458,35 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
         return head_base + (int64_t)__builtin_amdgcn_readlane(ids, k % 64) * page_bytes;
     };
     u32x4 kf[LOADS], vf[LOADS];
+    f32x4 ks[TILES];
     const int total = count * UNITS;
     const char* block = nullptr;
-    if (total > 0) {
-        block = block_of(0);
+    auto scales = [&](int at, int u, int t) __attribute__((always_inline)) {
+        return *reinterpret_cast<const f32x4*>(block + at + 4 * (4 * E * u + E * G + 4 * t));
+    };
+    auto fetch_k = [&](int un) __attribute__((always_inline)) {
+        const int u = un % UNITS;
+        if (u == 0) block = block_of(un / UNITS);
 #pragma unroll
-        for (int i = 0; i < LOADS; ++i) kf[i] = ld16_stream(block + i * kChunkBytes + lane * 16);
-    }
-    auto step = [&](int un, auto tag) __attribute__((always_inline)) {
-        constexpr bool MASK = decltype(tag)::value;
+        for (int i = 0; i < LOADS; ++i) kf[i] = ld16_stream(block + (u * LOADS + i) * kChunkBytes + lane * 16);
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) ks[t] = scales(B::KS, u, t);
+    };
+    if (total > 0) fetch_k(0);
+    // MORE is a constant: where the next loads were conditional the compiler's waits for V would have to
+    // cover the path without them, and so wait for them too
+    auto step = [&](int un, auto mask_tag, auto more_tag) __attribute__((always_inline)) {
+        constexpr bool MASK = decltype(mask_tag)::value, MORE = decltype(more_tag)::value;
         const int u = un % UNITS, page = page_lo + wave + 4 * (un / UNITS);
-        f32x4 kk[TILES], vs[TILES];
+        f32x4 vs[TILES], s[TILES], kk[TILES];
         int key0[TILES];
 #pragma unroll
-        for (int t = 0; t < TILES; ++t) {
-            const int o = 4 * E * u + E * G + 4 * t;
-            kk[t] = *reinterpret_cast<const f32x4*>(block + B::KS + 4 * o);
-            vs[t] = *reinterpret_cast<const f32x4*>(block + B::VS + 4 * o);
-            key0[t] = page * kKvPage + o;
-        }
-#pragma unroll
         for (int i = 0; i < LOADS; ++i) vf[i] = ld16_stream(block + B::PART + (u * LOADS + i) * kChunkBytes + lane * 16);
-        f32x4 s[TILES];
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) {
+            vs[t] = scales(B::VS, u, t);
+            key0[t] = page * kKvPage + 4 * E * u + E * G + 4 * t;
+        }
 #pragma unroll
         for (int t = 0; t < TILES; ++t) {
             s[t] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -489,19 +495,13 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 #pragma unroll
                 for (int j = 0; j < E / 8; ++j)
                     s[t] = mfma_chunk<__bf16>(frag<FMT>(kf[t * KC + c], j), qf[c * (E / 8) + j], s[t]);
+            kk[t] = ks[t] * a.sl2;
         }
-        if (un + 1 < total) {
-            const int nu = (un + 1) % UNITS;
-            if (nu == 0) block = block_of((un + 1) / UNITS);
-#pragma unroll
-            for (int i = 0; i < LOADS; ++i) kf[i] = ld16_stream(block + (nu * LOADS + i) * kChunkBytes + lane * 16);
-        }
-#pragma unroll
-        for (int t = 0; t < TILES; ++t) kk[t] *= a.sl2;
+        if constexpr (MORE) fetch_k(un + 1);
         u32x4 pf[TILES / 2];
         softmax_unit<TILES, D, MASK>(s, kk, vs, key0, lim, st, acc, pf);
-        if (MASK) {
-            const int keep = it.s.len - (page * kKvPage + 4 * E * u + E * G);
+        if constexpr (MASK) {
+            const int keep = it.len - (page * kKvPage + 4 * E * u + E * G);
 #pragma unroll
             for (int i = 0; i < LOADS; ++i) vf[i] = keep_tokens<FMT>(vf[i], keep);
         }
@@ -510,11 +510,14 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
 #pragma unroll
             for (int j = 0; j < E / 8; ++j) acc[n] = mfma_chunk<__bf16>(frag<FMT>(vf[n], j), pf[j], acc[n]);
     };
-    // pages that every query of the tile sees whole, then those that a mask cuts
+    // pages that every query of the tile sees whole, then those that a mask cuts, then the last unit
+    const std::true_type yes{};
+    const std::false_type no{};
     const int whole_pages = (lim_min + 1) / kKvPage - page_lo;
-    const int whole = min(whole_pages > wave ? (whole_pages - wave + 3) / 4 : 0, count) * UNITS;
-    for (int un = 0; un < whole; ++un) step(un, std::false_type{});
-    for (int un = whole; un < total; ++un) step(un, std::true_type{});
+    const int whole = min((whole_pages > wave ? (whole_pages - wave + 3) / 4 : 0) * UNITS, total - 1);
+    for (int un = 0; un < whole; ++un) step(un, no, yes);
+    for (int un = max(whole, 0); un < total - 1; ++un) step(un, yes, yes);
+    if (total > 0) step(total - 1, yes, no);
 
     // the four waves' sums
     const float l = sum_lane_groups(st.l);
@@ -548,12 +551,12 @@ __global__ __launch_bounds__(256) void decode_kernel(const Args a) {
             if (x == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{lt, m, 0.f, 0.f};
         } else {
             const int i_q = (int)(ro / a.group);
-            const bool none = a.kv_len && it.s.len - it.s.n + i_q < 0;  // no key at all: zero
+            const bool none = a.kv_len && it.len - it.n + i_q < 0;  // no key at all: zero
             const float inv = none ? 0.f : 1.0f / lt;
             uint32_t pk[PER / 2];
 #pragma unroll
             for (int e = 0; e < PER / 2; ++e) pk[e] = none ? 0u : pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-            const int64_t oh = (int64_t)(it.s.first + i_q) * a.heads * a.group + it.head * a.group + ro % a.group;
+            const int64_t oh = (int64_t)(it.first + i_q) * a.heads * a.group + it.head * a.group + ro % a.group;
             *reinterpret_cast<u32x4*>(a.out + oh * D + x) = u32x4{pk[0], pk[1], pk[2], pk[3]};
         }
     }
@@ -577,7 +580,7 @@ __device__ __forceinline__ void store_rows(const Args& a, const Item& it, int ro
     const int qi = (int)(row / a.group);
     const bool none = lim < 0;  // no key at all: zero
     const float inv = 1.0f / l;
-    const int64_t oh = (int64_t)(it.s.first + qi) * a.heads * a.group + it.head * a.group + row % a.group;
+    const int64_t oh = (int64_t)(it.first + qi) * a.heads * a.group + it.head * a.group + row % a.group;
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) {
         const uint2 v = {pack_bf16(acc[n][0] * inv, acc[n][1] * inv), pack_bf16(acc[n][2] * inv, acc[n][3] * inv)};
@@ -589,26 +592,29 @@ __device__ __forceinline__ void store_rows(const Args& a, const Item& it, int ro
 // page goes through LDS as bf16 operands (two slots, the next one filled while a page is worked on)
 // and serves the tile's four waves.  bf16 codes are copied there directly; e4m3 codes go through
 // registers and are widened once for all waves.
+template <int D>
+constexpr int tile_lds = 2 * (2 * kKvPage * D * 2 + 8 * kKvPage);
+
 template <int FMT, int D, int QW>
-__global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
+__device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
     using B = KvBlock<FMT, D>;
     constexpr int E = B::E, J = E / 8, R = 64 * QW, TILES = 4, KC = D / (4 * E), NB = D / 16;
     constexpr int FRAGS = 2 * kKvPage * D * 2 / kChunkBytes;  // operands of a page, 1 KiB each: K's, then V's
     constexpr int CHUNKS = FRAGS / J;                         // of 1 KiB in the cache
     constexpr int SCALES = FRAGS * kChunkBytes;               // then K's and V's scales
     constexpr int STEP = SCALES + 8 * kKvPage;
-    __shared__ __attribute__((aligned(1024))) char smem[2 * STEP];
+    static_assert(2 * STEP == tile_lds<D>, "");
 
     Item it;
-    if (!find_item(a, R, it)) return;
+    if (!find_item(a, id, R, it)) return;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int q = lane & 15, G = lane >> 4;
-    const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
+    const int keys = tile_keys(a, it.n, it.len, it.tile, R), chunks = tile_chunks(keys, it.per);
     if (it.chunk >= chunks) return;
     const bool partial = a.always_partial || chunks > 1;
     if (partial && (it.slot < 0 || it.slot >= a.slots)) return;
 
-    const int64_t rows_all = (int64_t)it.s.n * a.group;
+    const int64_t rows_all = (int64_t)it.n * a.group;
     const int64_t row0 = (int64_t)it.tile * R + wave * QW * 16;  // the wave's first row
     u32x4 qf[QW][D / 32];
     int lim[QW];
@@ -616,12 +622,12 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     for (int f = 0; f < QW; ++f) {
         const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
         const int qi = (int)(row / a.group), qh = it.head * a.group + (int)(row % a.group);
-        const __bf16* qp = a.Q + (int64_t)(it.s.first + qi) * a.q_stride + (int64_t)qh * D;
+        const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
 #pragma unroll
         for (int c = 0; c < KC; ++c)
 #pragma unroll
             for (int j = 0; j < E / 8; ++j) qf[f][c * (E / 8) + j] = ld16(qp + 4 * E * c + E * G + 8 * j);
-        lim[f] = a.kv_len ? it.s.len - it.s.n + qi : it.s.len - 1;
+        lim[f] = a.kv_len ? it.len - it.n + qi : it.len - 1;
     }
 
     f32x4 acc[QW][NB];
@@ -715,7 +721,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
 #pragma unroll
             for (int c = 0; c < G4; ++c) {
                 const int at = v * G4 + c, n = at / J % NB, u = at / J / NB, j = at % J;
-                if (MASK) fr[v & 1][c] = keep_tokens<kKvBf16>(fr[v & 1][c], it.s.len - (base + 4 * E * u + E * G + 8 * j));
+                if (MASK) fr[v & 1][c] = keep_tokens<kKvBf16>(fr[v & 1][c], it.len - (base + 4 * E * u + E * G + 8 * j));
 #pragma unroll
                 for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[v & 1][c], pf[f][u * J + j], acc[f][n]);
             }
@@ -724,7 +730,7 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
     };
     // pages that every query of the tile sees whole, then those that a mask cuts
     const int64_t tile_row = (int64_t)it.tile * R;
-    const int lim_min = a.kv_len ? it.s.len - it.s.n + (int)(tile_row / a.group) : it.s.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + (int)(tile_row / a.group) : it.len - 1;
     const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
     for (int k = 0; k < whole; ++k) step(k, std::false_type{});
     for (int k = whole; k < count; ++k) step(k, std::true_type{});
@@ -732,6 +738,35 @@ __global__ __launch_bounds__(256, 2) void tile_kernel(const Args a) {
 #pragma unroll
     for (int f = 0; f < QW; ++f)
         store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, partial ? it.slot : kWhole, lim[f], st[f], acc[f]);
+}
+
+// Items of `rows` query rows: 16, 64 or 128.
+template <int FMT, int D, int ROWS>
+__device__ __forceinline__ void item(const Args& a, int id, char* lds) {
+    if constexpr (ROWS == kDecodeRows)
+        decode_item<FMT, D>(a, id, lds);
+    else
+        tile_item<FMT, D, ROWS / 64>(a, id, lds);
+}
+template <int FMT, int D, int ROWS>
+constexpr int item_lds = ROWS == kDecodeRows ? decode_lds<FMT, D> : tile_lds<D>;
+
+template <int FMT, int D, int ROWS>
+__global__ __launch_bounds__(256, 2) void cache_kernel(const Args a) {
+    __shared__ __attribute__((aligned(1024))) char lds[item_lds<FMT, D, ROWS>];
+    item<FMT, D, ROWS>(a, blockIdx.x, lds);
+}
+
+// The shared prefix in tiles of ROWS rows and each sequence's own keys in tiles of 16, side by side in
+// one launch: either alone leaves most of the chip idle.
+template <int FMT, int D, int ROWS>
+__global__ __launch_bounds__(256, 2) void shared_kernel(const Args prefix, const Args own, int prefix_items) {
+    constexpr int LDS = item_lds<FMT, D, ROWS> > decode_lds<FMT, D> ? item_lds<FMT, D, ROWS> : decode_lds<FMT, D>;
+    __shared__ __attribute__((aligned(1024))) char lds[LDS];
+    if ((int)blockIdx.x < prefix_items)
+        item<FMT, D, ROWS>(prefix, blockIdx.x, lds);
+    else
+        decode_item<FMT, D>(own, blockIdx.x - prefix_items, lds);
 }
 
 // Tiles of 8 waves x 32 rows, two waves to a SIMD.  A page is an exponential phase (mask, maximum,
@@ -774,12 +809,12 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         count = __builtin_amdgcn_readfirstlane(p.hi) - page_lo;
         slot = __builtin_amdgcn_readfirstlane(p.slot);
         const Seq s = sequence(a, it.b);
-        it.s.first = __builtin_amdgcn_readfirstlane(s.first);
-        it.s.n = __builtin_amdgcn_readfirstlane(s.n);
-        it.s.len = __builtin_amdgcn_readfirstlane(s.len);
+        it.first = __builtin_amdgcn_readfirstlane(s.first);
+        it.n = __builtin_amdgcn_readfirstlane(s.n);
+        it.len = __builtin_amdgcn_readfirstlane(s.len);
     } else {
-        if (!find_item(a, R, it)) return;
-        const int keys = tile_keys(a, it.s, it.tile, R), chunks = tile_chunks(keys, it.per);
+        if (!find_item(a, blockIdx.x, R, it)) return;
+        const int keys = tile_keys(a, it.n, it.len, it.tile, R), chunks = tile_chunks(keys, it.per);
         if (it.chunk >= chunks) return;
         int page_hi;
         chunk_pages(keys, chunks, it.chunk, page_lo, page_hi);
@@ -788,7 +823,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     }
     if (slot == kNone || slot >= a.slots) continue;
 
-    const int64_t rows_all = (int64_t)it.s.n * a.group;
+    const int64_t rows_all = (int64_t)it.n * a.group;
     const int64_t tile_row = (int64_t)it.tile * R, row0 = tile_row + wave * QW * 16;  // the wave's first row
     u32x4 qf[QW][DC];
     int lim[QW];
@@ -796,10 +831,10 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     for (int f = 0; f < QW; ++f) {
         const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
         const int qi = (int)(row / a.group), qh = it.head * a.group + (int)(row % a.group);
-        const __bf16* qp = a.Q + (int64_t)(it.s.first + qi) * a.q_stride + (int64_t)qh * D;
+        const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
 #pragma unroll
         for (int c = 0; c < DC; ++c) qf[f][c] = ld16(qp + 4 * E * (c / J) + E * G + 8 * (c % J));
-        lim[f] = a.kv_len ? it.s.len - it.s.n + qi : it.s.len - 1;
+        lim[f] = a.kv_len ? it.len - it.n + qi : it.len - 1;
     }
     f32x4 acc[QW][NB], s[QW][TILES];
     State st[QW];
@@ -905,7 +940,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
                     const int at = i * DC + c, n = at / J % NB, u = at / J / NB, j = at % J;
                     if (MASK)
                         fr[i & 1][c] = keep_tokens<kKvBf16>(
-                            fr[i & 1][c], it.s.len - ((page_lo + k) * kKvPage + 4 * E * u + E * G + 8 * j));
+                            fr[i & 1][c], it.len - ((page_lo + k) * kKvPage + 4 * E * u + E * G + 8 * j));
 #pragma unroll
                     for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[i & 1][c], pf[f][u * J + j], acc[f][n]);
                 } else {
@@ -961,7 +996,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         if (!LATE || more) meet();
     };
     // pages that every query of the tile sees whole, then those that a mask cuts
-    const int lim_min = a.kv_len ? it.s.len - it.s.n + (int)(tile_row / a.group) : it.s.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + (int)(tile_row / a.group) : it.len - 1;
     const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
     if (count > 0) {
         if (late) {
@@ -1049,7 +1084,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
                 count = list.y;
                 if (!shared.parts && count == 0) write = false;
             } else {
-                const int chunks = w ? plan.z : tile_chunks(tile_keys(a, s, tile, set.rows), max(plan.y, 1));
+                const int chunks = w ? plan.z : tile_chunks(tile_keys(a, s.n, s.len, tile, set.rows), max(plan.y, 1));
                 if (!shared.parts && chunks == 1) write = false;
                 first = plan.x + tile * plan.z * a.heads + h;
                 count = chunks;
@@ -1105,19 +1140,34 @@ template <int FMT, int D>
 hipError_t launch(const Args& a, int rows, int64_t grid, hipStream_t s) {
     const dim3 g((unsigned)grid);
     if (rows == 16)
-        decode_kernel<FMT, D><<<g, 256, 0, s>>>(a);
+        cache_kernel<FMT, D, 16><<<g, 256, 0, s>>>(a);
     else if (rows == 64)
-        tile_kernel<FMT, D, 1><<<g, 256, 0, s>>>(a);
+        cache_kernel<FMT, D, 64><<<g, 256, 0, s>>>(a);
     else if (rows == 128)
-        tile_kernel<FMT, D, 2><<<g, 256, 0, s>>>(a);
+        cache_kernel<FMT, D, 128><<<g, 256, 0, s>>>(a);
     else
         wide_kernel<FMT, D><<<g, 512, 0, s>>>(a);
     return hipGetLastError();
 }
-hipError_t launch_any(const KvPool& c, const Args& a, int rows, int64_t grid, hipStream_t s) {
-    if (c.format == kKvBf16)
-        return c.d == 64 ? launch<kKvBf16, 64>(a, rows, grid, s) : launch<kKvBf16, 128>(a, rows, grid, s);
-    return c.d == 64 ? launch<kKvFp8, 64>(a, rows, grid, s) : launch<kKvFp8, 128>(a, rows, grid, s);
+template <int FMT, int D>
+hipError_t launch_shared(const Args& prefix, int rows, int64_t prefix_grid, const Args& own, int64_t grid, hipStream_t s) {
+    const dim3 g((unsigned)(prefix_grid + grid));
+    if (rows == 16)
+        shared_kernel<FMT, D, 16><<<g, 256, 0, s>>>(prefix, own, (int)prefix_grid);
+    else if (rows == 64)
+        shared_kernel<FMT, D, 64><<<g, 256, 0, s>>>(prefix, own, (int)prefix_grid);
+    else
+        shared_kernel<FMT, D, 128><<<g, 256, 0, s>>>(prefix, own, (int)prefix_grid);
+    return hipGetLastError();
+}
+// calls f with the cache's format and d as constants
+template <class F>
+hipError_t with_format(const KvPool& c, F&& f) {
+    using std::integral_constant;
+    const integral_constant<int, 64> d64{};
+    const integral_constant<int, 128> d128{};
+    if (c.format == kKvBf16) return c.d == 64 ? f(integral_constant<int, kKvBf16>{}, d64) : f(integral_constant<int, kKvBf16>{}, d128);
+    return c.d == 64 ? f(integral_constant<int, kKvFp8>{}, d64) : f(integral_constant<int, kKvFp8>{}, d128);
 }
 
 }  // namespace ca
@@ -1149,6 +1199,7 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
         return ca::Set{a.info, a.parts, a.pieces, p.slots, p.rows};
     };
     ca::Set shared{};
+    ca::Args prefix{};
     if (prefix_pages > 0) {
         a.table = c.prefix_table;
         a.width = prefix_pages;
@@ -1156,8 +1207,7 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
         a.B = 1;
         a.always_partial = 1;
         shared = planned(w.prefix, w.prefix_info, w.prefix_parts, 0);
-        const hipError_t e = ca::launch_any(c.pool, a, w.prefix.rows, w.prefix.grid, s);
-        if (e != hipSuccess) return e;
+        prefix = a;
     }
     a.table = c.table;
     a.width = c.width;
@@ -1165,13 +1215,22 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
     a.kv_len = c.kv_len;
     a.B = c.B;
     const ca::Set own = planned(w.own, w.own_info, w.own_parts, w.own_runs);
-    hipError_t e;
+    hipError_t e = hipSuccess;
     if (a.pieces) {
         ca::plan_kernel<<<dim3((unsigned)((w.own.target + 63) / 64)), 64, 0, s>>>(a, w.own.rows);
         e = hipGetLastError();
-        if (e != hipSuccess) return e;
     }
-    e = ca::launch_any(c.pool, a, w.own.rows, w.own.grid, s);
+    if (e == hipSuccess)
+        e = ca::with_format(c.pool, [&](auto fmt, auto d) {
+            constexpr int F = decltype(fmt)::value, D = decltype(d)::value;
+            if (prefix_pages > 0 && w.own.rows == 16)
+                return ca::launch_shared<F, D>(prefix, w.prefix.rows, w.prefix.grid, a, w.own.grid, s);
+            if (prefix_pages > 0) {
+                const hipError_t first = ca::launch<F, D>(prefix, w.prefix.rows, w.prefix.grid, s);
+                if (first != hipSuccess) return first;
+            }
+            return ca::launch<F, D>(a, w.own.rows, w.own.grid, s);
+        });
     if (e != hipSuccess || w.own.slots == 0) return e;
     return c.pool.d == 64 ? ca::launch_merge<64>(a, own, shared, s) : ca::launch_merge<128>(a, own, shared, s);
 }

@@ -79,8 +79,10 @@ inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, 
                             bool prefix, bool always_partial) {
     CachePlan p;
     p.rows = rows;
-    p.target = rows == 16 ? 768 : rows == 256 ? 256 : 512;
-    p.least = rows == 16 ? 8 : 4;
+    // a prefix's tiles share the chip with the sequences' own keys, and its partial sums are the more the
+    // more it is cut
+    p.target = rows == 16 ? 768 : rows == 256 || prefix ? 256 : 512;
+    p.least = rows == 16 && !prefix ? 8 : 4;
     p.tiles = heads * std::min(T * group, T * group / rows + std::min(B, T));
     const int64_t most = (table_width + p.least - 1) / p.least;  // chunks of one tile
     p.in_runs = rows == 256 && !prefix && !always_partial && most > 1;
@@ -113,7 +115,9 @@ inline CacheWorkspace cache_workspace(int64_t T, int64_t B, int64_t heads, int64
     w.total = w.prefix_parts;
     w.prefix = CachePlan{};
     if (prefix_pages > 0) {
-        w.prefix = cache_plan(T, 1, heads, group, prefix_pages, cache_rows(T, 1, group), true, true);
+        // beside tiles of 16 rows the prefix's go without the second half of 256 rows
+        const int rows = cache_rows(T, 1, group);
+        w.prefix = cache_plan(T, 1, heads, group, prefix_pages, w.own.rows == 16 ? std::min(rows, 128) : rows, true, true);
         w.total += (size_t)w.prefix.slots * cache_slot_bytes(w.prefix.rows, d);
     }
     return w;
