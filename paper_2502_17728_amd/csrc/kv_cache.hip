@@ -316,114 +316,142 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
 struct ReadArgs {
     const char* pool;
     const int32_t* slots;
-    int64_t tokens, total_slots;
-    int heads, tile;
+    int64_t tokens, total_slots, k_blocks;
+    int heads;
     __bf16* K;
     __bf16* V;
 };
 
 // 8 codes as fp32
 template <int FMT>
-__device__ __forceinline__ void decode8(const char* p, float scale, float* f);
-template <>
-__device__ __forceinline__ void decode8<kKvBf16>(const char* p, float scale, float* f) {
-    widen<__bf16>(ld16(p), f);
+__device__ __forceinline__ void decode8(const u32x4& v, float scale, float* f) {
+    if constexpr (FMT == kKvBf16) {
+        widen<__bf16>(v, f);
 #pragma unroll
-    for (int j = 0; j < 8; ++j) f[j] *= scale;
-}
-template <>
-__device__ __forceinline__ void decode8<kKvFp8>(const char* p, float scale, float* f) {
-    const uint2 w = *reinterpret_cast<const uint2*>(p);
-    const uint32_t u[2] = {w.x, w.y};
+        for (int j = 0; j < 8; ++j) f[j] *= scale;
+    } else {
+        const uint32_t u[2] = {v.x, v.y};
 #pragma unroll
-    for (int j = 0; j < 2; ++j) {
-        const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(u[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u[j], true);
-        f[4 * j] = lo[0] * scale;
-        f[4 * j + 1] = lo[1] * scale;
-        f[4 * j + 2] = hi[0] * scale;
-        f[4 * j + 3] = hi[1] * scale;
+        for (int j = 0; j < 2; ++j) {
+            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(u[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(u[j], true);
+            f[4 * j] = lo[0] * scale;
+            f[4 * j + 1] = lo[1] * scale;
+            f[4 * j + 2] = hi[0] * scale;
+            f[4 * j + 3] = hi[1] * scale;
+        }
     }
 }
 
-// append_kernel's way back: codes of `tile` slots into LDS rows, then whole rows out.
+// 4 words of bytes (rows) -> 4 words of bytes (columns); 2 x 2 halves of two words
+__device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
+    const uint32_t a = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), b = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+    const uint32_t c = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), d = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(b, a, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(b, a, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(d, c, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(d, c, 0x07060302u);
+}
+
+// From blocks to rows, one item to a thread.  The first `k_blocks` workgroups read K, 16 bytes of a token
+// to a lane, tokens fastest (neighbours lie in neighbouring rows of a chunk).  The others read V: a
+// lane takes four dimensions of E tokens that lie together (64 bytes in a row), turns them in
+// registers and writes four dimensions of each token; tokens that do not lie together go one by one.
+// Runs of E tokens are counted from the first slot of the workgroup's tokens.
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
     using B = KvBlock<FMT, D>;
-    constexpr int E = B::E, PITCH = D * B::BYTES + 16;
-    __shared__ __attribute__((aligned(16))) char smem[2 * kTile * PITCH];
-    __shared__ int32_t slot_of[kTile];
-    __shared__ float scale_of[2][kTile];
+    constexpr int E = B::E, LANES = D / 4, RUNS = 256 / LANES, PIECES = D / E;
     const int tid = threadIdx.x;
-    const int h = blockIdx.x % a.heads;
-    const int64_t t0 = (int64_t)(blockIdx.x / a.heads) * a.tile;
-    const int n = (int)min((int64_t)a.tile, a.tokens - t0);
-    if (tid < 2 * kTile) {
-        const int t = tid % kTile;
-        int32_t s = -1;
-        if (t < n) s = a.slots[t0 + t];
-        if ((uint64_t)(int64_t)s >= (uint64_t)a.total_slots) s = -1;
-        float scale = 0.f;
-        if (s >= 0)
-            scale = reinterpret_cast<const float*>(a.pool + ((int64_t)(s / kKvPage) * a.heads + h) * B::SIZE +
-                                                   (tid < kTile ? B::KS : B::VS))[s % kKvPage];
-        scale_of[tid / kTile][t] = scale;
-        if (tid < kTile) slot_of[t] = s;
-    }
-    __syncthreads();
-    for (int i = tid; i < a.tile * (D / E); i += 256) {
-        const int t = i % a.tile, piece = i / a.tile;
-        if (t >= n) continue;
-        const int32_t slot = slot_of[t];
+    auto block_of = [&](int32_t slot, int h) { return a.pool + ((int64_t)(slot / kKvPage) * a.heads + h) * B::SIZE; };
+    auto inside = [&](int32_t slot) { return (uint64_t)(int64_t)slot < (uint64_t)a.total_slots; };
+    if ((int64_t)blockIdx.x < a.k_blocks) {
+        constexpr int TOKENS = 256 / PIECES;
+        const int h = blockIdx.x % a.heads;
+        const int64_t t = (int64_t)(blockIdx.x / a.heads) * TOKENS + tid % TOKENS;
+        const int piece = tid / TOKENS;
+        if (t >= a.tokens) return;
+        const int32_t slot = a.slots[t];
+        __bf16* out = a.K + (t * a.heads + h) * (int64_t)D + piece * E;
         u32x4 v = {0, 0, 0, 0};
-        if (slot >= 0)
-            v = ld16(a.pool + ((int64_t)(slot / kKvPage) * a.heads + h) * B::SIZE + B::k_at(slot % kKvPage, piece * E));
-        *reinterpret_cast<u32x4*>(smem + t * PITCH + piece * 16) = v;
-    }
-    const int shift = slot_of[0] < 0 ? 0 : slot_of[0] % E;
-    const int runs = (n + shift + E - 1) / E;
-    char* vs = smem + kTile * PITCH;
-    for (int i = tid; i < runs * D; i += 256) {
-        const int x = i % D, t = i / D * E - shift;
-        bool whole = t >= 0 && t + E <= n;
-        const int32_t first = whole ? slot_of[t] : -1;
-        whole = whole && first >= 0 && first % E == 0;
-        if (whole)
-            for (int r = 1; r < E; ++r) whole = whole && slot_of[t + r] == first + r;
-        if (whole) {
-            union {
-                u32x4 v;
-                uint8_t b[16];
-                uint16_t s[8];
-            } c;
-            c.v = ld16(a.pool + ((int64_t)(first / kKvPage) * a.heads + h) * B::SIZE + B::PART +
-                       B::v_at(first % kKvPage, x));
+        float scale = 0.f;
+        if (inside(slot)) {
+            const char* block = block_of(slot, h);
+            v = ld16(block + B::k_at(slot % kKvPage, piece * E));
+            scale = reinterpret_cast<const float*>(block + B::KS)[slot % kKvPage];
+        }
 #pragma unroll
-            for (int r = 0; r < E; ++r) {
-                if constexpr (FMT == kKvBf16)
-                    *reinterpret_cast<uint16_t*>(vs + (t + r) * PITCH + x * 2) = c.s[r];
-                else
-                    *reinterpret_cast<uint8_t*>(vs + (t + r) * PITCH + x) = c.b[r];
-            }
-        } else {
-            for (int r = 0; r < E; ++r) {
-                if (t + r < 0 || t + r >= n) continue;
-                const int32_t slot = slot_of[t + r];
-                const char* at = a.pool + ((int64_t)(slot / kKvPage) * a.heads + h) * B::SIZE + B::PART +
-                                 B::v_at(slot % kKvPage, x);
-                if constexpr (FMT == kKvBf16)
-                    *reinterpret_cast<uint16_t*>(vs + (t + r) * PITCH + x * 2) =
-                        slot < 0 ? (uint16_t)0 : *reinterpret_cast<const uint16_t*>(at);
-                else
-                    vs[(t + r) * PITCH + x] = slot < 0 ? 0 : *at;
+        for (int j = 0; j < E / 8; ++j) {
+            float f[8];
+            decode8<FMT>(j ? u32x4{v.z, v.w, 0, 0} : v, scale, f);
+            *reinterpret_cast<u32x4*>(out + 8 * j) = narrow<__bf16>(f);
+        }
+        return;
+    }
+    const int id = blockIdx.x - (int)a.k_blocks, h = id % a.heads;
+    constexpr int TOKENS = (RUNS - 1) * E;  // with a first run cut short these are RUNS runs
+    const int64_t t0 = (int64_t)(id / a.heads) * TOKENS;
+    const int n = (int)min((int64_t)TOKENS, a.tokens - t0);
+    const int32_t start = a.slots[t0];
+    const int x = tid % LANES * 4, lane_r = tid % LANES, t = tid / LANES * E - (inside(start) ? start % E : 0);
+    // each lane of a run looks at one of its slots
+    int32_t mine = -1;
+    if (lane_r < E && t + lane_r >= 0 && t + lane_r < n) mine = a.slots[t0 + t + lane_r];
+    const int32_t first = __shfl(mine, 0, LANES);
+    const bool fits = lane_r >= E || (first >= 0 && first % E == 0 && mine == first + lane_r && inside(mine));
+    const uint64_t all = __ballot(fits) >> ((tid & 63) / LANES * LANES);
+    constexpr uint64_t RUN = LANES == 32 ? 0xffffffffull : 0xffffull;
+    if (t >= n) return;
+    const int64_t step = (int64_t)a.heads * D;
+    __bf16* out = a.V + ((t0 + t) * a.heads + h) * (int64_t)D + x;
+    if ((all & RUN) == RUN) {
+        const char* block = block_of(first, h);
+        const int o = first % kKvPage;
+        u32x4 v[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = ld16(block + B::PART + B::v_at(o, x) + 16 * k);
+#pragma unroll
+        for (int q = 0; q < E / 4; ++q) {  // four tokens
+            const f32x4 scale = *reinterpret_cast<const f32x4*>(block + B::VS + 4 * (o + 4 * q));
+            if constexpr (FMT == kKvFp8) {
+                uint32_t w[4] = {v[0][q], v[1][q], v[2][q], v[3][q]};
+                transpose_bytes(w);
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[r], false);
+                    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[r], true);
+                    *reinterpret_cast<uint2*>(out + (4 * q + r) * step) =
+                        uint2{pack_bf16(lo[0] * scale[r], lo[1] * scale[r]), pack_bf16(hi[0] * scale[r], hi[1] * scale[r])};
+                }
+            } else {
+#pragma unroll
+                for (int r = 0; r < 4; ++r) {
+                    const int w = 2 * q + r / 2;  // the word of each dimension that holds the token
+                    float f[4];
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) f[k] = (r & 1 ? bf_hi(v[k][w]) : bf_lo(v[k][w])) * scale[r];
+                    *reinterpret_cast<uint2*>(out + (4 * q + r) * step) = uint2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
+                }
             }
         }
+        return;
     }
-    __syncthreads();
-    for (int i = tid; i < 2 * n * (D / 8); i += 256) {
-        const int x = i % (D / 8) * 8, row = i / (D / 8), is_v = row >= n, t = is_v ? row - n : row;
-        float f[8];
-        decode8<FMT>(smem + (is_v ? kTile * PITCH : 0) + t * PITCH + x * B::BYTES, scale_of[is_v][t], f);
-        *reinterpret_cast<u32x4*>((is_v ? a.V : a.K) + ((t0 + t) * a.heads + h) * (int64_t)D + x) = narrow<__bf16>(f);
+    for (int r = 0; r < E; ++r) {
+        if (t + r < 0 || t + r >= n) continue;
+        const int32_t slot = a.slots[t0 + t + r];
+        float f[4] = {0.f, 0.f, 0.f, 0.f};
+        if (inside(slot)) {
+            const char* block = block_of(slot, h);
+            const char* at = block + B::PART + B::v_at(slot % kKvPage, x);
+            const float scale = reinterpret_cast<const float*>(block + B::VS)[slot % kKvPage];
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                if constexpr (FMT == kKvBf16)
+                    f[k] = bf_lo(*reinterpret_cast<const uint16_t*>(at + 16 * k)) * scale;
+                else
+                    f[k] = __builtin_amdgcn_cvt_pk_f32_fp8(*reinterpret_cast<const uint8_t*>(at + 16 * k), false)[0] * scale;
+            }
+        }
+        *reinterpret_cast<uint2*>(out + r * step) = uint2{pack_bf16(f[0], f[1]), pack_bf16(f[2], f[3])};
     }
 }
 
@@ -478,22 +506,20 @@ hipError_t launch_kv_append(const void* qkv, int64_t stride, const int32_t* slot
     return hipGetLastError();
 }
 
-hipError_t launch_kv_read(const KvPool& c, const int32_t* slots, int64_t tokens, void* K, void* V, hipStream_t s) {
-    kv::ReadArgs a{(const char*)c.data, slots, tokens, c.pages * kKvPage, (int)c.heads,
-                   kv::tile_tokens(tokens, c.heads), (__bf16*)K, (__bf16*)V};
-    const dim3 grid((unsigned)((tokens + a.tile - 1) / a.tile * c.heads));
-    if (c.format == kKvBf16) {
-        if (c.d == 64)
-            kv::read_kernel<kKvBf16, 64><<<grid, 256, 0, s>>>(a);
-        else
-            kv::read_kernel<kKvBf16, 128><<<grid, 256, 0, s>>>(a);
-    } else {
-        if (c.d == 64)
-            kv::read_kernel<kKvFp8, 64><<<grid, 256, 0, s>>>(a);
-        else
-            kv::read_kernel<kKvFp8, 128><<<grid, 256, 0, s>>>(a);
-    }
+template <int FMT, int D>
+static hipError_t launch_read(kv::ReadArgs a, hipStream_t s) {
+    using B = KvBlock<FMT, D>;
+    const int64_t k_tokens = 256 / (D / B::E), v_tokens = (256 / (D / 4) - 1) * B::E;
+    a.k_blocks = (a.tokens + k_tokens - 1) / k_tokens * a.heads;
+    const int64_t v_blocks = (a.tokens + v_tokens - 1) / v_tokens * a.heads;
+    kv::read_kernel<FMT, D><<<dim3((unsigned)(a.k_blocks + v_blocks)), 256, 0, s>>>(a);
     return hipGetLastError();
+}
+
+hipError_t launch_kv_read(const KvPool& c, const int32_t* slots, int64_t tokens, void* K, void* V, hipStream_t s) {
+    const kv::ReadArgs a{(const char*)c.data, slots, tokens, c.pages * kKvPage, 0, (int)c.heads, (__bf16*)K, (__bf16*)V};
+    if (c.format == kKvBf16) return c.d == 64 ? launch_read<kKvBf16, 64>(a, s) : launch_read<kKvBf16, 128>(a, s);
+    return c.d == 64 ? launch_read<kKvFp8, 64>(a, s) : launch_read<kKvFp8, 128>(a, s);
 }
 
 }  // namespace dn
