@@ -607,17 +607,20 @@ def _rows(t: torch.Tensor, name: str):
     """Pointer and token stride of t[T, H, d] (or [T, width]) whose tokens' values lie together."""
     if not t.is_cuda:
         raise ValueError(f"{name} must be a GPU tensor")
+    T = t.shape[0]
+    if t.is_contiguous() and T:
+        return t.data_ptr(), t.numel() // T
     st, n = t.stride(), 1
     for k in range(t.dim() - 1, 0, -1):
         if st[k] != n and t.shape[k] != 1:
             raise ValueError(f"{name} must be contiguous within a token")
         n *= t.shape[k]
-    return t.data_ptr(), (max(st[0], n) if t.shape[0] != 1 else n)
+    return t.data_ptr(), (max(st[0], n) if T != 1 else n)
 
 
 def _int32(t: torch.Tensor, name: str, shape, x: torch.Tensor):
     """Pointer of an int32 index tensor of this shape on x's device."""
-    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype == torch.int32 and t.is_contiguous()
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.shape == shape and t.is_contiguous()
             and t.get_device() == x.get_device()):
         _expect(t, name, shape, torch.int32, x.device)
         if not t.is_contiguous():
@@ -627,10 +630,19 @@ def _int32(t: torch.Tensor, name: str, shape, x: torch.Tensor):
 
 def _table_of(table: torch.Tensor, x: torch.Tensor):
     """Pointer, positions and turned dimensions of a rotary table."""
-    if not (isinstance(table, torch.Tensor) and table.dim() == 3 and table.shape[2] == 2 and
-            table.dtype == torch.float32 and table.get_device() == x.get_device()):
-        _expect(table, "table", (None, None, 2), torch.float32, x.device)
+    if isinstance(table, torch.Tensor) and table.dim() == 3:
+        rows, half, two = table.shape
+        if two == 2 and table.dtype is torch.float32 and table.get_device() == x.get_device() and table.is_contiguous():
+            return table.data_ptr(), rows, 2 * half
+    _expect(table, "table", (None, None, 2), torch.float32, x.device)
     return _dev(table, "table"), table.shape[0], 2 * table.shape[1]
+
+
+def _stream_of(stream, x: torch.Tensor) -> int:
+    """The stream given, or the current one of x's device."""
+    if stream is None and _raw_stream is not None:
+        return _raw_stream(x.get_device())
+    return _stream(stream)
 
 
 def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False,
@@ -644,11 +656,15 @@ def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, 
     tp, rows, rot = _table_of(table, x)
     if out is None:
         out = x.new_empty((T, H, d))
-    elif not _like(out, x.shape, x):
-        _expect(out, "out", (T, H, d), x.dtype, x.device)
-    op, os_ = _rows(out, "out")
-    _check("rotary_apply", _lib.rotary_apply(xp, xs, _int32(positions, "positions", (T,), x), tp, rows, T, H, d, rot,
-                                             int(interleaved), int(inverse), _dt(x), op, os_, _stream(stream)))
+        op, os_ = out.data_ptr(), H * d
+    else:
+        if not _like(out, x.shape, x):
+            _expect(out, "out", (T, H, d), x.dtype, x.device)
+        op, os_ = _rows(out, "out")
+    st = _lib.rotary_apply(xp, xs, _int32(positions, "positions", (T,), x), tp, rows, T, H, d, rot, interleaved, inverse,
+                           _dt(x), op, os_, _stream_of(stream, x))
+    if st:
+        raise DNError("rotary_apply", st)
     return out
 
 
@@ -659,6 +675,9 @@ class KVCache:
     page s // 64; which pages hold which sequence is the caller's."""
     data: torch.Tensor
     desc: KVCacheDesc
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.desc)
 
     @property
     def pages(self):
@@ -728,20 +747,25 @@ def kv_cache_append(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, posi
         raise ValueError(f"rows of {width} values do not hold a multiple of {heads} query heads and 2 x {heads} key and "
                          f"value heads of {d}")
     qp, qs = _rows(qkv, "qkv")
+    op = None
     if q_heads == 0:
         if q_out is not None:
             raise ValueError("the rows hold no queries")
     elif q_out is None:
         q_out = qkv.new_empty((T, q_heads, d))
-    elif not _like(q_out, (T, q_heads, d), qkv):
-        _expect(q_out, "q_out", (T, q_heads, d), qkv.dtype, qkv.device)
+        op = q_out.data_ptr()
+    else:
+        if not _like(q_out, (T, q_heads, d), qkv):
+            _expect(q_out, "q_out", (T, q_heads, d), qkv.dtype, qkv.device)
+        op = _dev(q_out, "q_out")
     tp, rows, rot, pp = None, 0, 0, None
     if table is not None:
         tp, rows, rot = _table_of(table, qkv)
         pp = _int32(positions, "positions", (T,), qkv)
-    _check("kv_cache_append", _lib.kv_cache_append(
-        ctypes.byref(desc), qp, qs, _int32(slots, "slots", (T,), qkv), pp, tp, rows, rot, int(interleaved), T, q_heads,
-        _dt(qkv), _dev(q_out, "q_out"), _stream(stream)))
+    st = _lib.kv_cache_append(cache.ref, qp, qs, _int32(slots, "slots", (T,), qkv), pp, tp, rows, rot, interleaved, T,
+                              q_heads, _dt(qkv), op, _stream_of(stream, qkv))
+    if st:
+        raise DNError("kv_cache_append", st)
     return q_out
 
 
@@ -751,16 +775,21 @@ def kv_cache_read(cache: KVCache, slots: torch.Tensor, K: Optional[torch.Tensor]
     desc = _check_cache(cache, slots)
     if slots.dim() != 1:
         raise ValueError(f"slots has shape {list(slots.shape)}, expected [T]")
-    shape = (slots.shape[0], desc.heads, desc.d)
+    T = slots.shape[0]
+    shape = (T, desc.heads, desc.d)
     for name, t in (("K", K), ("V", V)):
-        _expect(t, name, shape, torch.bfloat16, slots.device)
-    if K is None:
-        K = torch.empty(shape, dtype=torch.bfloat16, device=slots.device)
-    if V is None:
-        V = torch.empty(shape, dtype=torch.bfloat16, device=slots.device)
-    _check("kv_cache_read", _lib.kv_cache_read(
-        ctypes.byref(desc), _int32(slots, "slots", (shape[0],), slots), shape[0], DN_BF16, _dev(K, "K"), _dev(V, "V"),
-        _stream(stream)))
+        if t is not None:
+            _expect(t, name, shape, torch.bfloat16, slots.device)
+    if K is None and V is None:
+        K, V = slots.new_empty((2, *shape), dtype=torch.bfloat16).unbind()
+    elif K is None:
+        K = torch.empty_like(V)
+    elif V is None:
+        V = torch.empty_like(K)
+    st = _lib.kv_cache_read(cache.ref, _int32(slots, "slots", (T,), slots), T, DN_BF16, _dev(K, "K"), _dev(V, "V"),
+                            _stream_of(stream, slots))
+    if st:
+        raise DNError("kv_cache_read", st)
     return K, V
 
 
@@ -780,17 +809,21 @@ def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, sc
     qp, qs = _rows(Q, "Q")
     if out is None:
         out = Q.new_empty((T, q_heads, d))
-    elif not _like(out, Q.shape, Q):
-        _expect(out, "out", (T, q_heads, d), Q.dtype, Q.device)
+        op = out.data_ptr()
+    else:
+        if not _like(out, Q.shape, Q):
+            _expect(out, "out", (T, q_heads, d), Q.dtype, Q.device)
+        op = _dev(out, "out")
     if workspace is None:
         n = attention_cache_workspace_bytes(T, B, q_heads, desc.heads, d, width, prefix_len)
         workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=Q.device)
-    elif workspace.dtype != torch.uint8 or workspace.get_device() != Q.get_device():
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != Q.get_device() or not workspace.is_contiguous():
         _expect(workspace, "workspace", None, torch.uint8, Q.device)
-    head = (qp, qs, T, q_heads, ctypes.byref(desc))
+        _dev(workspace, "workspace")
+    head = (qp, qs, T, q_heads, cache.ref)
     tail = (_int32(block_table, "block_table", (B, width), Q), width, _int32(q_start, "q_start", (B + 1,), Q),
             _int32(kv_len, "kv_len", (B,), Q), B, d ** -0.5 if scale is None else float(scale), _dt(Q),
-            _dev(workspace, "workspace"), workspace.numel(), _dev(out, "out"))
+            workspace.data_ptr(), workspace.numel(), op)
     return head, tail, out
 
 
@@ -802,7 +835,9 @@ def attention_cache_deferred(Q: torch.Tensor, cache: KVCache, block_table: torch
     Q[T, q_heads, d] are sequence b's new tokens, the last of its kv_len[b] cached ones, which lie in
     pages block_table[b]; each sees the keys up to its own.  scale defaults to 1/sqrt(d)."""
     head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out)
-    _check("attention_cache_deferred", _lib.attention_cache_deferred(*head, *tail, _stream(stream)))
+    st = _lib.attention_cache_deferred(*head, *tail, _stream_of(stream, Q))
+    if st:
+        raise DNError("attention_cache_deferred", st)
     return out
 
 
@@ -818,6 +853,7 @@ def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_tab
         raise ValueError(f"prefix_table has shape {list(prefix_table.shape)}, expected [at least {pages}]")
     head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out)
     pp = _int32(prefix_table, "prefix_table", tuple(prefix_table.shape), Q)
-    _check("attention_shared_prefix_deferred",
-           _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream(stream)))
+    st = _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream_of(stream, Q))
+    if st:
+        raise DNError("attention_shared_prefix_deferred", st)
     return out
