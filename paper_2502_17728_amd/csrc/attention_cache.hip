@@ -191,6 +191,14 @@ __device__ __forceinline__ int cut_page(int64_t at, int64_t weight, int pages) {
     return p < 2 ? 0 : pages - p < 2 ? pages : p;
 }
 
+// a / b for 0 <= a, 0 < b: through doubles, which are far shorter than the 64-bit division
+__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
+    int64_t q = (int64_t)((double)a / (double)b);
+    if (q * b > a) --q;
+    if ((q + 1) * b <= a) ++q;
+    return q;
+}
+
 // Lists every run's pieces, a run to a thread.  Piece (tile + run) of the line: both only grow.
 __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
     const int lane = threadIdx.x;
@@ -202,7 +210,7 @@ __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    const int64_t per = max((total + a.target - 1) / a.target, a.least * kKvPage * a.group);
+    const int64_t per = max(quotient(total + a.target - 1, a.target), a.least * kKvPage * a.group);
     const int64_t x0 = run * per, x1 = min(x0 + per, total);
     // the sequence in which the run starts: 64 sequences at a time, one to a lane
     int64_t start = 0, tile_start = 0, b = -1, b_start = 0, b_tiles = 0;
@@ -250,7 +258,7 @@ __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
         Weights w = weights(a, s, rows);
         int tiles = tiles_of(a, s, rows);
         const int64_t head_weight = w.before(tiles);
-        int head = (int)((x0 - b_start) / head_weight);
+        int head = (int)quotient(x0 - b_start, head_weight);
         const int64_t at = x0 - b_start - head * head_weight;
         int tile = 0, high = tiles - 1;  // the last tile that starts at `at` or before
         while (tile < high) {
@@ -272,7 +280,7 @@ __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
             a.pieces[piece] = Piece{(int)b, head, tile, lo, hi,
                                     lo == 0 && hi == pages && (pages > 0 || x >= x0) ? kWhole : lo < hi ? slot : kNone};
             if (x >= x0) {
-                const int64_t last = (x + weight - 1) / per;
+                const int64_t last = x + weight <= x1 ? run : quotient(x + weight - 1, per);
                 // a run is longer than a start and two pages, so one of any three cuts divides the tile
                 bool whole = true;
                 for (int64_t r = run + 1; r <= min(last, run + 3); ++r) {
@@ -321,15 +329,16 @@ __device__ __forceinline__ u32x4 frag<kKvFp8>(const u32x4& c, int j) {
     return u32x4{fp8_pair(lo, false), fp8_pair(lo, true), fp8_pair(hi, false), fp8_pair(hi, true)};
 }
 
-// Zeroes the codes of a V chunk's tokens from the `keep`-th of the lane's on.
+// All ones over the first `keep` tokens of a lane's 16 bytes of V, zeros over the others.  Words, not
+// lane masks: those would fill the scalar registers.
 template <int FMT>
-__device__ __forceinline__ u32x4 keep_tokens(u32x4 c, int keep) {
+__device__ __forceinline__ u32x4 keep_tokens(int keep) {
     constexpr int PER = FMT == kKvBf16 ? 2 : 4, BITS = 32 / PER;  // tokens in a word
-    uint32_t w[4] = {c.x, c.y, c.z, c.w};
+    uint32_t w[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        const int left = keep - j * PER;
-        w[j] = left >= PER ? w[j] : left <= 0 ? 0u : w[j] & ((1u << (left * BITS)) - 1u);
+        const int left = min(max(keep - j * PER, 0), PER);
+        w[j] = left == PER ? ~0u : (1u << (left * BITS)) - 1u;
     }
     return u32x4{w[0], w[1], w[2], w[3]};
 }
@@ -501,9 +510,9 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
         u32x4 pf[TILES / 2];
         softmax_unit<TILES, D, MASK>(s, kk, vs, key0, lim, st, acc, pf);
         if constexpr (MASK) {
-            const int keep = it.len - (page * kKvPage + 4 * E * u + E * G);
+            const u32x4 keep = keep_tokens<FMT>(it.len - (page * kKvPage + 4 * E * u + E * G));
 #pragma unroll
-            for (int i = 0; i < LOADS; ++i) vf[i] = keep_tokens<FMT>(vf[i], keep);
+            for (int i = 0; i < LOADS; ++i) vf[i] &= keep;
         }
 #pragma unroll
         for (int n = 0; n < NB; ++n)
@@ -715,13 +724,19 @@ __device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
         u32x4 pf[QW][TILES / 2];
 #pragma unroll
         for (int f = 0; f < QW; ++f) softmax_unit<TILES, D, MASK>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
+        u32x4 keep[TILES / 2];
+        if constexpr (MASK) {
+#pragma unroll
+            for (int c = 0; c < TILES / 2; ++c)
+                keep[c] = keep_tokens<kKvBf16>(it.len - (base + 4 * E * (c / J) + E * G + 8 * (c % J)));
+        }
 #pragma unroll
         for (int v = 0; v < VG; ++v) {
             if (v + 1 < VG) read(slot, (TILES + v + 1) * G4, fr[(v + 1) & 1]);
 #pragma unroll
             for (int c = 0; c < G4; ++c) {
                 const int at = v * G4 + c, n = at / J % NB, u = at / J / NB, j = at % J;
-                if (MASK) fr[v & 1][c] = keep_tokens<kKvBf16>(fr[v & 1][c], it.len - (base + 4 * E * u + E * G + 8 * j));
+                if constexpr (MASK) fr[v & 1][c] &= keep[u * J + j];
 #pragma unroll
                 for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[v & 1][c], pf[f][u * J + j], acc[f][n]);
             }
@@ -788,8 +803,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     constexpr int SCALES = 8 * kKvPage;
     __shared__ __attribute__((aligned(1024))) char smem[SRING + 4 * SCALES];
 
-    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int q = lane & 15, G = lane >> 4;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     Item it;
     int page_lo, count, slot;
     int2 list = {0, 1};
@@ -823,6 +837,9 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
     }
     if (slot == kNone || slot >= a.slots) continue;
 
+    int lane = tid & 63;
+    asm volatile("" : "+v"(lane));
+    const int q = lane & 15, G = lane >> 4;
     const int64_t rows_all = (int64_t)it.n * a.group;
     const int64_t tile_row = (int64_t)it.tile * R, row0 = tile_row + wave * QW * 16;  // the wave's first row
     u32x4 qf[QW][DC];
@@ -924,6 +941,12 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
             else
                 read(kb, (i - V0) * DC, fr[i & 1]);
         };
+        u32x4 keep[TILES / 2];
+        if constexpr (MASK && PV) {
+#pragma unroll
+            for (int c = 0; c < TILES / 2; ++c)
+                keep[c] = keep_tokens<kKvBf16>(it.len - ((page_lo + k) * kKvPage + 4 * E * (c / J) + E * G + 8 * (c % J)));
+        }
         if constexpr (QK) {
 #pragma unroll
             for (int f = 0; f < QW; ++f)
@@ -938,9 +961,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
             for (int c = 0; c < DC; ++c) {
                 if (i < V0) {
                     const int at = i * DC + c, n = at / J % NB, u = at / J / NB, j = at % J;
-                    if (MASK)
-                        fr[i & 1][c] = keep_tokens<kKvBf16>(
-                            fr[i & 1][c], it.len - ((page_lo + k) * kKvPage + 4 * E * u + E * G + 8 * j));
+                    if constexpr (MASK && PV) fr[i & 1][c] &= keep[u * J + j];
 #pragma unroll
                     for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[i & 1][c], pf[f][u * J + j], acc[f][n]);
                 } else {
@@ -1023,9 +1044,12 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         }
     }
 
+    // the lane's rows anew: what an address needs of them would else be held through the pages
+    int rows_at = wave * QW * 16 + q;
+    asm volatile("" : "+v"(rows_at));
 #pragma unroll
     for (int f = 0; f < QW; ++f)
-        store_rows<D>(a, it, R, row0 + f * 16 + q, rows_all, slot, lim[f], st[f], acc[f]);
+        store_rows<D>(a, it, R, tile_row + rows_at + f * 16, rows_all, slot, lim[f], st[f], acc[f]);
     __syncthreads();  // before the next piece's pages
     }
 }
@@ -1046,19 +1070,29 @@ struct Set {
 template <int D, int NS>
 __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own, const Set shared) {
     constexpr int NX = D / 4, ROWS = 256 / (NX * NS);
-    __shared__ int found[ROWS];
     __shared__ __attribute__((aligned(16))) float red[ROWS][NS][D + 4];
     const int tid = threadIdx.x, heads = a.heads * a.group;
     const int in = tid / (NX * NS), g = tid / NX % NS, x = tid % NX * 4;
     const int64_t row_id = (int64_t)blockIdx.x * ROWS + in, token = row_id / heads;
     const bool is_row = token < a.T;
-    if (tid < ROWS) found[tid] = -1;
-    __syncthreads();
-    if (is_row)
-        for (int64_t b = tid % (NX * NS); b < a.B; b += NX * NS)
-            if (a.q_start[b] <= token && token < a.q_start[b + 1]) found[in] = (int)b;
-    __syncthreads();
-    const int b = found[in];
+    // the token's sequence: the one of its own number where each has one token, else a search
+    int b = -1;
+    if (is_row) {
+        const int64_t guess = min(token, a.B - 1);
+        if (a.q_start[guess] <= token && token < a.q_start[guess + 1]) {
+            b = (int)guess;
+        } else {
+            int low = 0, high = (int)a.B - 1;  // the last that starts at the token or before
+            while (low < high) {
+                const int mid = (low + high + 1) >> 1;
+                if (a.q_start[mid] <= token)
+                    low = mid;
+                else
+                    high = mid - 1;
+            }
+            if (a.q_start[low] <= token && token < a.q_start[low + 1]) b = low;
+        }
+    }
     bool write = is_row && b >= 0;
     const int hq = (int)(row_id - token * heads), h = hq / a.group, r = hq % a.group;
     const Set* sets[2] = {&own, &shared};
