@@ -1124,6 +1124,9 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
                 count = chunks;
             }
             if (!write) break;
+            // q_start out of order can leave a sequence no workgroup: what it reads here is then no list
+            const int64_t most = set.pieces ? a.tiles_most + a.target : set.slots;
+            if (first < 0 || count > most || first > most - count) count = 0;
             for (int c = g; c < count; c += NS) {
                 const int slot = set.pieces ? set.pieces[first + c].slot : first + c * a.heads;
                 if (slot < 0 || slot >= set.slots) continue;  // a run with none of its pages; q_start out of order
