@@ -1163,10 +1163,13 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
 
 template <int D>
 hipError_t launch_merge(const Args& a, const Set& own, const Set& shared, hipStream_t s) {
-    // a workgroup to each row until the rows fill the chip
+    // A workgroup to each row until the rows fill the chip.  Measured, with one part at a time / a workgroup's
+    // worth at a time (the whole call, us, fp8, 32 and 8 heads of 128): 32 rows of 65536 keys 68.5 / 34.3, 512 of
+    // 4096 32.8 / 31.2, 1024 of 2048 32.3 / 32.1, 2048 of 1024 30.9 / 33.0, 32768 of 16384 293 / 328.  A shared
+    // prefix leaves each row more parts: 2048 rows behind 8192 keys 39.6 / 32.7.
     const int64_t rows = a.T * a.heads * a.group;
     constexpr int MOST = 256 / (D / 4);
-    if (rows <= 2048)
+    if (rows <= (shared.parts ? 2048 : 1024))
         merge_kernel<D, MOST><<<dim3((unsigned)rows), 256, 0, s>>>(a, own, shared);
     else
         merge_kernel<D, 1><<<dim3((unsigned)((rows + MOST - 1) / MOST)), 256, 0, s>>>(a, own, shared);

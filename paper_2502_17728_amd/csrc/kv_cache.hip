@@ -184,8 +184,6 @@ struct Codes<kKvFp8> {
     }
 };
 
-constexpr int kTile = 32;  // tokens of a workgroup at most
-
 struct AppendArgs {
     const __bf16* qkv;
     int64_t stride;
@@ -207,6 +205,7 @@ __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
     using B = KvBlock<FMT, D>;
     constexpr int E = B::E, N = 8, ITEMS = D / 16;       // items of a head (two pieces of 8)
     constexpr int PITCH = D * B::BYTES + 16;             // LDS row, 16-byte aligned
+    constexpr int kTile = kAppendTile;
     __shared__ __attribute__((aligned(16))) char smem[2 * kTile * PITCH];
     __shared__ int32_t slot_of[kTile];
     const int tid = threadIdx.x;
@@ -455,9 +454,6 @@ __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
     }
 }
 
-// Few tokens: more workgroups of 4, each with one pass over its items.  Many: 32, which fill V's pieces.
-inline int tile_tokens(int64_t tokens, int64_t heads) { return (tokens + kTile - 1) / kTile * heads >= 256 ? kTile : 4; }
-
 }  // namespace kv
 
 hipError_t launch_rotary_table(const double* inv_freq, int64_t rot, int64_t rows, double amplitude, float* table,
@@ -489,7 +485,7 @@ hipError_t launch_kv_append(const void* qkv, int64_t stride, const int32_t* slot
                             const float* table, int64_t rows, int64_t rot, int interleaved, int64_t tokens,
                             int64_t q_heads, const KvPool& c, void* q_out, hipStream_t s) {
     kv::AppendArgs a{(const __bf16*)qkv, stride, slots, positions, table, rows, tokens, c.pages * kKvPage, (int)c.heads,
-                     (int)(q_heads / c.heads), (int)rot, interleaved, kv::tile_tokens(tokens, c.heads), (char*)c.data,
+                     (int)(q_heads / c.heads), (int)rot, interleaved, append_tile(tokens, c.heads, q_heads / c.heads, c.d), (char*)c.data,
                      (__bf16*)q_out};
     const dim3 grid((unsigned)((tokens + a.tile - 1) / a.tile * c.heads));
     if (c.format == kKvBf16) {

@@ -49,6 +49,19 @@ inline size_t kv_block_bytes(int64_t d, int format) {
     return (size_t)(2 * kKvPage * d * (format == kKvBf16 ? 2 : 1) + 8 * kKvPage);
 }
 
+// ------------------------------------------------------------------- writing
+constexpr int kAppendTile = 16;  // tokens of a workgroup at most
+// Tokens of a workgroup, which takes one key/value head of them: as few as give its 256 threads an item
+// each (two pieces of 8 elements), and 16, which fill V's pieces, once those alone fill the chip.
+// Measured at 4 / 8 / 16 tokens, us: 32 query and 8 key/value heads of 128, fp8, 32 tokens 4.6 / 6.0 / 7.3,
+// 1000 tokens 9.4 / 9.2 / 9.4, 2048 tokens 16.2 / 16.0 / 13.6, 4096 tokens 28.3 / 26.4 / 23.2; 12 and 12 heads
+// of 64, bf16, 1000 tokens 8.7 / 6.6 / 6.0.  (32 tokens: 7.1 for the last, 23.0 for the one before, 16.4 at 2048.)
+inline int append_tile(int64_t tokens, int64_t heads, int64_t group, int64_t d) {
+    if ((tokens + kAppendTile - 1) / kAppendTile * heads >= 768) return kAppendTile;
+    const int64_t items = (group + 2) * d / 16;
+    return 4 * items > 128 ? 4 : 8 * items > 128 ? 8 : kAppendTile;
+}
+
 // ------------------------------------------------------------------- attention over the cache
 // Work is dealt on the device, where the lengths are.  Of sequence b the n g query rows of one
 // key/value head (n new tokens, g query heads) make tiles of `rows`.  Two deals:
@@ -69,10 +82,14 @@ struct CachePlan {
 };
 
 // Tiles of 16 rows while the sequences have no more rows than that on average; keys are then used
-// once and go straight to registers.
+// once and go straight to registers.  Measured at rows 16 / 64 / 128 / 256, us: 8 sequences of n tokens
+// with 32 query and 8 key/value heads of 128, 4096 keys, fp8: n = 4 21.9 / 26.8 / 32.9 / 53.8, n = 5 28.9 / 27.1 /
+// 33.2 / 55.2, n = 16 38.5 / 29.8 / 35.6 / 54.8, n = 17 45.0 / 39.6 / 35.9 / 54.6, n = 64 80.8 / 67.8 / 57.4 / 62.8;
+// 128 / 256: n = 96 107 / 100, n = 384 266 / 244.  bf16: n = 4 31.5 / 31.2 / 33.8 / 49.1, n = 5 41.5 / 31.3 / 34.4 / 49.8,
+// n = 17 71.8 / 37.6 / 37.5 / 53.5, n = 64 152 / 61.9 / 56.4 / 60.1; n = 96 98 / 92.
 inline int cache_rows(int64_t T, int64_t B, int64_t group) {
     const int64_t rows = (T * group + B - 1) / B;
-    return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 128 ? 128 : 256;
+    return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 256 ? 128 : 256;
 }
 
 inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, int64_t table_width, int rows,
