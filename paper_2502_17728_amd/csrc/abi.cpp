@@ -559,7 +559,9 @@ static bool attention_cache_sizes(int64_t T, int64_t B, int64_t q_heads, int64_t
     constexpr int64_t k31 = INT32_MAX;
     return T <= k31 / 128 && B <= (int64_t(1) << 20) && q_heads <= (int64_t(1) << 16) && T * q_heads <= k31 / 2 &&
            width <= k31 / DN_KV_PAGE && prefix <= k31 - DN_KV_PAGE && (T + B) * heads <= k31 / 4 &&
-           B * width < (int64_t(1) << 40) && (d == 64 || d == 128);
+           B * width < (int64_t(1) << 40) && (d == 64 || d == 128) &&
+           // the weight of all work dealt in runs
+           (T * q_heads / 256 + B * heads) * (q_heads / heads) <= (int64_t(1) << 61) / (width * DN_KV_PAGE + 256);
 }
 
 DN_API size_t attention_cache_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d,

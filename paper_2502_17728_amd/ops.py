@@ -615,13 +615,15 @@ def _rows(t: torch.Tensor, name: str):
         if st[k] != n and t.shape[k] != 1:
             raise ValueError(f"{name} must be contiguous within a token")
         n *= t.shape[k]
-    return t.data_ptr(), (max(st[0], n) if T != 1 else n)
+    return t.data_ptr(), (st[0] if T != 1 else n)  # tokens that lie on one another: refused by the library
 
 
 def _int32(t: torch.Tensor, name: str, shape, x: torch.Tensor):
     """Pointer of an int32 index tensor of this shape on x's device."""
     if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.shape == shape and t.is_contiguous()
             and t.get_device() == x.get_device()):
+        if t is None:
+            raise ValueError(f"{name} is required")
         _expect(t, name, shape, torch.int32, x.device)
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
@@ -634,6 +636,8 @@ def _table_of(table: torch.Tensor, x: torch.Tensor):
         rows, half, two = table.shape
         if two == 2 and table.dtype is torch.float32 and table.get_device() == x.get_device() and table.is_contiguous():
             return table.data_ptr(), rows, 2 * half
+    if table is None:
+        raise ValueError("table is required")
     _expect(table, "table", (None, None, 2), torch.float32, x.device)
     return _dev(table, "table"), table.shape[0], 2 * table.shape[1]
 
