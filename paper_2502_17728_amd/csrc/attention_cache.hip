@@ -71,6 +71,10 @@ __device__ __forceinline__ Seq sequence(const Args& a, int64_t b) {
     return s;
 }
 
+// Row and head numbers: the host refuses calls whose rows (T * group, rounded up to a tile) pass 31 bits, so
+// their quotients are 32-bit ones, a third of a 64-bit one's instructions.
+__device__ __forceinline__ int quotient32(int64_t a, int b) { return (int)((uint32_t)a / (uint32_t)b); }
+
 struct Item {
     int b, tile, chunk, head;
     int per;   // pages per chunk
@@ -151,7 +155,7 @@ __device__ __forceinline__ bool find_item(const Args& a, int id, int rows, Item&
 // Keys that some query of the tile sees.
 __device__ __forceinline__ int tile_keys(const Args& a, int n, int len, int tile, int rows) {
     if (!a.kv_len) return len;
-    const int last = (int)min((int64_t)n - 1, ((int64_t)tile * rows + rows - 1) / a.group);
+    const int last = min(n - 1, quotient32((int64_t)tile * rows + rows - 1, a.group));
     return min(len, max(len - n + last + 1, 0));
 }
 __device__ __forceinline__ int tile_chunks(int keys, int per) {
@@ -439,7 +443,7 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
     const int64_t row = (int64_t)it.tile * R + q;
     const int rows_here = (int)min((int64_t)R, (int64_t)it.n * a.group - (int64_t)it.tile * R);
     const int64_t rr = q < rows_here ? row : row - q;
-    const int qi = (int)(rr / a.group), qh = it.head * a.group + (int)(rr % a.group);
+    const int qi = quotient32(rr, a.group), qh = it.head * a.group + ((int)rr - qi * a.group);
     const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
     u32x4 qf[D / 32];
 #pragma unroll
@@ -448,7 +452,7 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
         for (int j = 0; j < E / 8; ++j) qf[c * (E / 8) + j] = ld16(qp + 4 * E * c + E * G + 8 * j);
     const int lim = a.kv_len ? it.len - it.n + qi : it.len - 1;
     // the first query of the tile sees the fewest keys
-    const int lim_min = a.kv_len ? it.len - it.n + (int)((int64_t)it.tile * R / a.group) : it.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + quotient32((int64_t)it.tile * R, a.group) : it.len - 1;
 
     f32x4 acc[NB];
 #pragma unroll
@@ -559,13 +563,13 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
             *reinterpret_cast<f32x4*>(part + x + 4) = f32x4{o[4], o[5], o[6], o[7]};
             if (x == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{lt, m, 0.f, 0.f};
         } else {
-            const int i_q = (int)(ro / a.group);
+            const int i_q = quotient32(ro, a.group);
             const bool none = a.kv_len && it.len - it.n + i_q < 0;  // no key at all: zero
             const float inv = none ? 0.f : 1.0f / lt;
             uint32_t pk[PER / 2];
 #pragma unroll
             for (int e = 0; e < PER / 2; ++e) pk[e] = none ? 0u : pack_bf16(o[2 * e] * inv, o[2 * e + 1] * inv);
-            const int64_t oh = (int64_t)(it.first + i_q) * a.heads * a.group + it.head * a.group + ro % a.group;
+            const int64_t oh = (int64_t)(it.first + i_q) * a.heads * a.group + it.head * a.group + ((int)ro - i_q * a.group);
             *reinterpret_cast<u32x4*>(a.out + oh * D + x) = u32x4{pk[0], pk[1], pk[2], pk[3]};
         }
     }
@@ -586,10 +590,10 @@ __device__ __forceinline__ void store_rows(const Args& a, const Item& it, int ro
         if (G == 0) *reinterpret_cast<f32x4*>(part + D) = f32x4{l, st.m, 0.f, 0.f};
         return;
     }
-    const int qi = (int)(row / a.group);
+    const int qi = quotient32(row, a.group);
     const bool none = lim < 0;  // no key at all: zero
     const float inv = 1.0f / l;
-    const int64_t oh = (int64_t)(it.first + qi) * a.heads * a.group + it.head * a.group + row % a.group;
+    const int64_t oh = (int64_t)(it.first + qi) * a.heads * a.group + it.head * a.group + ((int)row - qi * a.group);
 #pragma unroll
     for (int n = 0; n < D / 16; ++n) {
         const uint2 v = {pack_bf16(acc[n][0] * inv, acc[n][1] * inv), pack_bf16(acc[n][2] * inv, acc[n][3] * inv)};
@@ -630,7 +634,7 @@ __device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
 #pragma unroll
     for (int f = 0; f < QW; ++f) {
         const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
-        const int qi = (int)(row / a.group), qh = it.head * a.group + (int)(row % a.group);
+        const int qi = quotient32(row, a.group), qh = it.head * a.group + ((int)row - qi * a.group);
         const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
 #pragma unroll
         for (int c = 0; c < KC; ++c)
@@ -745,7 +749,7 @@ __device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
     };
     // pages that every query of the tile sees whole, then those that a mask cuts
     const int64_t tile_row = (int64_t)it.tile * R;
-    const int lim_min = a.kv_len ? it.len - it.n + (int)(tile_row / a.group) : it.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + quotient32(tile_row, a.group) : it.len - 1;
     const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
     for (int k = 0; k < whole; ++k) step(k, std::false_type{});
     for (int k = whole; k < count; ++k) step(k, std::true_type{});
@@ -847,7 +851,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
 #pragma unroll
     for (int f = 0; f < QW; ++f) {
         const int64_t row = min(row0 + f * 16 + q, rows_all - 1);
-        const int qi = (int)(row / a.group), qh = it.head * a.group + (int)(row % a.group);
+        const int qi = quotient32(row, a.group), qh = it.head * a.group + ((int)row - qi * a.group);
         const __bf16* qp = a.Q + (int64_t)(it.first + qi) * a.q_stride + (int64_t)qh * D;
 #pragma unroll
         for (int c = 0; c < DC; ++c) qf[f][c] = ld16(qp + 4 * E * (c / J) + E * G + 8 * (c % J));
@@ -1017,7 +1021,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         if (!LATE || more) meet();
     };
     // pages that every query of the tile sees whole, then those that a mask cuts
-    const int lim_min = a.kv_len ? it.len - it.n + (int)(tile_row / a.group) : it.len - 1;
+    const int lim_min = a.kv_len ? it.len - it.n + quotient32(tile_row, a.group) : it.len - 1;
     const int whole = min(max((lim_min + 1) / kKvPage - page_lo, 0), count);
     if (count > 0) {
         if (late) {
@@ -1073,7 +1077,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
     __shared__ __attribute__((aligned(16))) float red[ROWS][NS][D + 4];
     const int tid = threadIdx.x, heads = a.heads * a.group;
     const int in = tid / (NX * NS), g = tid / NX % NS, x = tid % NX * 4;
-    const int64_t row_id = (int64_t)blockIdx.x * ROWS + in, token = row_id / heads;
+    const int64_t row_id = (int64_t)blockIdx.x * ROWS + in, token = quotient32(row_id, heads);
     const bool is_row = token < a.T;
     // the token's sequence: the one of its own number where each has one token, else a search
     int b = -1;
@@ -1094,7 +1098,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
         }
     }
     bool write = is_row && b >= 0;
-    const int hq = (int)(row_id - token * heads), h = hq / a.group, r = hq % a.group;
+    const int hq = (int)(row_id - token * heads), h = quotient32(hq, a.group), r = hq - h * a.group;
     const Set* sets[2] = {&own, &shared};
     float m = kLowest, l = 0.f;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
@@ -1107,8 +1111,8 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
             const Set& set = *sets[w];
             if (!set.parts) continue;
             const int4 plan = set.info[w ? 0 : b];
-            const int64_t row = (w ? token : token - s.first) * a.group + r;
-            const int tile = (int)(row / set.rows);
+            const int row = (int)(w ? token : token - s.first) * a.group + r;
+            const int tile = row >> (31 - __builtin_clz(set.rows)), in_tile = row & (set.rows - 1);  // powers of two
             int count, first;
             if (set.pieces) {
                 const int64_t ordinal = plan.w + (int64_t)h * tiles_of(a, s, set.rows) + tile;
@@ -1130,7 +1134,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
             for (int c = g; c < count; c += NS) {
                 const int slot = set.pieces ? set.pieces[first + c].slot : first + c * a.heads;
                 if (slot < 0 || slot >= set.slots) continue;  // a run with none of its pages; q_start out of order
-                const float* part = set.parts + ((int64_t)slot * set.rows + row % set.rows) * (D + 4);
+                const float* part = set.parts + ((int64_t)slot * set.rows + in_tile) * (D + 4);
                 const f32x4 v = *reinterpret_cast<const f32x4*>(part + x), t = *reinterpret_cast<const f32x4*>(part + D);
                 const float mn = fmaxf(m, t[1]), wo = weight(m, mn), wn = weight(t[1], mn);
                 l = wo * l + wn * t[0];
