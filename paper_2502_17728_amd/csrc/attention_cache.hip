@@ -1067,14 +1067,15 @@ struct Set {
     int rows;
 };
 
-// Output rows (token, query head): D / 4 threads over a row's dimensions, NS such groups over its
-// partial sums, the other threads over rows.  `shared` (parts null: none) holds the partial sums over
+// Output rows (token, query head): D / (4 NV) threads over a row's dimensions (NV vectors each), NS such groups
+// over its partial sums, the other threads over rows.  `shared` (parts null: none) holds the partial sums over
 // the prefix, `own` those over the sequence's own keys; without a prefix rows whose tile has one
 // chunk are already written.
-template <int D, int NS>
+template <int D, int NS, int NV>
 __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own, const Set shared) {
-    constexpr int NX = D / 4, ROWS = 256 / (NX * NS);
-    __shared__ __attribute__((aligned(16))) float red[ROWS][NS][D + 4];
+    constexpr int NX = D / (4 * NV), STEP = 4 * NX, ROWS = 256 / (NX * NS);
+    static_assert(NS == 1 || NV == 1, "");
+    __shared__ __attribute__((aligned(16))) float red[NS > 1 ? ROWS : 1][NS][D + 4];
     const int tid = threadIdx.x, heads = a.heads * a.group;
     const int in = tid / (NX * NS), g = tid / NX % NS, x = tid % NX * 4;
     const int64_t row_id = (int64_t)blockIdx.x * ROWS + in, token = quotient32(row_id, heads);
@@ -1101,7 +1102,9 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
     const int hq = (int)(row_id - token * heads), h = quotient32(hq, a.group), r = hq - h * a.group;
     const Set* sets[2] = {&own, &shared};
     float m = kLowest, l = 0.f;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+    f32x4 o[NV];
+#pragma unroll
+    for (int v = 0; v < NV; ++v) o[v] = f32x4{0.f, 0.f, 0.f, 0.f};
     bool none = false;
     if (write) {
         const Seq s = sequence(a, b);
@@ -1135,16 +1138,20 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
                 const int slot = set.pieces ? set.pieces[first + c].slot : first + c * a.heads;
                 if (slot < 0 || slot >= set.slots) continue;  // a run with none of its pages; q_start out of order
                 const float* part = set.parts + ((int64_t)slot * set.rows + in_tile) * (D + 4);
-                const f32x4 v = *reinterpret_cast<const f32x4*>(part + x), t = *reinterpret_cast<const f32x4*>(part + D);
+                f32x4 p[NV];
+#pragma unroll
+                for (int v = 0; v < NV; ++v) p[v] = *reinterpret_cast<const f32x4*>(part + x + v * STEP);
+                const f32x4 t = *reinterpret_cast<const f32x4*>(part + D);
                 const float mn = fmaxf(m, t[1]), wo = weight(m, mn), wn = weight(t[1], mn);
                 l = wo * l + wn * t[0];
-                o = o * wo + v * wn;
+#pragma unroll
+                for (int v = 0; v < NV; ++v) o[v] = o[v] * wo + p[v] * wn;
                 m = mn;
             }
         }
     }
     if constexpr (NS > 1) {
-        *reinterpret_cast<f32x4*>(&red[in][g][x]) = o;
+        *reinterpret_cast<f32x4*>(&red[in][g][x]) = o[0];
         if (x == 0) {
             red[in][g][D] = l;
             red[in][g][D + 1] = m;
@@ -1155,14 +1162,17 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
         for (int v = 1; v < NS; ++v) {
             const float mv = red[in][v][D + 1], mn = fmaxf(m, mv), wo = weight(m, mn), wn = weight(mv, mn);
             l = wo * l + wn * red[in][v][D];
-            o = o * wo + *reinterpret_cast<const f32x4*>(&red[in][v][x]) * wn;
+            o[0] = o[0] * wo + *reinterpret_cast<const f32x4*>(&red[in][v][x]) * wn;
             m = mn;
         }
     }
     if (!write) return;
     const float inv = 1.0f / l;
-    const uint2 v = {pack_bf16(o[0] * inv, o[1] * inv), pack_bf16(o[2] * inv, o[3] * inv)};
-    *reinterpret_cast<uint2*>(a.out + row_id * D + x) = none ? uint2{0, 0} : v;
+#pragma unroll
+    for (int v = 0; v < NV; ++v) {
+        const uint2 w = {pack_bf16(o[v][0] * inv, o[v][1] * inv), pack_bf16(o[v][2] * inv, o[v][3] * inv)};
+        *reinterpret_cast<uint2*>(a.out + row_id * D + x + v * STEP) = none ? uint2{0, 0} : w;
+    }
 }
 
 template <int D>
@@ -1171,12 +1181,17 @@ hipError_t launch_merge(const Args& a, const Set& own, const Set& shared, hipStr
     // worth at a time (the whole call, us, fp8, 32 and 8 heads of 128): 32 rows of 65536 keys 68.5 / 34.3, 512 of
     // 4096 32.8 / 31.2, 1024 of 2048 32.3 / 32.1, 2048 of 1024 30.9 / 33.0, 32768 of 16384 293 / 328.  A shared
     // prefix leaves each row more parts: 2048 rows behind 8192 keys 39.6 / 32.7.
+    // Past that a row's lookups are VALU work that fewer threads a row spread over more dimensions: 1 / 2 / 4
+    // vectors a thread, us: two chunks of 1000 against 8191 keys 231.6 / 226.8 / 225.0 (the merge 21.6 / 15.8 / 14.9),
+    // four of 500 against 4096 170 / 164 / 163; 4096 rows behind 8192 keys, which have many parts, 53.3 / 51.4 / 54.2.
     const int64_t rows = a.T * a.heads * a.group;
     constexpr int MOST = 256 / (D / 4);
     if (rows <= (shared.parts ? 2048 : 1024))
-        merge_kernel<D, MOST><<<dim3((unsigned)rows), 256, 0, s>>>(a, own, shared);
+        merge_kernel<D, MOST, 1><<<dim3((unsigned)rows), 256, 0, s>>>(a, own, shared);
+    else if (shared.parts)
+        merge_kernel<D, 1, 2><<<dim3((unsigned)((rows + 2 * MOST - 1) / (2 * MOST))), 256, 0, s>>>(a, own, shared);
     else
-        merge_kernel<D, 1><<<dim3((unsigned)((rows + MOST - 1) / MOST)), 256, 0, s>>>(a, own, shared);
+        merge_kernel<D, 1, 4><<<dim3((unsigned)((rows + 4 * MOST - 1) / (4 * MOST))), 256, 0, s>>>(a, own, shared);
     return hipGetLastError();
 }
 
