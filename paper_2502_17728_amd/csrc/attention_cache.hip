@@ -21,13 +21,6 @@
 namespace dn {
 namespace ca {
 
-// A run's share of a tile: pages [lo, hi), and where its partial sums go (kWhole: it has all pages and
-// writes the output; kNone: no pages).
-struct Piece {
-    int b, head, tile, lo, hi, slot;
-};
-constexpr int kWhole = -1, kNone = -2;
-
 struct Args {
     const __bf16* Q;
     int64_t q_stride;
@@ -53,9 +46,6 @@ struct Args {
     __bf16* out;   // [T][heads * group][d]
 };
 
-struct Seq {
-    int first, n, len, pages;  // first token, tokens, keys, pages of keys
-};
 __device__ __forceinline__ Seq sequence(const Args& a, int64_t b) {
     Seq s;
     if (!a.q_start) {
@@ -70,10 +60,6 @@ __device__ __forceinline__ Seq sequence(const Args& a, int64_t b) {
     s.pages = (s.len + kKvPage - 1) / kKvPage;
     return s;
 }
-
-// Row and head numbers: the host refuses calls whose rows (T * group, rounded up to a tile) pass 31 bits, so
-// their quotients are 32-bit ones, a third of a 64-bit one's instructions.
-__device__ __forceinline__ int quotient32(int64_t a, int b) { return (int)((uint32_t)a / (uint32_t)b); }
 
 struct Item {
     int b, tile, chunk, head;
@@ -154,9 +140,7 @@ __device__ __forceinline__ bool find_item(const Args& a, int id, int rows, Item&
 
 // Keys that some query of the tile sees.
 __device__ __forceinline__ int tile_keys(const Args& a, int n, int len, int tile, int rows) {
-    if (!a.kv_len) return len;
-    const int last = min(n - 1, quotient32((int64_t)tile * rows + rows - 1, a.group));
-    return min(len, max(len - n + last + 1, 0));
+    return a.kv_len ? seen_keys(n, len, a.group, tile, rows) : len;
 }
 __device__ __forceinline__ int tile_chunks(int keys, int per) {
     return max(1, ((keys + kKvPage - 1) / kKvPage + per - 1) / per);
@@ -170,60 +154,27 @@ __device__ __forceinline__ void chunk_pages(int keys, int chunks, int chunk, int
 }
 
 // ----------------------------------------------------------------------------- runs
-// Long tiles are dealt in equal runs.  The work is laid on a line: sequences, of each its key/value
-// heads, of each its tiles, of each its pages.  A tile weighs the query-key pairs of its rows' largest
-// query, times `group`, and a start; a sequence's tiles then sum to a closed form.  Every run is an
-// equal stretch of the line, so all end together whatever the lengths.  A tile that several runs
-// share leaves partial sums, two slots to a run at most: its first tile's and its last's.
-struct Weights {
-    int64_t each, more;  // tile t weighs each + (t + 1) more
-    __device__ __forceinline__ int64_t before(int64_t t) const { return t * each + more * (t * (t + 1) / 2); }
-    __device__ __forceinline__ int64_t of(int64_t t) const { return each + (t + 1) * more; }
-};
-constexpr int kStart = 128;  // a tile's start and end, in keys
-__device__ __forceinline__ Weights weights(const Args& a, const Seq& s, int rows) {
-    return Weights{(int64_t)(max(s.len - s.n, 0) + kStart) * a.group, rows};
-}
-__device__ __forceinline__ int tiles_of(const Args& a, const Seq& s, int rows) {
-    return (int)(((int64_t)s.n * a.group + rows - 1) / rows);
-}
-// The page at which the line is cut `at` into a tile; nobody is left a single page.
-__device__ __forceinline__ int cut_page(int64_t at, int64_t weight, int pages) {
-    if (at <= 0) return 0;
-    if (at >= weight) return pages;
-    const int p = (int)((double)at * (double)pages / (double)weight);
-    return p < 2 ? 0 : pages - p < 2 ? pages : p;
-}
-
-// a / b for 0 <= a, 0 < b: through doubles, which are far shorter than the 64-bit division
-__device__ __forceinline__ int64_t quotient(int64_t a, int64_t b) {
-    int64_t q = (int64_t)((double)a / (double)b);
-    if (q * b > a) --q;
-    if ((q + 1) * b <= a) ++q;
-    return q;
-}
-
-// Lists every run's pieces, a run to a thread.  Piece (tile + run) of the line: both only grow.
+// Lists every run's pieces, a run to a thread (kv_layout.hpp: deal_run).
 __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
     const int lane = threadIdx.x;
     const int64_t run = (int64_t)blockIdx.x * 64 + lane;
     int64_t total = 0;
     for (int64_t b = lane; b < a.B; b += 64) {
         const Seq s = sequence(a, b);
-        total += weights(a, s, rows).before(tiles_of(a, s, rows)) * a.heads;
+        total += weights(s, a.group, rows).before(tiles_of(s, a.group, rows)) * a.heads;
     }
 #pragma unroll
     for (int o = 32; o >= 1; o >>= 1) total += __shfl_xor(total, o);
-    const int64_t per = max(quotient(total + a.target - 1, a.target), a.least * kKvPage * a.group);
-    const int64_t x0 = run * per, x1 = min(x0 + per, total);
+    const Line line{a.B, a.heads, a.target, total, run_length(total, a.target, a.least, a.group), a.group, rows, a.tiles_most};
+    const int64_t x0 = run * line.per;
     // the sequence in which the run starts: 64 sequences at a time, one to a lane
     int64_t start = 0, tile_start = 0, b = -1, b_start = 0, b_tiles = 0;
     for (int64_t b0 = 0; b0 < a.B; b0 += 64) {
         int64_t sum = 0, tiles = 0;
         if (b0 + lane < a.B) {
             const Seq s = sequence(a, b0 + lane);
-            tiles = tiles_of(a, s, rows);
-            sum = weights(a, s, rows).before(tiles) * a.heads;
+            tiles = tiles_of(s, a.group, rows);
+            sum = weights(s, a.group, rows).before(tiles) * a.heads;
             tiles *= a.heads;
         }
         int64_t to = sum, tiles_to = tiles;
@@ -256,58 +207,11 @@ __global__ __launch_bounds__(64) void plan_kernel(const Args a, int rows) {
         tile_start = __shfl(tiles_to, 63);
     }
     if (run >= a.target) return;
-    int2 list = {0, 0};
-    if (b >= 0 && x0 < x1) {
-        Seq s = sequence(a, b);
-        Weights w = weights(a, s, rows);
-        int tiles = tiles_of(a, s, rows);
-        const int64_t head_weight = w.before(tiles);
-        int head = (int)quotient(x0 - b_start, head_weight);
-        const int64_t at = x0 - b_start - head * head_weight;
-        int tile = 0, high = tiles - 1;  // the last tile that starts at `at` or before
-        while (tile < high) {
-            const int mid = (tile + high + 1) >> 1;
-            if (w.before(mid) <= at)
-                tile = mid;
-            else
-                high = mid - 1;
-        }
-        int64_t x = x0 - at + w.before(tile);  // where the tile starts
-        int64_t ordinal = b_tiles + (int64_t)head * tiles + tile;
-        list.x = (int)(ordinal + run);
-        while (true) {
-            const int64_t weight = w.of(tile), piece = ordinal + run;
-            const int pages = (tile_keys(a, s.n, s.len, tile, rows) + kKvPage - 1) / kKvPage;
-            const int lo = cut_page(x0 - x, weight, pages), hi = cut_page(x1 - x, weight, pages);
-            if (ordinal >= a.tiles_most) break;  // q_start out of order
-            const int slot = (int)(2 * run) + (x > x0 ? 1 : 0);
-            a.pieces[piece] = Piece{(int)b, head, tile, lo, hi,
-                                    lo == 0 && hi == pages && (pages > 0 || x >= x0) ? kWhole : lo < hi ? slot : kNone};
-            if (x >= x0) {
-                const int64_t last = x + weight <= x1 ? run : quotient(x + weight - 1, per);
-                // a run is longer than a start and two pages, so one of any three cuts divides the tile
-                bool whole = true;
-                for (int64_t r = run + 1; r <= min(last, run + 3); ++r) {
-                    const int cut = cut_page(r * per - x, weight, pages);
-                    whole = whole && (cut == 0 || cut == pages);
-                }
-                a.tile_pieces[ordinal] = int2{(int)piece, whole ? 0 : (int)(last - run) + 1};
-            }
-            ++list.y;
-            x += weight;
-            if (x >= x1) break;
-            ++ordinal;
-            if (++tile < tiles) continue;
-            tile = 0;
-            if (++head < a.heads) continue;
-            head = 0;
-            do
-                if (++b >= a.B) break;
-            while ((tiles = tiles_of(a, s = sequence(a, b), rows)) == 0);
-            if (b >= a.B) break;
-            w = weights(a, s, rows);
-        }
-    }
+    int2 list;
+    deal_run(
+        line, run, b, b_start, b_tiles, [&](int64_t at) { return sequence(a, at); },
+        [&](int64_t at, const Piece& p) { a.pieces[at] = p; },
+        [&](int64_t at, int first, int pieces) { a.tile_pieces[at] = int2{first, pieces}; }, list.x, list.y);
     a.run_pieces[run] = list;
 }
 
@@ -1127,7 +1031,7 @@ __global__ __launch_bounds__(256) void merge_kernel(const Args a, const Set own,
             const int tile = row >> (31 - __builtin_clz(set.rows)), in_tile = row & (set.rows - 1);  // powers of two
             int count, first;
             if (set.pieces) {
-                const int64_t ordinal = plan.w + (int64_t)h * tiles_of(a, s, set.rows) + tile;
+                const int64_t ordinal = plan.w + (int64_t)h * tiles_of(s, a.group, set.rows) + tile;
                 int2 list = {0, 0};
                 if (ordinal >= 0 && ordinal < a.tiles_most) list = a.tile_pieces[ordinal];
                 first = list.x;
@@ -1262,7 +1166,7 @@ hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s) {
         a.parts = (float*)(ws + parts);
         a.run_pieces = p.in_runs ? (int2*)(ws + runs) : nullptr;
         a.tile_pieces = p.in_runs ? a.run_pieces + p.target : nullptr;
-        a.pieces = p.in_runs ? (ca::Piece*)(a.tile_pieces + p.tiles) : nullptr;
+        a.pieces = p.in_runs ? (Piece*)(a.tile_pieces + p.tiles) : nullptr;
         a.tiles_most = p.tiles;
         return ca::Set{a.info, a.parts, a.pieces, p.slots, p.rows};
     };

@@ -140,4 +140,140 @@ inline CacheWorkspace cache_workspace(int64_t T, int64_t B, int64_t heads, int64
     return w;
 }
 
+// ------------------------------------------------------------------- runs
+// Long tiles are dealt in equal runs.  The work is laid on a line: sequences, of each its key/value
+// heads, of each its tiles, of each its pages.  A tile weighs the query-key pairs of its rows' largest
+// query, times `group`, and a start; a sequence's tiles then sum to a closed form.  Every run is an
+// equal stretch of the line, so all end together whatever the lengths.  A tile that several runs
+// share leaves partial sums, two slots to a run at most: its first tile's and its last's.
+
+// A run's share of a tile: pages [lo, hi), and where its partial sums go (kWhole: it has all pages and
+// writes the output; kNone: no pages).
+struct Piece {
+    int b, head, tile, lo, hi, slot;
+};
+constexpr int kWhole = -1, kNone = -2;
+
+struct Seq {
+    int first, n, len, pages;  // first token, tokens, keys, pages of keys
+};
+
+struct Weights {
+    int64_t each, more;  // tile t weighs each + (t + 1) more
+    DN_HD int64_t before(int64_t t) const { return t * each + more * (t * (t + 1) / 2); }
+    DN_HD int64_t of(int64_t t) const { return each + (t + 1) * more; }
+};
+constexpr int kStart = 128;  // a tile's start and end, in keys
+DN_HD Weights weights(const Seq& s, int group, int rows) {
+    const int behind = s.len - s.n;
+    return Weights{(int64_t)((behind > 0 ? behind : 0) + kStart) * group, rows};
+}
+DN_HD int tiles_of(const Seq& s, int group, int rows) { return (int)(((int64_t)s.n * group + rows - 1) / rows); }
+
+// Row and head numbers: the host refuses calls whose rows (T * group, rounded up to a tile) pass 31 bits, so
+// their quotients are 32-bit ones, a third of a 64-bit one's instructions.
+DN_HD int quotient32(int64_t a, int b) { return (int)((uint32_t)a / (uint32_t)b); }
+
+// Keys that some query of the tile sees, where each sees those up to its own.
+DN_HD int seen_keys(int n, int len, int group, int tile, int rows) {
+    const int row = quotient32((int64_t)tile * rows + rows - 1, group), last = row < n - 1 ? row : n - 1;
+    const int keys = len - n + last + 1;
+    return keys < 0 ? 0 : keys < len ? keys : len;
+}
+
+// The page at which the line is cut `at` into a tile (it grows with `at`); nobody is left a single page.
+DN_HD int cut_page(int64_t at, int64_t weight, int pages) {
+    if (at <= 0) return 0;
+    if (at >= weight) return pages;
+    const int p = (int)((double)at * (double)pages / (double)weight);
+    return p < 2 ? 0 : pages - p < 2 ? pages : p;
+}
+
+// a / b for 0 <= a, 0 < b: through doubles, which are far shorter than the 64-bit division
+DN_HD int64_t quotient(int64_t a, int64_t b) {
+    int64_t q = (int64_t)((double)a / (double)b);
+    if (q * b > a) --q;
+    if ((q + 1) * b <= a) ++q;
+    return q;
+}
+
+// The line: `target` runs of `per` each, the last one shorter.
+struct Line {
+    int64_t B, heads, target, total, per;
+    int group, rows;
+    int64_t tiles_most;
+};
+DN_HD int64_t run_length(int64_t total, int64_t target, int64_t least, int group) {
+    const int64_t even = quotient(total + target - 1, target), short_one = least * kKvPage * group;
+    return even > short_one ? even : short_one;
+}
+
+// Lists the pieces of one run, which starts in sequence b (its first tile `b_start` on the line and
+// number `b_tiles` of all).  Piece (tile + run) of the line: both only grow.  sequence(b) gives the
+// lengths, piece(i, ...) and tile(i, first piece, pieces) take what is found; the first piece and
+// their number are returned through `first` and `count`.
+template <class Sequence, class PieceOut, class TileOut>
+DN_HD void deal_run(const Line& line, int64_t run, int64_t b, int64_t b_start, int64_t b_tiles, Sequence&& sequence,
+                    PieceOut&& piece_out, TileOut&& tile_out, int& first, int& count) {
+    const int64_t per = line.per, x0 = run * per, x1 = x0 + per < line.total ? x0 + per : line.total;
+    first = count = 0;
+    if (b < 0 || x0 >= x1) return;
+    const int group = line.group, rows = line.rows;
+    Seq s = sequence(b);
+    Weights w = weights(s, group, rows);
+    int tiles = tiles_of(s, group, rows);
+    const int64_t head_weight = w.before(tiles);
+    int head = (int)quotient(x0 - b_start, head_weight);
+    const int64_t at = x0 - b_start - head * head_weight;
+    int tile = 0, high = tiles - 1;  // the last tile that starts at `at` or before
+    while (tile < high) {
+        const int mid = (tile + high + 1) >> 1;
+        if (w.before(mid) <= at)
+            tile = mid;
+        else
+            high = mid - 1;
+    }
+    int64_t x = x0 - at + w.before(tile);  // where the tile starts
+    int64_t ordinal = b_tiles + (int64_t)head * tiles + tile;
+    first = (int)(ordinal + run);
+    while (true) {
+        const int64_t weight = w.of(tile), piece = ordinal + run;
+        const int pages = (seen_keys(s.n, s.len, group, tile, rows) + kKvPage - 1) / kKvPage;
+        const int lo = cut_page(x0 - x, weight, pages), hi = cut_page(x1 - x, weight, pages);
+        if (ordinal >= line.tiles_most) break;  // q_start out of order
+        const int slot = (int)(2 * run) + (x > x0 ? 1 : 0);
+        piece_out(piece, Piece{(int)b, head, tile, lo, hi,
+                               lo == 0 && hi == pages && (pages > 0 || x >= x0) ? kWhole : lo < hi ? slot : kNone});
+        if (x >= x0) {
+            const int64_t last = x + weight <= x1 ? run : quotient(x + weight - 1, per);
+            // The tile is divided where some cut leaves pages on both sides: the first one that leaves any
+            // before it tells, for cuts only grow.  Its place is found by bisection, whatever the tile weighs
+            // for its pages (queries before the first key weigh like others and see none).
+            int64_t r = run + 1, end = last + 1;
+            while (r < end) {
+                const int64_t mid = (r + end) >> 1;
+                if (cut_page(mid * per - x, weight, pages) == 0)
+                    r = mid + 1;
+                else
+                    end = mid;
+            }
+            const bool divided = r <= last && cut_page(r * per - x, weight, pages) < pages;
+            tile_out(ordinal, (int)piece, divided ? (int)(last - run) + 1 : 0);
+        }
+        ++count;
+        x += weight;
+        if (x >= x1) break;
+        ++ordinal;
+        if (++tile < tiles) continue;
+        tile = 0;
+        if (++head < line.heads) continue;
+        head = 0;
+        do
+            if (++b >= line.B) break;
+        while ((tiles = tiles_of(s = sequence(b), group, rows)) == 0);
+        if (b >= line.B) break;
+        w = weights(s, group, rows);
+    }
+}
+
 }  // namespace dn
