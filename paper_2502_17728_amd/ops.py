@@ -803,6 +803,8 @@ def attention_cache_workspace_bytes(T: int, B: int, q_heads: int, heads: int, d:
 
 
 def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out):
+    """The call's arguments before and after the prefix's, and the output and scratch, which the caller holds
+    until the kernels are launched."""
     desc = _check_cache(cache, Q)
     if Q.dim() != 3 or Q.shape[2] != desc.d or Q.shape[1] % desc.heads:
         raise ValueError(f"Q has shape {list(Q.shape)}, expected [T, a multiple of {desc.heads}, {desc.d}]")
@@ -828,7 +830,7 @@ def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, sc
     tail = (_int32(block_table, "block_table", (B, width), Q), width, _int32(q_start, "q_start", (B + 1,), Q),
             _int32(kv_len, "kv_len", (B,), Q), B, d ** -0.5 if scale is None else float(scale), _dt(Q),
             workspace.data_ptr(), workspace.numel(), op)
-    return head, tail, out
+    return head, tail, out, workspace
 
 
 def attention_cache_deferred(Q: torch.Tensor, cache: KVCache, block_table: torch.Tensor, q_start: torch.Tensor,
@@ -838,7 +840,7 @@ def attention_cache_deferred(Q: torch.Tensor, cache: KVCache, block_table: torch
     """Attention of ragged sequences over the cache: rows q_start[b] .. q_start[b + 1] - 1 of
     Q[T, q_heads, d] are sequence b's new tokens, the last of its kv_len[b] cached ones, which lie in
     pages block_table[b]; each sees the keys up to its own.  scale defaults to 1/sqrt(d)."""
-    head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out)
+    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out)
     st = _lib.attention_cache_deferred(*head, *tail, _stream_of(stream, Q))
     if st:
         raise DNError("attention_cache_deferred", st)
@@ -855,7 +857,7 @@ def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_tab
     pages = (prefix_len + DN_KV_PAGE - 1) // DN_KV_PAGE
     if prefix_table.dim() != 1 or prefix_table.shape[0] < pages:
         raise ValueError(f"prefix_table has shape {list(prefix_table.shape)}, expected [at least {pages}]")
-    head, tail, out = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out)
+    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out)
     pp = _int32(prefix_table, "prefix_table", tuple(prefix_table.shape), Q)
     st = _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream_of(stream, Q))
     if st:
