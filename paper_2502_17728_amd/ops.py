@@ -2,7 +2,8 @@
 
 Every function here has the name of the C entry point it calls, takes torch
 tensors that live on the GPU, passes their device pointers and sizes through
-ctypes, and launches on the current torch stream (or the one given).  All
+ctypes, and launches on the current torch stream (or the one given: what the
+call makes itself then belongs to that stream, as inside torch.cuda.stream).  All
 arithmetic happens in the HIP kernels; nothing here computes on the host, and
 there is no fallback: if ``libdn.so`` is missing the import fails.
 """
@@ -172,6 +173,25 @@ def _stream(stream) -> int:
     return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
+def _on(stream, x: torch.Tensor):
+    """The stream given, as torch's current one on x's device.  What a call makes for itself on another
+    stream than the current one (outputs, scratch, copies) is made in this: torch's allocator orders a
+    block's uses by the stream that it was made on, so a block made on the current stream could still
+    be in use there when the call's kernels write it, or be given to someone else before they end."""
+    if not isinstance(stream, torch.cuda.Stream):
+        handle = _stream(stream)
+        stream = torch.cuda.ExternalStream(handle, device=x.device) if handle else torch.cuda.default_stream(x.device)
+    return torch.cuda.stream(stream)
+
+
+def _empty(x: torch.Tensor, shape, stream, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
+    """A tensor made for a call on `stream`, of x's dtype (or the one given) on x's device."""
+    if stream is not None:
+        with _on(stream, x):
+            return _empty(x, shape, None, dtype)
+    return x.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=x.device)
+
+
 # The wrappers below run on every token of a decode loop, where the kernels take 5-20 us: a
 # call's checks are one comparison each in the usual case, and _expect, which words the error,
 # runs only where one fails.
@@ -235,7 +255,7 @@ def ln_linear_prepare(W: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch
     nbytes = ln_linear_packed_bytes(K, N, dt)
     if nbytes == 0:
         raise DNError("ln_linear_packed_bytes", 1)
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=W.device)
+    packed = _empty(W, nbytes, stream, torch.uint8)
     desc = LnLinearWeights()
     fn = "ln_linear_prepare_centered" if centered else "ln_linear_prepare"
     _check(fn, getattr(_lib, fn)(
@@ -248,7 +268,7 @@ def ln_linear_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = x.new_empty((M, w.desc.N))
+        out = _empty(x, (M, w.desc.N), stream)
     _check("ln_linear_deferred", _lib.ln_linear_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -258,9 +278,9 @@ def ln_linear_serial(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5, stat
                      out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out, stats)
     if out is None:
-        out = torch.empty((M, w.N), dtype=x.dtype, device=x.device)
+        out = _empty(x, (M, w.N), stream)
     if stats is None:
-        stats = torch.empty(2 * M, dtype=torch.float32, device=x.device)
+        stats = _empty(x, 2 * M, stream, torch.float32)
     _check("ln_linear_serial", _lib.ln_linear_serial(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(stats, "stats"), _dev(out, "out"), _stream(stream)))
     return out
@@ -272,9 +292,9 @@ def ln_linear_norm_on_load(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5
     """Ablation: statistics pre-pass, then x normalized on load into the product (no deferral)."""
     M = _check_rows(x, w, out, stats)
     if out is None:
-        out = torch.empty((M, w.N), dtype=x.dtype, device=x.device)
+        out = _empty(x, (M, w.N), stream)
     if stats is None:
-        stats = torch.empty(2 * M, dtype=torch.float32, device=x.device)
+        stats = _empty(x, 2 * M, stream, torch.float32)
     _check("ln_linear_norm_on_load", _lib.ln_linear_norm_on_load(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(stats, "stats"), _dev(out, "out"), _stream(stream)))
     return out
@@ -291,11 +311,11 @@ def linear_deferred_post(x: torch.Tensor, w: PreparedLinear, gamma: torch.Tensor
     _expect(beta, "beta", (K,), x.dtype, x.device)
     _expect(y, "y", (M, K), x.dtype, x.device)
     if out is None:
-        out = torch.empty((M, w.N), dtype=x.dtype, device=x.device)
+        out = _empty(x, (M, w.N), stream)
     if y is None:
-        y = torch.empty_like(x)
+        y = _empty(x, (M, K), stream)
     if stats is None:
-        stats = torch.empty(2 * M, dtype=torch.float32, device=x.device)
+        stats = _empty(x, 2 * M, stream, torch.float32)
     if rms:
         if beta is not None:
             raise ValueError("RMSNorm has no shift")
@@ -314,7 +334,7 @@ def rms_linear_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = x.new_empty((M, w.desc.N))
+        out = _empty(x, (M, w.desc.N), stream)
     _check("rms_linear_deferred", _lib.rms_linear_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -334,7 +354,7 @@ def swiglu_prepare(W_gate: torch.Tensor, W_up: torch.Tensor, gamma: torch.Tensor
     nbytes = swiglu_packed_bytes(K, N, dt)
     if nbytes == 0:
         raise DNError("swiglu_packed_bytes", 1)
-    packed = torch.empty(nbytes, dtype=torch.uint8, device=W_gate.device)
+    packed = _empty(W_gate, nbytes, stream, torch.uint8)
     desc = LnLinearWeights()
     _check("swiglu_prepare", _lib.swiglu_prepare(
         _dev(W_gate, "W_gate"), _dev(W_up, "W_up"), _dev(gamma, "gamma"), K, N, dt, _dev(packed, "packed"),
@@ -346,7 +366,7 @@ def rms_swiglu_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = x.new_empty((M, w.desc.N))
+        out = _empty(x, (M, w.desc.N), stream)
     _check("rms_swiglu_deferred", _lib.rms_swiglu_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -362,7 +382,7 @@ def softmax_pv_deferred(S: torch.Tensor, V: torch.Tensor, causal: bool = False,
         _expect(V, "V", (BH, Lk, d), S.dtype, S.device)
         _expect(out, "out", (BH, Lq, d), S.dtype, S.device)
     if out is None:
-        out = S.new_empty((BH, Lq, d))
+        out = _empty(S, (BH, Lq, d), stream)
     _check("softmax_pv_deferred", _lib.softmax_pv_deferred(
         _dev(S, "S"), _dev(V, "V"), BH, Lq, Lk, d, int(causal), _dt(S), _dev(out, "out"), _stream(stream)))
     return out
@@ -397,7 +417,7 @@ def attention_deferred(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor, causal
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
     if out is None:
-        out = torch.empty_like(Q)
+        out = _empty(Q, Q.shape, stream)
     if g == 1:
         st = _lib.attention_deferred(_dev(Q, "Q"), _dev(K, "K"), _dev(V, "V"), BH, Lq, Lk, d, int(causal),
                                      float(scale), _dt(Q), _dev(out, "out"), _stream(stream))
@@ -426,16 +446,21 @@ def attention_decode_deferred(Q: torch.Tensor, K: torch.Tensor, V: torch.Tensor,
     _expect(workspace, "workspace", None, torch.uint8, Q.device)
     g = BHq // BH
     if out is None:
-        out = torch.empty_like(Q)
+        out = _empty(Q, Q.shape, stream)
     out_k = out
     if not (Q.is_contiguous() and out.is_contiguous()):  # contiguous ones are [BH, g * Lq, d] as they lie
-        Q, out_k = Q.reshape(BH, g * Lq, d), out.view(BH, g * Lq, d)
+        if stream is None:
+            Q = Q.reshape(BH, g * Lq, d)
+        else:
+            with _on(stream, Q):
+                Q = Q.reshape(BH, g * Lq, d)
+        out_k = out.view(BH, g * Lq, d)
     Lq = g * Lq
     if scale is None:
         scale = 1.0 / float(d) ** 0.5
     if workspace is None:
         nbytes = attention_decode_workspace_bytes(BH, Lq, Lk, d)
-        workspace = torch.empty(max(nbytes, 16), dtype=torch.uint8, device=Q.device)
+        workspace = _empty(Q, max(nbytes, 16), stream, torch.uint8)
     _check("attention_decode_deferred", _lib.attention_decode_deferred(
         _dev(Q, "Q"), _dev(K, "K"), _dev(V, "V"), BH, Lq, Lk, d, float(scale), _dt(Q), _dev(workspace, "workspace"),
         workspace.numel(), _dev(out_k, "out"), _stream(stream)))
@@ -451,7 +476,7 @@ def attention_decode_deferred_noalloc(Q: torch.Tensor, K: torch.Tensor, V: torch
     BHq, Lq, d, BH, Lk = _check_qkv(Q, K, V, out)
     g = BHq // BH
     if out is None:
-        out = torch.empty_like(Q)
+        out = _empty(Q, Q.shape, stream)
     if not (Q.is_contiguous() and out.is_contiguous()):
         raise ValueError("Q and out must be contiguous")
     if scale is None:
@@ -476,7 +501,7 @@ def layernorm(x: torch.Tensor, gamma: torch.Tensor, beta: Optional[torch.Tensor]
               out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M, K = _check_norm(x, gamma, beta, out)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x, (M, K), stream)
     _check("layernorm", _lib.layernorm(_dev(x, "x"), _dev(gamma, "gamma"), _dev(beta, "beta"), M, K, eps,
                                        _dt(x), _dev(out, "out"), _stream(stream)))
     return out
@@ -486,7 +511,7 @@ def rmsnorm(x: torch.Tensor, gamma: torch.Tensor, eps: float = 1e-5, out: Option
             stream=None) -> torch.Tensor:
     M, K = _check_norm(x, gamma, None, out)
     if out is None:
-        out = torch.empty_like(x)
+        out = _empty(x, (M, K), stream)
     _check("rmsnorm", _lib.rmsnorm(_dev(x, "x"), _dev(gamma, "gamma"), M, K, eps, _dt(x), _dev(out, "out"),
                                    _stream(stream)))
     return out
@@ -496,7 +521,7 @@ def silu_mul(g: torch.Tensor, u: torch.Tensor, out: Optional[torch.Tensor] = Non
     _expect(u, "u", tuple(g.shape), g.dtype, g.device)
     _expect(out, "out", None, g.dtype, g.device, numel=g.numel())
     if out is None:
-        out = torch.empty_like(g)
+        out = _empty(g, g.shape, stream)
     _check("silu_mul", _lib.silu_mul(_dev(g, "g"), _dev(u, "u"), g.numel(), _dt(g), _dev(out, "out"),
                                      _stream(stream)))
     return out
@@ -508,7 +533,7 @@ def softmax(S: torch.Tensor, causal: int = 0, out: Optional[torch.Tensor] = None
     BH, Lq, Lk = S.shape
     _expect(out, "out", tuple(S.shape), S.dtype, S.device)
     if out is None:
-        out = torch.empty_like(S)
+        out = _empty(S, S.shape, stream)
     _check("softmax", _lib.softmax(_dev(S, "S"), BH, Lq, Lk, int(causal), _dt(S), _dev(out, "out"),
                                    _stream(stream)))
     return out
@@ -543,7 +568,7 @@ def gemm(A: torch.Tensor, B, bias: Optional[torch.Tensor] = None, b_layout: int 
     _expect(out, "out", (batch, M, N), A.dtype, A.device)
     bptr = _dev(B.packed, "B") if isinstance(B, PreparedLinear) else _dev(B3, "B")
     if out is None:
-        out = torch.empty((batch, M, N), dtype=A.dtype, device=A.device)
+        out = _empty(A, (batch, M, N), stream)
     _check("gemm", _lib.gemm(_dev(A3, "A"), bptr, _dev(bias, "bias"), batch, M, K, N, int(b_layout),
                              int(a_causal), _dt(A), _dev(out, "out"), _stream(stream)))
     return out[0] if squeeze else out
@@ -597,7 +622,7 @@ def rotary_table(inv_freq: torch.Tensor, positions: int, amplitude: float = 1.0,
         raise ValueError(f"inv_freq has shape {list(inv_freq.shape)}, expected [rot / 2]")
     _expect(inv_freq, "inv_freq", None, torch.float64)
     half = inv_freq.shape[0]
-    table = torch.empty((max(int(positions), 0), half, 2), dtype=torch.float32, device=inv_freq.device)
+    table = _empty(inv_freq, (max(int(positions), 0), half, 2), stream, torch.float32)
     _check("rotary_table", _lib.rotary_table(_dev(inv_freq, "inv_freq"), 2 * half, int(positions), float(amplitude),
                                              _dev(table, "table") or None, _stream(stream)))
     return table
@@ -659,7 +684,7 @@ def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, 
     xp, xs = _rows(x, "x")
     tp, rows, rot = _table_of(table, x)
     if out is None:
-        out = x.new_empty((T, H, d))
+        out = _empty(x, (T, H, d), stream)
         op, os_ = out.data_ptr(), H * d
     else:
         if not _like(out, x.shape, x):
@@ -756,7 +781,7 @@ def kv_cache_append(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, posi
         if q_out is not None:
             raise ValueError("the rows hold no queries")
     elif q_out is None:
-        q_out = qkv.new_empty((T, q_heads, d))
+        q_out = _empty(qkv, (T, q_heads, d), stream)
         op = q_out.data_ptr()
     else:
         if not _like(q_out, (T, q_heads, d), qkv):
@@ -785,11 +810,11 @@ def kv_cache_read(cache: KVCache, slots: torch.Tensor, K: Optional[torch.Tensor]
         if t is not None:
             _expect(t, name, shape, torch.bfloat16, slots.device)
     if K is None and V is None:
-        K, V = slots.new_empty((2, *shape), dtype=torch.bfloat16).unbind()
+        K, V = _empty(slots, (2, *shape), stream, torch.bfloat16).unbind()
     elif K is None:
-        K = torch.empty_like(V)
+        K = _empty(V, shape, stream)
     elif V is None:
-        V = torch.empty_like(K)
+        V = _empty(K, shape, stream)
     st = _lib.kv_cache_read(cache.ref, _int32(slots, "slots", (T,), slots), T, DN_BF16, _dev(K, "K"), _dev(V, "V"),
                             _stream_of(stream, slots))
     if st:
@@ -802,7 +827,7 @@ def attention_cache_workspace_bytes(T: int, B: int, q_heads: int, heads: int, d:
     return int(_lib.attention_cache_workspace_bytes(T, B, q_heads, heads, d, table_width, prefix_len))
 
 
-def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out):
+def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out, stream):
     """The call's arguments before and after the prefix's, and the output and scratch, which the caller holds
     until the kernels are launched."""
     desc = _check_cache(cache, Q)
@@ -814,7 +839,7 @@ def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, sc
     B, width = block_table.shape
     qp, qs = _rows(Q, "Q")
     if out is None:
-        out = Q.new_empty((T, q_heads, d))
+        out = _empty(Q, (T, q_heads, d), stream)
         op = out.data_ptr()
     else:
         if not _like(out, Q.shape, Q):
@@ -822,7 +847,7 @@ def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, sc
         op = _dev(out, "out")
     if workspace is None:
         n = attention_cache_workspace_bytes(T, B, q_heads, desc.heads, d, width, prefix_len)
-        workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=Q.device)
+        workspace = _empty(Q, max(n, 16), stream, torch.uint8)
     elif workspace.dtype is not torch.uint8 or workspace.get_device() != Q.get_device() or not workspace.is_contiguous():
         _expect(workspace, "workspace", None, torch.uint8, Q.device)
         _dev(workspace, "workspace")
@@ -840,7 +865,7 @@ def attention_cache_deferred(Q: torch.Tensor, cache: KVCache, block_table: torch
     """Attention of ragged sequences over the cache: rows q_start[b] .. q_start[b + 1] - 1 of
     Q[T, q_heads, d] are sequence b's new tokens, the last of its kv_len[b] cached ones, which lie in
     pages block_table[b]; each sees the keys up to its own.  scale defaults to 1/sqrt(d)."""
-    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out)
+    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, 0, scale, workspace, out, stream)
     st = _lib.attention_cache_deferred(*head, *tail, _stream_of(stream, Q))
     if st:
         raise DNError("attention_cache_deferred", st)
@@ -857,7 +882,8 @@ def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_tab
     pages = (prefix_len + DN_KV_PAGE - 1) // DN_KV_PAGE
     if prefix_table.dim() != 1 or prefix_table.shape[0] < pages:
         raise ValueError(f"prefix_table has shape {list(prefix_table.shape)}, expected [at least {pages}]")
-    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out)
+    head, tail, out, held = _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, scale, workspace, out,
+                                                  stream)
     pp = _int32(prefix_table, "prefix_table", tuple(prefix_table.shape), Q)
     st = _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream_of(stream, Q))
     if st:

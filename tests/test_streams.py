@@ -1,4 +1,5 @@
-"""What a call makes for itself (outputs, scratch, copies) is held until its kernels are launched."""
+"""Calls on a stream of their own: what a call makes for itself (outputs, scratch, copies) belongs to the stream
+that it launches on, and its scratch is held until the kernels are launched."""
 import contextlib
 import weakref
 
@@ -96,3 +97,68 @@ def test_scratch_is_held_until_the_launch(name, monkeypatch):
     launch = Launch(monkeypatch)
     calls()[name]()
     assert launch.calls == 1
+
+
+@pytest.mark.parametrize("name", sorted(calls()))
+def test_what_a_call_makes_belongs_to_its_stream(name, monkeypatch):
+    call = calls()[name]
+    launch = Launch(monkeypatch)
+    call()
+    assert launch.calls == 1 and launch.made and all(on is None for _, on, _ in launch.made)
+    for stream in (5, 0):  # a handle; the default stream's
+        launch.made.clear()
+        call(stream=stream)
+        assert launch.made and all(on == stream for _, on, _ in launch.made), launch.made
+    assert launch.calls == 3 and launch.on is None
+
+
+# ------------------------------------------------------------------------------- on the device
+def stream_of(t):
+    """The stream that the allocator holds a tensor's memory for."""
+    for s in torch.cuda.memory_snapshot():
+        if s["address"] <= t.data_ptr() < s["address"] + s["total_size"]:
+            return s["stream"]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("as_handle", [False, True])
+@pytest.mark.parametrize("seqs,prefix", [([(1, 5000), (1, 900)], 0), ([(20, 3000)], 0), ([(300, 3000)], 0), ([(1, 50)] * 6, 3000)])
+def test_attention_over_the_cache_on_a_stream_given(seqs, prefix, as_handle):
+    """Scratch of the call's own, while the current stream takes and writes memory of the same sizes."""
+    from test_attention_cache import Batch
+    b = Batch(seqs, 4, 1, 64, "fp8", prefix=prefix)
+    want = b.run()
+    b.check(want)
+    n = ops.attention_cache_workspace_bytes(b.Q.shape[0], len(seqs), 4, 1, 64, b.table.shape[1], prefix)
+    side = torch.cuda.Stream()
+    Q = b.Q.cuda()
+    torch.cuda.synchronize()
+    held = []
+    for _ in range(4):
+        got = b.run(Q=Q, stream=side.cuda_stream if as_handle else side)
+        assert stream_of(got) == side.cuda_stream
+        held.append(got)
+        for size in (n, got.numel() * 2):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    torch.cuda.synchronize()
+    assert all(torch.equal(want, got) for got in held)
+
+
+@pytest.mark.gpu
+def test_decode_attention_on_a_stream_given():
+    g = torch.Generator().manual_seed(3)
+    k, v = (torch.randn((2, 5000, 64), generator=g).to(BF16).cuda() for _ in range(2))
+    q = torch.randn((3, 4, 64), generator=g).to(BF16).cuda().transpose(0, 1)  # heads apart: copied by the call
+    want = ops.attention_decode_deferred(q.contiguous(), k, v)
+    n = ops.attention_decode_workspace_bytes(2, 6, 5000, 64)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    held = []
+    for _ in range(4):
+        got = ops.attention_decode_deferred(q, k, v, stream=side)
+        assert stream_of(got) == side.cuda_stream
+        held.append(got)
+        for size in (n, q.numel() * 2):
+            torch.empty(size, dtype=torch.uint8, device="cuda").fill_(0xFF)
+    torch.cuda.synchronize()
+    assert all(torch.equal(want, got) for got in held)
