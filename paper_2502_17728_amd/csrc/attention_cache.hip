@@ -7,8 +7,15 @@
 // products are taken transposed, as in attention.hip: a lane keeps one query, and the numerators
 // go from the scores' accumulators straight into the second product (kv_layout.hpp).
 //
-// Numerators are rounded to bf16, the matrix cores' operand (2^-8 relative at most, the size of the
-// output's own rounding); scores, maximum, sums and partial sums are fp32.  Queries see keys up to
+// Scores, maximum, sums and partial sums are fp32.  Numerators enter the product with V as bf16, the matrix
+// cores' operand: in tiles of 16 rows, which wait for memory, as two parts, the rounded value and what
+// rounding left (2^-16 relative); in larger tiles, where the products and the operations beside them
+// set the time, as the rounded value alone (2^-8 relative at most, the size of the output's own
+// rounding).  The row sums take the numerators before that.  Measured, error in the 2-norm against
+// 64 bits: 1.6e-3 to 1.8e-3 in two parts, the error of the exact result rounded once, and 2.1e-3 to 2.4e-3 in
+// one.  Time in one part / in two, us: 32 sequences of one token against 4196 to 8192 keys, fp8, 73.1 / 73.7, against
+// 4096, bf16, 90.0 / 90.1; 8 sequences of 16 tokens against 4096 keys, fp8, 31.0 / 33.4, of 64 53.3 / 63.3; two chunks of 1000
+// against 8191 225 / 334; 2048 tokens against 16384, bf16, 477 / 656.  Queries see keys up to
 // their own: query i of n sees keys 0 .. kv_len - n + i.  A masked key weighs exactly 0 whatever
 // its slot holds: its numerator is selected away, and V codes past kv_len are zeroed before the
 // product (codes below are finite: rows with NaN or infinities are held as a NaN scale).
@@ -262,13 +269,13 @@ struct State {
     float m, l;
 };
 
-// Scores of TILES key tiles (16 each, of one unit) -> numerators as operands.  s holds q . K; kk the
+// Scores of TILES key tiles (16 each, of one unit) -> numerators as operands, in PARTS.  s holds q . K; kk the
 // lane's K scales (of each tile's four keys) times scale log2(e), vs its V scales; lim: the last key
 // that this lane's query sees.
-template <int TILES, int D, bool MASK>
+template <int TILES, int D, bool MASK, int PARTS>
 __device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x4 (&kk)[TILES], const f32x4 (&vs)[TILES],
                                              const int (&key0)[TILES], int lim, State& st, f32x4 (&acc)[D / 16],
-                                             u32x4 (&pf)[TILES / 2]) {
+                                             u32x4 (&pf)[PARTS][TILES / 2]) {
     f32x4 x[TILES];
     float top = -__builtin_inff();
 #pragma unroll
@@ -312,7 +319,17 @@ __device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x
                 st.l += on ? e : 0.f;
                 p[4 * h + i] = on ? e * vs[t + h][i] : 0.f;
             }
-        pf[t / 2] = u32x4{pack_bf16(p[0], p[1]), pack_bf16(p[2], p[3]), pack_bf16(p[4], p[5]), pack_bf16(p[6], p[7])};
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+            uint32_t w[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                w[i] = pack_bf16(p[2 * i], p[2 * i + 1]);
+                p[2 * i] -= bf_lo(w[i]);
+                p[2 * i + 1] -= bf_hi(w[i]);
+            }
+            pf[part][t / 2] = u32x4{w[0], w[1], w[2], w[3]};
+        }
     }
 }
 
@@ -322,7 +339,7 @@ __device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x
 // the four waves' sums meet in LDS at the end.  Measured, 32 sequences against 4196 to 8192 keys, 32 query over
 // 8 key/value heads of 128, fp8 (418 MB): 70 us, 6.0 TB/s; the call with its merge 75 us.  fp8 takes 218
 // registers, so two workgroups to a CU; held to 168 for three it spills (157 us).
-constexpr int kDecodeRows = 16;
+constexpr int kDecodeRows = 16, kDecodeParts = 2;
 template <int FMT, int D>
 constexpr int decode_lds = 4 * kDecodeRows * (D + 4) * 4 + 8 * kDecodeRows * 4;
 
@@ -417,7 +434,7 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
             kk[t] = ks[t] * a.sl2;
         }
         if constexpr (MORE) fetch_k(un + 1);
-        u32x4 pf[TILES / 2];
+        u32x4 pf[kDecodeParts][TILES / 2];
         softmax_unit<TILES, D, MASK>(s, kk, vs, key0, lim, st, acc, pf);
         if constexpr (MASK) {
             const u32x4 keep = keep_tokens<FMT>(it.len - (page * kKvPage + 4 * E * u + E * G));
@@ -427,7 +444,10 @@ __device__ __forceinline__ void decode_item(const Args& a, int id, char* lds) {
 #pragma unroll
         for (int n = 0; n < NB; ++n)
 #pragma unroll
-            for (int j = 0; j < E / 8; ++j) acc[n] = mfma_chunk<__bf16>(frag<FMT>(vf[n], j), pf[j], acc[n]);
+            for (int j = 0; j < E / 8; ++j)
+#pragma unroll
+                for (int part = 0; part < kDecodeParts; ++part)
+                    acc[n] = mfma_chunk<__bf16>(frag<FMT>(vf[n], j), pf[part][j], acc[n]);
     };
     // pages that every query of the tile sees whole, then those that a mask cuts, then the last unit
     const std::true_type yes{};
@@ -632,7 +652,7 @@ __device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
             vs[t] = *reinterpret_cast<const f32x4*>(slot + SCALES + 4 * kKvPage + 4 * o);
             key0[t] = base + o;
         }
-        u32x4 pf[QW][TILES / 2];
+        u32x4 pf[QW][1][TILES / 2];
 #pragma unroll
         for (int f = 0; f < QW; ++f) softmax_unit<TILES, D, MASK>(s[f], kk, vs, key0, lim[f], st[f], acc[f], pf[f]);
         u32x4 keep[TILES / 2];
@@ -649,7 +669,7 @@ __device__ __forceinline__ void tile_item(const Args& a, int id, char* smem) {
                 const int at = v * G4 + c, n = at / J % NB, u = at / J / NB, j = at % J;
                 if constexpr (MASK) fr[v & 1][c] &= keep[u * J + j];
 #pragma unroll
-                for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[v & 1][c], pf[f][u * J + j], acc[f][n]);
+                for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[v & 1][c], pf[f][0][u * J + j], acc[f][n]);
             }
         }
         if (k + 1 < count) land(k + 1);  // page k + 1 has landed, and every wave is done with page k
@@ -841,7 +861,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
         for (int c = 0; c < DC; ++c) fr[c] = lds_ld16(lds_ptr((char*)slot + (first + c) * kChunkBytes + lane * 16));
     };
     constexpr int VG = FRAGS / DC;  // groups of V operands
-    u32x4 pf[QW][TILES / 2];
+    u32x4 pf[QW][1][TILES / 2];
     // The product of page k's numerators with V, then the scores of page k + 1.  Operands are read
     // from LDS one group of DC ahead of their products, in an order fixed by scheduling groups: left
     // to itself the compiler reads each beside its use and waits for it.
@@ -879,7 +899,7 @@ __global__ __launch_bounds__(512) void wide_kernel(const Args a) {
                     const int at = i * DC + c, n = at / J % NB, u = at / J / NB, j = at % J;
                     if constexpr (MASK && PV) fr[i & 1][c] &= keep[u * J + j];
 #pragma unroll
-                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[i & 1][c], pf[f][u * J + j], acc[f][n]);
+                    for (int f = 0; f < QW; ++f) acc[f][n] = mfma_chunk<__bf16>(fr[i & 1][c], pf[f][0][u * J + j], acc[f][n]);
                 } else {
                     const int t = i - V0;
 #pragma unroll
