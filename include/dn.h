@@ -388,8 +388,9 @@ DN_API dn_status rotary_apply(const void* x, int64_t x_stride, const int32_t* po
  * Formats: DN_KV_BF16 holds bfloat16; DN_KV_FP8 holds OCP e4m3 codes with one
  * fp32 scale per token and head, x = code * scale, scale = max(max |x| / 448,
  * 2^-120), the code rounded to nearest even.  Either way a row (K or V of one
- * token and head) that holds a NaN or an infinity is held as all NaN: codes 0,
- * scale NaN (the scale is 1 elsewhere in DN_KV_BF16).
+ * token and head) that holds a NaN or an infinity (in DN_KV_BF16 also a turned
+ * key that would round to one) is held as all NaN: codes 0, scale NaN (the scale
+ * is 1 elsewhere in DN_KV_BF16).
  * Layout (version 1) of `data`: [pages][heads][block], block = K codes, V codes,
  * 64 K scales, 64 V scales.  With E = 8 (bf16) or 16 (fp8) elements in 16 bytes,
  * token 4E u + E a + 8 j + 4 t + i, dimension 4E c + E g + r of K lies at byte

@@ -144,12 +144,12 @@ __global__ __launch_bounds__(256) void rotary_kernel(const T* x, int64_t x_strid
 }
 
 // ----------------------------------------------------------------------------- codes
-// Scale of a row from the largest |x| among its threads' bits; NaN where one of its elements is no
-// finite number (bits at or past infinity's): the row's codes are then 0 and it reads back as NaN,
-// and no masked product with it can spread.
+// Scale of a row from the largest |x| among its threads' bits; NaN where one of its elements is held as no
+// finite number (bits at or past infinity's, in bf16 at or past those that round to it, halfway above its
+// largest): the row's codes are then 0 and it reads back as NaN, and no masked product with it can spread.
 template <int FMT>
 __device__ __forceinline__ float row_scale(uint32_t top, float& inv) {
-    if (top >= 0x7f800000u) {
+    if (top >= (FMT == kKvBf16 ? 0x7f7f8000u : 0x7f800000u)) {
         inv = 0.f;
         return __builtin_nanf("");
     }
