@@ -423,6 +423,8 @@ DN_API dn_status gemm(const void* A, const void* B, const void* bias, int64_t ba
 }
 
 // ------------------------------------------------------------------- rotary positions, paged cache
+constexpr int64_t kMaxThreads = 0xffffffff;  // of a launch, as HIP counts them
+
 // What a strided [T][width] array spans, from its first to past its last element.
 static bool span_of(int64_t T, int64_t stride, int64_t width, int64_t es, size_t* out) {
     size_t all, last;
@@ -439,7 +441,7 @@ DN_API dn_status rotary_table(const double* inv_freq, int64_t rot, int64_t posit
     if (rot % 16) return DN_ERR_UNSUPPORTED;
     if (!aligned(inv_freq, 8) || !aligned(table, 16)) return DN_ERR_MISALIGNED;
     if (overlaps(table, tb, inv_freq, (size_t)rot * 4)) return DN_ERR_INVALID_ARG;
-    if (positions > INT32_MAX || (positions * (rot / 2) + 255) / 256 > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    if (positions > INT32_MAX || positions * (rot / 2) > kMaxThreads - 255) return DN_ERR_UNSUPPORTED;
     return from_hip(dn::launch_rotary_table(inv_freq, rot, positions, amplitude, table, stream));
 }
 
@@ -461,7 +463,7 @@ DN_API dn_status rotary_apply(const void* x, int64_t x_stride, const int32_t* po
         overlaps(out, ob, positions, (size_t)T * 4))
         return DN_ERR_INVALID_ARG;
     const int64_t items = H * d / (dtype == DN_F32 ? 8 : 16);
-    if (items > INT32_MAX || T > INT32_MAX || T > (kMaxGridX * 256 - 255) / items) return DN_ERR_UNSUPPORTED;
+    if (items > INT32_MAX || T > INT32_MAX || T > (kMaxThreads - 255) / items) return DN_ERR_UNSUPPORTED;
     return from_hip(dn::launch_rotary(x, x_stride, positions, table, table_rows, T, H, d, rot, interleaved, inverse,
                                       dtype, out, out_stride, stream));
 }
@@ -530,9 +532,10 @@ DN_API dn_status kv_cache_append(const kv_cache* cache, const void* qkv, int64_t
         if (overlaps(cache->data, cb, ins[i], in_bytes[i]) || overlaps(q_out, qb, ins[i], in_bytes[i]))
             return DN_ERR_INVALID_ARG;
     if (overlaps(cache->data, cb, q_out, qb)) return DN_ERR_INVALID_ARG;
-    // a workgroup's items and the grid fit 31 bits
-    if (width > (int64_t(1) << 24) || T > INT32_MAX / 4 || (T + 3) / 4 > kMaxGridX / cache->heads)
-        return DN_ERR_UNSUPPORTED;
+    // a workgroup's items fit 31 bits
+    if (width > (int64_t(1) << 24) || T > INT32_MAX / 4) return DN_ERR_UNSUPPORTED;
+    const int64_t tile = dn::append_tile(T, cache->heads, q_heads / cache->heads, cache->d);
+    if ((T + tile - 1) / tile > kMaxThreads / 256 / cache->heads) return DN_ERR_UNSUPPORTED;
     return from_hip(dn::launch_kv_append(qkv, stride, slots, positions, table, table_rows, rot, interleaved, T, q_heads,
                                          pool_of(cache), q_out, stream));
 }
@@ -549,19 +552,28 @@ DN_API dn_status kv_cache_read(const kv_cache* cache, const int32_t* slots, int6
     if (overlaps(K, ob, V, ob) || overlaps(K, ob, cache->data, cb) || overlaps(V, ob, cache->data, cb) ||
         overlaps(K, ob, slots, ib) || overlaps(V, ob, slots, ib))
         return DN_ERR_INVALID_ARG;
-    if (T > INT32_MAX / 4 || (T + 3) / 4 > kMaxGridX / cache->heads) return DN_ERR_UNSUPPORTED;
+    // a workgroup takes 16 tokens of a head's K or 56 of its V at least
+    if (T > INT32_MAX / 4 || (T + 15) / 16 + (T + 55) / 56 > kMaxThreads / 256 / cache->heads) return DN_ERR_UNSUPPORTED;
     return from_hip(dn::launch_kv_read(pool_of(cache), slots, T, K, V, stream));
 }
 
-// Sizes for which every count of the attention kernels fits its type.
+// Sizes for which every count of the attention kernels fits its type, and every launch the device.
 static bool attention_cache_sizes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d, int64_t width,
                                   int64_t prefix) {
     constexpr int64_t k31 = INT32_MAX;
-    return T <= k31 / 128 && B <= (int64_t(1) << 20) && q_heads <= (int64_t(1) << 16) && T * q_heads <= k31 / 2 &&
-           width <= k31 / DN_KV_PAGE && prefix <= k31 - DN_KV_PAGE && (T + B) * heads <= k31 / 4 &&
-           B * width < (int64_t(1) << 40) && (d == 64 || d == 128) &&
-           // the weight of all work dealt in runs
-           (T * q_heads / 256 + B * heads) * (q_heads / heads) <= (int64_t(1) << 61) / (width * DN_KV_PAGE + 256);
+    const bool counts =
+        T <= k31 / 128 && B <= (int64_t(1) << 20) && q_heads <= (int64_t(1) << 16) && T * q_heads <= k31 / 2 &&
+        width <= k31 / DN_KV_PAGE && prefix <= k31 - DN_KV_PAGE && (T + B) * heads <= k31 / 4 &&
+        B * width < (int64_t(1) << 40) && (d == 64 || d == 128) &&
+        // the weight of all work dealt in runs
+        (T * q_heads / 256 + B * heads) * (q_heads / heads) <= (int64_t(1) << 61) / (width * DN_KV_PAGE + 256);
+    if (!counts) return false;
+    const dn::CacheWorkspace w =
+        dn::cache_workspace(T, B, heads, q_heads / heads, d, width, (prefix + DN_KV_PAGE - 1) / DN_KV_PAGE);
+    const int64_t own = w.own.grid * (w.own.rows == 256 ? 512 : 256), prefixes = w.prefix.grid * (w.prefix.rows == 256 ? 512 : 256);
+    // tiles of 16 rows share a launch with the prefix's; the merge takes d / 16 threads a row, d / 8 behind a prefix
+    return own + (w.own.rows == 16 ? prefixes : 0) <= kMaxThreads && prefixes <= kMaxThreads &&
+           (w.own.slots == 0 || T * q_heads <= (kMaxThreads - 255) / (d / (prefix ? 8 : 16)));
 }
 
 DN_API size_t attention_cache_workspace_bytes(int64_t T, int64_t B, int64_t q_heads, int64_t heads, int64_t d,

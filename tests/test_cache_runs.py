@@ -168,3 +168,27 @@ def test_tiles_of_runs_on_the_device(seqs, Hq, Hkv, fmt, d):
     first = b.run(out=out).clone()
     b.check(first)
     assert torch.equal(first, b.run(out=out.fill_(float("nan"))))
+
+
+# ------------------------------------------------------------------------------- launches past what HIP takes
+def test_launches_past_the_devices_limit_are_refused():
+    """2^32 threads and more in one launch: refused before anything is launched, where the device would refuse it;
+    the largest that fits is taken."""
+    from paper_2502_17728_amd import ops
+    wb = ops._lib.attention_cache_workspace_bytes
+    # one new token of a million sequences, 16-row tiles of 256 threads: 2^20 heads + 2^16 heads + 768 of them
+    assert wb(1 << 20, 1 << 20, 15, 15, 64, 8, 0) > 0 == wb(1 << 20, 1 << 20, 16, 16, 64, 8, 0)
+    # behind a prefix both kinds of tile share the launch
+    assert wb(986000, 986000, 17, 17, 64, 8, 0) > 0 == wb(986000, 986000, 17, 17, 64, 8, 6400)
+    # the merge: 2^28 rows of d = 128, 8 threads each; behind a prefix 16
+    assert wb(1 << 13, 1, 1 << 15, 1, 128, 64, 0) > 0
+    assert wb(1 << 13, 1, 1 << 15, 1, 128, 64, 64) == 0 < wb(1 << 12, 1, 1 << 15, 1, 128, 64, 64)
+    P = 0x7F0000000000
+    UNSUPPORTED = 2
+    far = lambda k: P + (k << 42)
+    desc = ops.KVCacheDesc(64, 64, 64, 2, 1, P)
+    big = 1 << 28
+    assert ops._lib.kv_cache_append(ctypes.byref(desc), far(1), 128 * 64, far(2), None, None, 0, 0, 0, big, 0, 1, None, None) == UNSUPPORTED
+    assert ops._lib.kv_cache_read(ctypes.byref(desc), far(1), big, 1, far(2), far(3), None) == UNSUPPORTED
+    assert ops._lib.rotary_apply(far(1), 1 << 14, far(2), far(3), 4, 1 << 24, 256, 64, 64, 0, 0, 1, far(4), 1 << 14, None) == UNSUPPORTED
+    assert ops._lib.rotary_table(far(1), 256, 1 << 26, 1.0, far(2), None) == UNSUPPORTED
