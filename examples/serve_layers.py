@@ -51,10 +51,11 @@ class Server:
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.sequences, self.prompt = sequences, prompt
         own = -(-room // PAGE)
+        self.room = own * PAGE  # tokens of a sequence behind the prompt at most
         self.prefix_pages = -(-prompt // PAGE)
         pages = self.prefix_pages + sequences * own
         self.layers = [Layer(hidden, q_heads, heads, d, ffn, pages, fmt, g) for _ in range(layers)]
-        self.table = ops.rotary_table(ops.rotary_frequencies(d)[0], prompt + room)
+        self.table = ops.rotary_table(ops.rotary_frequencies(d)[0], prompt + self.room)
         self.embed = torch.randn((vocabulary, hidden), generator=g, device="cuda").to(torch.bfloat16)
         self.head = ops.ln_linear_prepare(self.embed.t().contiguous() * hidden ** -0.5,
                                           torch.ones(hidden, dtype=torch.bfloat16, device="cuda"))
@@ -89,8 +90,9 @@ class Server:
                                                                      kv_len, workspace=workspace)
 
     def slots_of(self, sequence, at):
-        page = self.own[sequence.long(), (at // PAGE).long()]
-        return (page * PAGE + at % PAGE).int()
+        """Where tokens `at` of the sequences lie; -1 (written nowhere) past a sequence's room."""
+        page = self.own[sequence.long(), (at // PAGE).long().clamp(max=self.own.shape[1] - 1)]
+        return torch.where(at < self.room, page * PAGE + at % PAGE, -1).int()
 
     def read_texts(self, texts):
         """Each sequence's own tokens, all in one ragged call; the tokens that follow."""
@@ -104,11 +106,12 @@ class Server:
         return self.next_tokens(x[q_start[1:].long() - 1])
 
     def step(self, tokens):
-        """One token of every sequence: the lengths move on the device, so the step can be replayed."""
+        """One token of every sequence: the lengths move on the device, so the step can be replayed.  A sequence
+        whose room is full stays as it is: its further tokens see it, and are not kept."""
         at = self.kv_len.clone()
-        self.kv_len += 1
+        self.kv_len.add_(1).clamp_(max=self.room)
         attend = self.attend_behind_prompt(self.one_each, self.kv_len, self.workspace)
-        x = self.run(tokens, attend, self.slots_of(self.one_each[:-1], at), self.prompt + at)
+        x = self.run(tokens, attend, self.slots_of(self.one_each[:-1], at), (self.prompt + at).clamp(max=len(self.table) - 1))
         tokens.copy_(self.next_tokens(x))
 
     def move(self, slots, to, distance):
