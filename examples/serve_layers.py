@@ -96,7 +96,11 @@ class Server:
 
     def read_texts(self, texts):
         """Each sequence's own tokens, all in one ragged call; the tokens that follow."""
+        if len(texts) != self.sequences or min(map(len, texts)) < 1:
+            raise ValueError(f"a text of one token at least is needed for each of {self.sequences} sequences")
         lengths = ints([len(t) for t in texts])
+        if int((self.kv_len + lengths).max()) > self.room:
+            raise ValueError(f"a sequence has room for {self.room} tokens")
         q_start = torch.cat([lengths.new_zeros(1), lengths.cumsum(0, dtype=torch.int32)])
         sequence = torch.repeat_interleave(torch.arange(self.sequences, device="cuda"), lengths.long())
         at = (torch.arange(len(sequence), device="cuda") - q_start[sequence] + self.kv_len[sequence]).int()
@@ -117,6 +121,8 @@ class Server:
     def move(self, slots, to, distance):
         """The keys and values at `slots` of every layer, put at slots `to` as if they were `distance` tokens
         further on: a rotation by p, then by the distance, is the rotation by their sum."""
+        if not 0 <= distance < len(self.table):
+            raise ValueError(f"the table turns by less than {len(self.table)} positions")
         by = torch.full_like(slots, distance)
         for layer in self.layers:
             K, V = ops.kv_cache_read(layer.cache, slots)

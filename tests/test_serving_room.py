@@ -1,4 +1,4 @@
-"""examples/serve_layers.py at the end of a sequence's room (GPU)."""
+"""examples/serve_layers.py at the end of a sequence's room, and what it refuses (GPU)."""
 import pytest
 import torch
 
@@ -44,3 +44,16 @@ def test_slots_past_the_room():
     at = torch.tensor([0, 63, 64, 100000], device="cuda")
     first = int(s.own[1, 0]) * 64
     assert s.slots_of(torch.ones(4, device="cuda"), at).tolist() == [first, first + 63, -1, -1]
+
+
+def test_texts_that_do_not_fit_are_refused():
+    s = server(64)
+    for texts in (draw(5, 5), draw(5, 0, 5), draw(65, 1, 1)):
+        with pytest.raises(ValueError):
+            s.read_texts(texts)
+    s.read_texts(draw(64, 1, 1))
+    with pytest.raises(ValueError):
+        s.read_texts(draw(1, 1, 1))
+    assert s.kv_len.tolist() == [64, 1, 1]
+    with pytest.raises(ValueError):
+        s.move(torch.zeros(1, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda"), 10000)
