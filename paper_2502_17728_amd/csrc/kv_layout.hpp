@@ -186,13 +186,20 @@ DN_HD int seen_keys(int n, int len, int group, int tile, int rows) {
     return keys < 0 ? 0 : keys < len ? keys : len;
 }
 
-// The page at which the line is cut `at` into a tile (it grows with `at`); nobody is left a single page.
-DN_HD int cut_page(int64_t at, int64_t weight, int pages) {
-    if (at <= 0) return 0;
-    if (at >= weight) return pages;
-    const int p = (int)((double)at * (double)pages / (double)weight);
-    return p < 2 ? 0 : pages - p < 2 ? pages : p;
-}
+// Where the line cuts a tile that weighs `weight` for `pages`: the page `at` into it, which grows with `at`;
+// nobody is left a single page.
+struct Cuts {
+    int64_t weight;
+    int pages;
+    double scale;
+    DN_HD Cuts(int64_t w, int p) : weight(w), pages(p), scale((double)p / (double)w) {}
+    DN_HD int page(int64_t at) const {
+        if (at <= 0) return 0;
+        if (at >= weight) return pages;
+        const int p = (int)((double)at * scale);
+        return p < 2 ? 0 : pages - p < 2 ? pages : p;
+    }
+};
 
 // a / b for 0 <= a, 0 < b: through doubles, which are far shorter than the 64-bit division
 DN_HD int64_t quotient(int64_t a, int64_t b) {
@@ -244,7 +251,8 @@ DN_HD void deal_run(const Line& line, int64_t run, int64_t b, int64_t b_start, i
     while (true) {
         const int64_t weight = w.of(tile), piece = ordinal + run;
         const int pages = (seen_keys(s.n, s.len, group, tile, rows) + kKvPage - 1) / kKvPage;
-        const int lo = cut_page(x0 - x, weight, pages), hi = cut_page(x1 - x, weight, pages);
+        const Cuts cuts(weight, pages);
+        const int lo = cuts.page(x0 - x), hi = cuts.page(x1 - x);
         if (ordinal >= line.tiles_most) break;  // q_start out of order
         const int slot = (int)(2 * run) + (x > x0 ? 1 : 0);
         piece_out(piece, Piece{(int)b, head, tile, lo, hi,
@@ -252,17 +260,22 @@ DN_HD void deal_run(const Line& line, int64_t run, int64_t b, int64_t b_start, i
         if (x >= x0) {
             const int64_t last = x + weight <= x1 ? run : quotient(x + weight - 1, per);
             // The tile is divided where some cut leaves pages on both sides: the first one that leaves any
-            // before it tells, for cuts only grow.  Its place is found by bisection, whatever the tile weighs
-            // for its pages (queries before the first key weigh like others and see none).
-            int64_t r = run + 1, end = last + 1;
-            while (r < end) {
-                const int64_t mid = (r + end) >> 1;
-                if (cut_page(mid * per - x, weight, pages) == 0)
-                    r = mid + 1;
-                else
-                    end = mid;
+            // before it tells, for cuts only grow.  It is mostly the run's own end, else found by bisection,
+            // whatever the tile weighs for its pages (queries before the first key weigh like others and
+            // see none).
+            int cut = hi;
+            if (last > run && cut == 0) {
+                int64_t r = run + 2, end = last;
+                while (r < end) {
+                    const int64_t mid = (r + end) >> 1;
+                    if (cuts.page(mid * per - x) == 0)
+                        r = mid + 1;
+                    else
+                        end = mid;
+                }
+                if (r <= last) cut = cuts.page(r * per - x);
             }
-            const bool divided = r <= last && cut_page(r * per - x, weight, pages) < pages;
+            const bool divided = last > run && cut > 0 && cut < pages;
             tile_out(ordinal, (int)piece, divided ? (int)(last - run) + 1 : 0);
         }
         ++count;
