@@ -186,7 +186,7 @@ def _on(stream, x: torch.Tensor):
 
 def _empty(x: torch.Tensor, shape, stream, dtype: Optional[torch.dtype] = None) -> torch.Tensor:
     """A tensor made for a call on `stream`, of x's dtype (or the one given) on x's device."""
-    if stream is not None:
+    if stream is not None and _stream(stream) != _stream_of(None, x):
         with _on(stream, x):
             return _empty(x, shape, None, dtype)
     return x.new_empty(shape) if dtype is None else torch.empty(shape, dtype=dtype, device=x.device)

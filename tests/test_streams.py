@@ -24,8 +24,8 @@ class Launch:
             m.setattr(ops._lib, name, self.call)
         m.setattr(ops, "_dev", lambda t, name: None if t is None else t.data_ptr())
         m.setattr(ops, "_rows", lambda t, name: (t.data_ptr(), t.numel() // t.shape[0]))
-        m.setattr(ops, "_stream_of", lambda stream, x: 0 if stream is None else stream)
-        m.setattr(ops, "_stream", lambda stream: 0 if stream is None else stream)
+        m.setattr(ops, "_stream_of", lambda stream, x: 77 if stream is None else stream)
+        m.setattr(ops, "_stream", lambda stream: 77 if stream is None else stream)
         m.setattr(torch.cuda, "ExternalStream", lambda handle, device=None: handle)
         m.setattr(torch.cuda, "default_stream", lambda device=None: 0)
         m.setattr(torch.cuda, "stream", self.current)
@@ -110,6 +110,13 @@ def test_what_a_call_makes_belongs_to_its_stream(name, monkeypatch):
         call(stream=stream)
         assert launch.made and all(on == stream for _, on, _ in launch.made), launch.made
     assert launch.calls == 3 and launch.on is None
+
+
+def test_the_current_stream_given_by_name(monkeypatch):
+    """No switch of streams where the one given is the current one."""
+    launch = Launch(monkeypatch)
+    calls()["attention_cache_deferred"](stream=77)
+    assert launch.calls == 1 and len(launch.made) == 2 and all(on is None for _, on, _ in launch.made)
 
 
 # ------------------------------------------------------------------------------- on the device
