@@ -363,9 +363,10 @@ DN_API dn_status attention_decode_deferred_noalloc(const void* Q, const void* K,
  *
  * rotary_apply turns x[T][H][d] (DN_F32 or DN_BF16; x_stride elements between
  * tokens, heads contiguous) by table row positions[t] into out (out_stride
- * likewise).  inverse = 1 turns back: the transpose, so the gradient with respect
- * to x from the gradient with respect to out.  out may be x itself with equal
- * strides; other overlaps are refused.  rot is a multiple of 16 up to d, d a
+ * likewise).  inverse = 1 is the transpose: the gradient with respect to x from
+ * the gradient with respect to out, and with amplitude 1 the turn back (else
+ * amplitude^2 times it).  out may be x itself with equal strides; other overlaps
+ * are refused.  rot is a multiple of 16 up to d, d a
  * multiple of 16, strides multiples of 16 bytes and at least H * d.  A position
  * outside the table gives NaN in the turned dimensions.  positions: int32, 4-byte
  * aligned.  Arithmetic is fp32, each result rounded once.
@@ -443,14 +444,19 @@ DN_API dn_status kv_cache_read(const kv_cache* cache, const int32_t* slots, int6
  * ascending from 0 to T; a sequence may have none); its kv_len[b] cached tokens,
  * the new ones last, lie in pages block_table[b][0], [1], .. (table_width entries
  * a row).  Query i of n sees keys 0 .. kv_len[b] - n + i: one new token is a decode
- * step, many are a prefill chunk, and both may meet in one call.  Query head h
+ * step, many are a prefill chunk, and both may meet in one call.  One tile size,
+ * by the mean of the new tokens, serves the whole call: a long chunk beside single
+ * tokens runs faster as two calls, each over its own sequences.  Query head h
  * reads key/value head h / (q_heads / heads).  out[T][q_heads][d]; Q has q_stride
  * elements between tokens (a multiple of 8), scale finite and > 0, dtype DN_BF16.
  * q_start, kv_len and block_table are int32 device arrays, read on the device, so a
- * recorded graph replays with their new contents.  A query that sees no key gives
- * zeros; one whose scores are all -inf gives NaN.  Entries outside the cache, the
- * table or [0, T] are kept inside (page 0, the table's width, T): memory stays
- * safe, the rows concerned are unspecified.
+ * recorded graph replays with their new contents.  Rows of Q and out past
+ * q_start[B] are neither read nor written.  A query that sees no key gives
+ * zeros; one whose scores are all -inf gives NaN.  Sums over values are fp32 and
+ * divided last, with numerators up to 2^8: the largest value times the number of
+ * keys is to stay below 2^119.  Entries outside the cache, the table or [0, T] are
+ * kept inside (page 0, the table's width, T): memory stays safe, the rows
+ * concerned are unspecified.
  * workspace: caller-owned, 256-byte aligned, attention_cache_workspace_bytes
  * (with prefix_len = 0), scratch.  Where one workgroup reads a tile's keys whole
  * one launch writes out; else partial sums go through the workspace as in

@@ -337,8 +337,8 @@ __device__ __forceinline__ void softmax_unit(const f32x4 (&s)[TILES], const f32x
 // Tiles of 16 rows.  Bound by HBM: each wave takes pages of the chunk in turn, its codes straight to
 // registers (V of a unit and K of the next in flight while the unit's scores are worked on), and
 // the four waves' sums meet in LDS at the end.  Measured, 32 sequences against 4196 to 8192 keys, 32 query over
-// 8 key/value heads of 128, fp8 (418 MB): 70 us, 6.0 TB/s; the call with its merge 75 us.  fp8 takes 218
-// registers, so two workgroups to a CU; held to 168 for three it spills (157 us).
+// 8 key/value heads of 128, fp8 (418 MB): 72 us, 5.8 TB/s; the call with its merge 75 us.  fp8 takes 217
+// registers, so two workgroups to a CU; held to 168 for three it spills (157 us, with numerators in one part).
 constexpr int kDecodeRows = 16, kDecodeParts = 2;
 template <int FMT, int D>
 constexpr int decode_lds = 4 * kDecodeRows * (D + 4) * 4 + 8 * kDecodeRows * 4;
@@ -724,7 +724,7 @@ __global__ __launch_bounds__(256, 2) void shared_kernel(const Args prefix, const
 // that runs behind (late) fills the rings, one page ahead: stage k is K of page k + 1 and V of page k.
 // With phases counted from the first scores of the early half (-1), early waves work on page k in 2k
 // and 2k + 1, late ones in 2k + 1 and 2k + 2; stage k lands by the end of 2k in slots last read in 2k - 2.
-// Bound by the VALU beside the matrix cores (52 % and 40 % busy, fp8).  Measured, 32 query over 8 key/value heads of
+// Bound by the VALU beside the matrix cores (53 % and 41 % busy, fp8).  Measured, 32 query over 8 key/value heads of
 // 128: one 2048-token chunk against 16384 keys 1050 TFLOP/s (bf16), 820 to 870 (fp8, which the late waves widen);
 // two ragged chunks of 1000 against 8191 keys, fp8, 225 us a call, 825 TFLOP/s.
 template <int FMT, int D>

@@ -70,6 +70,10 @@ inline int append_tile(int64_t tokens, int64_t heads, int64_t group, int64_t d) 
 //   itself by a scan of the lengths.  For work whose chunks are short.
 // - runs: a kernel before lists, for each of `target` workgroups, an equal stretch of all tiles' keys.
 //   It costs a launch; chunks of uneven tiles leave more of the chip idle once they are long.
+//   Measured, tiles of 256 rows in chunks / in runs, us, fp8, 32 query over 8 key/value heads of 128: two chunks of
+//   1000 tokens against 8191 keys 302 / 250, four of 500 against 4096 153 / 137, two of 512 against 2048 78.7 / 67.1, four
+//   ragged ones 272 / 233, 2048 against 16384 496 / 500.  Prompts with nothing cached before them go the other way, of
+//   4096 tokens 164 / 191, of 1024 39.1 / 48.5, eight of 1024 131 / 150; the lengths, which would tell, are on the device.
 // A tile that is cut leaves partial sums, which a last kernel merges.
 struct CachePlan {
     int rows;        // query rows per tile: 16 (keys straight to registers), 64, 128 or 256 (through LDS)
@@ -87,6 +91,10 @@ struct CachePlan {
 // 33.2 / 55.2, n = 16 38.5 / 29.8 / 35.6 / 54.8, n = 17 45.0 / 39.6 / 35.9 / 54.6, n = 64 80.8 / 67.8 / 57.4 / 62.8;
 // 128 / 256: n = 96 107 / 100, n = 384 266 / 244.  bf16: n = 4 31.5 / 31.2 / 33.8 / 49.1, n = 5 41.5 / 31.3 / 34.4 / 49.8,
 // n = 17 71.8 / 37.6 / 37.5 / 53.5, n = 64 152 / 61.9 / 56.4 / 60.1; n = 96 98 / 92.
+// The mean serves calls of like sequences.  Calls that mix a chunk and single tokens, us, against the two as
+// calls of their own: 2048 tokens beside 31 single ones, 8192 keys each 538 / 257 + 89 (single tokens in tiles of 256
+// rows), 512 beside 31, bf16, 4096 keys 162 / 62 + 87, 512 beside 255, 2048 keys 222 / 54 + 183, 300 beside 7, 4096 keys
+// 76 / 61 + 17.
 inline int cache_rows(int64_t T, int64_t B, int64_t group) {
     const int64_t rows = (T * group + B - 1) / B;
     return rows <= 16 ? 16 : rows <= 64 ? 64 : rows <= 256 ? 128 : 256;
@@ -96,9 +104,16 @@ inline CachePlan cache_plan(int64_t T, int64_t B, int64_t heads, int64_t group, 
                             bool prefix, bool always_partial) {
     CachePlan p;
     p.rows = rows;
-    // a prefix's tiles share the chip with the sequences' own keys, and its partial sums are the more the
-    // more it is cut
+    // A prefix's tiles share the chip with the sequences' own keys, and its partial sums are the more the
+    // more it is cut.  Measured, us, fp8, 32 query over 8 key/value heads of 128.  16 rows, 32 sequences of up to 8192
+    // keys, 512 / 768 / 1024 / 1536: 76.0 / 75.1 / 77.0 / 79.3.  64 and 128 rows, 256 / 512 / 1024: 8 sequences of 16 tokens, 4096
+    // keys 34.5 / 31.0 / 43.1, of 64 70.8 / 53.4 / 64.9, 32 of 16, 1024 keys 31.5 / 28.9 / 37.0.  256 rows, 256 / 512: two chunks of 1000
+    // against 8191 keys 247 / 261, 2048 against 16384 498 / 521, four ragged prompts 128 / 137.  Behind a prefix, 128 / 256 /
+    // 512: 64 sequences, 8192 keys 44.4 / 33.6 / 41.8, 128 69.7 / 49.6 / 59.3, 16 21.8 / 21.2 / 21.8; 30000 keys 117 / 69 / 62.
     p.target = rows == 16 ? 768 : rows == 256 || prefix ? 256 : 512;
+    // 16 rows at 4 / 8 / 16: one sequence of 8192 keys 12.0 / 12.4 / 14.1, four of 2000 11.9 / 11.8 / 14.1, 16 of 4096 30.0 / 30.1 / 27.2,
+    // 256 of up to 1000 67.0 / 67.1 / 62.0.  Others at 2 / 4 / 8: two of 16 tokens, 8192 keys 21.3 / 21.5 / 22.8, 64 sequences behind
+    // 8192 keys 34.8 / 33.6 / 33.6, behind 2000 29.8 / 26.2 / 28.5.
     p.least = rows == 16 && !prefix ? 8 : 4;
     p.tiles = heads * std::min(T * group, T * group / rows + std::min(B, T));
     const int64_t most = (table_width + p.least - 1) / p.least;  // chunks of one tile

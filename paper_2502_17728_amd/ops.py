@@ -588,7 +588,10 @@ def rotary_frequencies(rot: int, base: float = 10000.0, scaling: Optional[str] =
       by factor, one that turns more than ``high`` times is left, those between are blended linearly
       in their number of turns.
     - "parts_log": the same, blended linearly in the dimension (so in the logarithm of the number of
-      turns), and with the amplitude 0.1 ln(factor) + 1.
+      turns), and with the amplitude 0.1 ln(factor) + 1.  The blend starts and ends where ``high`` and
+      ``low`` turns fall, between two dimensions as it may be; for a model whose limits were rounded to
+      whole dimensions, or that was trained with other limits than the defaults here (``high`` = 32 is
+      common with this scaling), give its limits, or its own frequencies to rotary_table.
     """
     if rot < 2 or rot % 2 or not base > 0 or not factor > 0:
         raise ValueError("rot must be even and positive, base and factor positive")
@@ -677,7 +680,8 @@ def _stream_of(stream, x: torch.Tensor) -> int:
 def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, interleaved: bool = False,
                  inverse: bool = False, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """x[T, H, d] turned by each token's position (tokens may be strided, as the query heads of QKV
-    rows are; out may be x).  inverse turns back: the gradient with respect to x of the turned x."""
+    rows are; out may be x).  inverse is the transpose: the gradient with respect to x from that with
+    respect to the turned x, and the turn back where the table's amplitude is 1."""
     if x.dim() != 3:
         raise ValueError(f"x has shape {list(x.shape)}, expected [T, H, d]")
     T, H, d = x.shape
