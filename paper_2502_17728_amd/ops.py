@@ -268,7 +268,7 @@ def ln_linear_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                        out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = _empty(x, (M, w.desc.N), stream)
+        out = x.new_empty((M, w.desc.N)) if stream is None else _empty(x, (M, w.desc.N), stream)
     _check("ln_linear_deferred", _lib.ln_linear_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -334,7 +334,7 @@ def rms_linear_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = _empty(x, (M, w.desc.N), stream)
+        out = x.new_empty((M, w.desc.N)) if stream is None else _empty(x, (M, w.desc.N), stream)
     _check("rms_linear_deferred", _lib.rms_linear_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -366,7 +366,7 @@ def rms_swiglu_deferred(x: torch.Tensor, w: PreparedLinear, eps: float = 1e-5,
                         out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     M = _check_rows(x, w, out)
     if out is None:
-        out = _empty(x, (M, w.desc.N), stream)
+        out = x.new_empty((M, w.desc.N)) if stream is None else _empty(x, (M, w.desc.N), stream)
     _check("rms_swiglu_deferred", _lib.rms_swiglu_deferred(
         _dev(x, "x"), ctypes.byref(w.desc), M, eps, _dev(out, "out"), _stream(stream)))
     return out
@@ -382,7 +382,7 @@ def softmax_pv_deferred(S: torch.Tensor, V: torch.Tensor, causal: bool = False,
         _expect(V, "V", (BH, Lk, d), S.dtype, S.device)
         _expect(out, "out", (BH, Lq, d), S.dtype, S.device)
     if out is None:
-        out = _empty(S, (BH, Lq, d), stream)
+        out = S.new_empty((BH, Lq, d)) if stream is None else _empty(S, (BH, Lq, d), stream)
     _check("softmax_pv_deferred", _lib.softmax_pv_deferred(
         _dev(S, "S"), _dev(V, "V"), BH, Lq, Lk, d, int(causal), _dt(S), _dev(out, "out"), _stream(stream)))
     return out
@@ -688,7 +688,7 @@ def rotary_apply(x: torch.Tensor, positions: torch.Tensor, table: torch.Tensor, 
     xp, xs = _rows(x, "x")
     tp, rows, rot = _table_of(table, x)
     if out is None:
-        out = _empty(x, (T, H, d), stream)
+        out = x.new_empty((T, H, d)) if stream is None else _empty(x, (T, H, d), stream)
         op, os_ = out.data_ptr(), H * d
     else:
         if not _like(out, x.shape, x):
@@ -785,7 +785,7 @@ def kv_cache_append(cache: KVCache, qkv: torch.Tensor, slots: torch.Tensor, posi
         if q_out is not None:
             raise ValueError("the rows hold no queries")
     elif q_out is None:
-        q_out = _empty(qkv, (T, q_heads, d), stream)
+        q_out = qkv.new_empty((T, q_heads, d)) if stream is None else _empty(qkv, (T, q_heads, d), stream)
         op = q_out.data_ptr()
     else:
         if not _like(q_out, (T, q_heads, d), qkv):
@@ -814,7 +814,9 @@ def kv_cache_read(cache: KVCache, slots: torch.Tensor, K: Optional[torch.Tensor]
         if t is not None:
             _expect(t, name, shape, torch.bfloat16, slots.device)
     if K is None and V is None:
-        K, V = _empty(slots, (2, *shape), stream, torch.bfloat16).unbind()
+        both = (slots.new_empty((2, *shape), dtype=torch.bfloat16) if stream is None
+                else _empty(slots, (2, *shape), stream, torch.bfloat16))
+        K, V = both.unbind()
     elif K is None:
         K = _empty(V, shape, stream)
     elif V is None:
@@ -843,7 +845,7 @@ def _attention_cache_args(Q, cache, block_table, q_start, kv_len, prefix_len, sc
     B, width = block_table.shape
     qp, qs = _rows(Q, "Q")
     if out is None:
-        out = _empty(Q, (T, q_heads, d), stream)
+        out = Q.new_empty((T, q_heads, d)) if stream is None else _empty(Q, (T, q_heads, d), stream)
         op = out.data_ptr()
     else:
         if not _like(out, Q.shape, Q):
