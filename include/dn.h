@@ -458,7 +458,8 @@ DN_API dn_status kv_cache_read(const kv_cache* cache, const int32_t* slots, int6
  * kept inside (page 0, the table's width, T): memory stays safe, the rows
  * concerned are unspecified.
  * workspace: caller-owned, 256-byte aligned, attention_cache_workspace_bytes
- * (with prefix_len = 0), scratch.  Where one workgroup reads a tile's keys whole
+ * (with prefix_len = 0), scratch of one call at a time: the kernels keep lists in
+ * it that they follow.  Where one workgroup reads a tile's keys whole
  * one launch writes out; else partial sums go through the workspace as in
  * attention_decode_deferred.
  *
