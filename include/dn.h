@@ -43,7 +43,8 @@ extern "C" {
 
 #define DN_API __attribute__((visibility("default")))
 
-typedef enum { DN_F32 = 0, DN_BF16 = 1 } dn_dtype;
+/* DN_E4M3 (OCP e4m3 codes) only where an entry point names it. */
+typedef enum { DN_F32 = 0, DN_BF16 = 1, DN_E4M3 = 2 } dn_dtype;
 
 typedef enum {
     DN_OK = 0,
@@ -484,6 +485,133 @@ DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_strid
                                            const int32_t* block_table, int64_t table_width, const int32_t* q_start,
                                            const int32_t* kv_len, int64_t B, float scale, int dtype, void* workspace,
                                            size_t workspace_bytes, void* out, hipStream_t stream);
+
+/* ======================================================================= */
+/* Products in 8 bits: rows to codes, the product, its epilogue             */
+/* ======================================================================= */
+
+/*
+ * Rows as OCP e4m3 codes with one fp32 scale per row, x = code * scale:
+ * scale = max(max |x| / 448, 2^-120), the code x / scale rounded to nearest even.
+ * A row that holds a NaN or an infinity is held as codes 0 and a NaN scale, so
+ * every product with it is NaN.
+ *
+ * residual_rmsnorm: sum = x + residual and y = RMSNorm(sum) * gamma (Eq. (6), eps
+ * as for rms_linear_deferred), all [M][K] of `dtype` (DN_F32 or DN_BF16).  The
+ * norm is taken of the fp32 sum, before its rounding; sum and y are rounded once
+ * each.  residual may be NULL (sum is then NULL too: y = RMSNorm(x) * gamma), gamma
+ * NULL is all ones (as where a product's weights already hold it).  sum may be x or
+ * residual itself (the stream updated in place); y and every other pair of ranges
+ * must not overlap.
+ *
+ * residual_rmsnorm_fp8: the same with y as codes[M][K] and scales[M].  1 / rms is a
+ * positive factor of the whole row, so it scales the row's scale and leaves its codes
+ * alone: the codes are those of sum * gamma, and the normalization is deferred to the
+ * product's epilogue, where the scale is applied.
+ *
+ * rows_fp8: the codes and scales of x[M][K] itself.
+ *
+ * K is a multiple of 8 (of 16 where codes are written) up to 65536 (DN_BF16) or 32768
+ * (DN_F32), else DN_ERR_UNSUPPORTED; |sum| >= 2^64 (fp32 overflow of its square) is
+ * outside the supported range of the norms.
+ */
+DN_API dn_status residual_rmsnorm(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K, float eps,
+                           int dtype, void* sum, void* y, hipStream_t stream);
+
+DN_API dn_status residual_rmsnorm_fp8(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K,
+                               float eps, int dtype, void* sum, void* codes, float* scales, hipStream_t stream);
+
+DN_API dn_status rows_fp8(const void* x, int64_t M, int64_t K, int dtype, void* codes, float* scales, hipStream_t stream);
+
+/*
+ * Weights of an 8-bit product, laid out once per weight set.  W[K][N] is
+ *   DN_E4M3          codes, with scales[N] (fp32, one per column; W = code * scale), or
+ *   DN_F32, DN_BF16  values, quantised here: with gamma[K] (W's type, NULL: ones) the
+ *                    columns of Diag(gamma) W, each by the rule for rows above; scales
+ *                    is NULL.
+ * bias[N] (fp32) may be NULL.  W_up[K][N] (NULL: none), with its own up_scales and
+ * up_bias, makes the weights gated.  `packed`: caller-owned device memory, 256-byte
+ * aligned, linear_fp8_packed_bytes(K, N, gated) bytes.  K is a multiple of 16 below
+ * 2^23, N of 8 below 2^24.
+ * Layout (version 1): 16-column x 64-byte chunks [blocks][K padded to 128, / 64][64 lanes]
+ * [16 B] (lane l holds column l & 15, k 16 (l >> 4) ..), zero padded, then scales and bias
+ * (fp32) of every column.  blocks = ceil(N / 16); of gated weights 2 ceil(N / 16), gate and up
+ * blocks in turn.
+ */
+#define DN_FP8_LAYOUT_VERSION 1
+
+typedef struct {
+    int64_t K, N;           /* reduced dim, output features                  */
+    int32_t gated;          /* 1: packed holds gate and up columns            */
+    int32_t layout_version; /* DN_FP8_LAYOUT_VERSION when produced by prepare */
+    void* packed;
+} linear_fp8_weights;
+
+DN_API size_t linear_fp8_packed_bytes(int64_t K, int64_t N, int gated);
+
+DN_API dn_status linear_fp8_prepare(const void* W, const float* scales, const void* gamma, const float* bias,
+                             const void* W_up, const float* up_scales, const float* up_bias, int64_t K, int64_t N,
+                             int dtype, void* packed, size_t packed_bytes, linear_fp8_weights* w_out,
+                             hipStream_t stream);
+
+/*
+ * out[M][N] = act(z) + residual, z = x . W + bias of codes x[M][K] with their scales
+ * x_scales[M]; gated weights: out = act(x . W + bias) * (x . W_up + up_bias) + residual.
+ * The scales, the bias, the activation (fp32) and the residual follow once, in the
+ * epilogue, before the single rounding to out_dtype (DN_F32 or DN_BF16).  With DN_F32
+ * the codes are widened to bf16 (exactly) and their products summed in fp32; with DN_BF16
+ * the 8-bit matrix instructions sum them, twice as fast, which keep the products of 16
+ * neighbours along K to 2^-13 of their largest: 1.5e-5 of a result of normal data in the
+ * 2-norm, a hundredth of the output's rounding.  residual[M][N] (out_dtype) may
+ * be NULL, and may be out itself.
+ * workspace: caller-owned, 256-byte aligned, linear_fp8_workspace_bytes(M, w) bytes
+ * (NULL where that is 0), scratch of one call at a time: calls of few tiles split K over
+ * several workgroups, whose fp32 partial sums a second kernel joins in a fixed order.
+ * Any size is taken: a smaller workspace means fewer splits.
+ */
+typedef enum {
+    DN_ACT_NONE = 0,
+    DN_ACT_RELU = 1,
+    DN_ACT_SILU = 2,      /* z / (1 + e^-z)                                             */
+    DN_ACT_GELU = 3,      /* z (1 + erf(z / sqrt 2)) / 2                                */
+    DN_ACT_GELU_TANH = 4  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2          */
+} dn_activation;
+
+DN_API size_t linear_fp8_workspace_bytes(int64_t M, const linear_fp8_weights* w);
+
+DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_fp8_weights* w, int64_t M, int activation,
+                     const void* residual, int out_dtype, void* workspace, size_t workspace_bytes, void* out,
+                     hipStream_t stream);
+
+/* ======================================================================= */
+/* Log probabilities of tokens                                              */
+/* ======================================================================= */
+
+/*
+ * For each row of logits[T][V] (DN_F32 or DN_BF16, `stride` elements between rows, at
+ * least V; rows may start at any element): with p = softmax(scale * logits) in fp32,
+ *   logprobs[T][n]      ln p of targets[T][n] (int32): 0 for a negative target (padding),
+ *                       NaN for one past the vocabulary; n = 0: targets and logprobs NULL
+ *   entropy[T]          -sum p ln p (0 where p is 0); NULL: not wanted
+ *   top_ids[T][top]     the `top` likeliest tokens by their logits, the lowest id first
+ *                       among equals, and their ln p in top_logprobs[T][top]; top = 0: both
+ *                       NULL
+ * One pass over the logits: the softmax's maximum, its denominator and the entropy's sum
+ * are kept together and the normalization is applied to what is asked for alone.  Logits
+ * of -inf (forbidden tokens) have p = 0 and rank last.  A row whose logits are all -inf, or
+ * that holds +inf or a NaN, gives NaN (targets < 0 excepted); NaN logits have no rank, and
+ * a rank that no token has is id -1.  top <= min(V, 64), V < 2^31, scale finite and > 0.
+ * logits is aligned to its element, every other array to 16 bytes.
+ * workspace: caller-owned, 256-byte aligned, token_logprobs_workspace_bytes bytes (NULL
+ * where that is 0), scratch of one call at a time: long rows are read by several
+ * workgroups each, whose sums and ranks a second kernel joins in a fixed order.
+ */
+DN_API size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t top);
+
+DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
+                         const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
+                         float* top_logprobs, int32_t* top_ids, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
 
 /* ======================================================================= */
 /* Unfused comparators: the conventional sub-graph of Fig. 1(a)             */

@@ -23,7 +23,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libdn.so")
 SOURCES = ["ln_gemm.hip", "ln_skinny.hip", "ln_skinny_f32.hip", "softmax_pv.hip", "attention.hip", "baselines.hip",
-           "kv_cache.hip", "attention_cache.hip", "abi.cpp"]
+           "kv_cache.hip", "attention_cache.hip", "norm_fp8.hip", "linear_fp8.hip", "logprobs.hip", "abi.cpp"]
 ARCH = "gfx950"
 
 

@@ -1,11 +1,13 @@
 // abi.cpp -- the C ABI of libdn (declared in include/dn.h): argument
 // validation on the host, then dispatch to the kernel launchers.  No entry
 // point touches the HIP runtime before its arguments have been validated.
+#include <algorithm>
 #include <math.h>
 #include <stdint.h>
 
 #include "dn.h"
 #include "dn_launch.hpp"
+#include "fp8_rules.hpp"
 #include "kv_layout.hpp"
 #include "launch_rules.hpp"
 
@@ -633,6 +635,178 @@ DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_strid
     if (!prefix_table || prefix_len < 1) return DN_ERR_INVALID_ARG;
     return attention_cache(Q, q_stride, T, q_heads, cache, prefix_table, prefix_len, block_table, table_width, q_start,
                            kv_len, B, scale, dtype, workspace, workspace_bytes, out, stream);
+}
+
+// ------------------------------------------------------------------------------- products in 8 bits
+// One range of an argument list; of its outputs none overlaps another or an input.
+namespace {
+struct Range {
+    const void* p;
+    size_t n;
+};
+bool any_overlap(const Range& a, const Range* others, int count) {
+    for (int i = 0; i < count; ++i)
+        if (overlaps(a.p, a.n, others[i].p, others[i].n)) return true;
+    return false;
+}
+}  // namespace
+
+static dn_status rows_call(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K, float eps, int dtype,
+                           void* sum, void* y, float* scales, bool fp8, bool norm, hipStream_t stream) {
+    if (!x || !y || (fp8 && !scales) || M < 1 || K < 1 || !valid_dtype(dtype) || !isfinite(eps) || eps < 0.f)
+        return DN_ERR_INVALID_ARG;
+    if (!residual != !sum) return DN_ERR_INVALID_ARG;
+    size_t xb, yb;
+    if (!bytes_of(M, K, (int64_t)esize(dtype), &xb) || !bytes_of(M, K, fp8 ? 1 : (int64_t)esize(dtype), &yb))
+        return DN_ERR_INVALID_ARG;
+    if (K % (fp8 ? 16 : 8) || K > (dtype == DN_F32 ? dn::kMaxRowF32 : dn::kMaxRowBf16) || M > kMaxGridX)
+        return DN_ERR_UNSUPPORTED;
+    if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(gamma, 16) || !aligned(sum, 16) || !aligned(y, 16) ||
+        !aligned(scales, 16))
+        return DN_ERR_MISALIGNED;
+    const Range in[3] = {{x, xb}, {residual, xb}, {gamma, (size_t)K * esize(dtype)}};
+    const Range out_y{y, yb}, out_s{scales, (size_t)M * 4}, out_sum{sum, xb};
+    if (any_overlap(out_y, in, 3) || any_overlap(out_s, in, 3) || any_overlap(out_sum, &out_y, 1) ||
+        any_overlap(out_sum, &out_s, 1) || any_overlap(out_y, &out_s, 1) || any_overlap(out_sum, in + 2, 1))
+        return DN_ERR_INVALID_ARG;
+    if ((sum != x && any_overlap(out_sum, in, 1)) || (sum != residual && any_overlap(out_sum, in + 1, 1)))
+        return DN_ERR_INVALID_ARG;
+    if (!norm) return from_hip(dn::launch_rows_fp8(x, M, K, dtype, y, scales, stream));
+    return from_hip(dn::launch_residual_rmsnorm(x, residual, gamma, M, K, eps, dtype, sum, y, scales, stream));
+}
+
+DN_API dn_status residual_rmsnorm(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K, float eps,
+                                  int dtype, void* sum, void* y, hipStream_t stream) {
+    return rows_call(x, residual, gamma, M, K, eps, dtype, sum, y, nullptr, false, true, stream);
+}
+
+DN_API dn_status residual_rmsnorm_fp8(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K, float eps,
+                                      int dtype, void* sum, void* codes, float* scales, hipStream_t stream) {
+    return rows_call(x, residual, gamma, M, K, eps, dtype, sum, codes, scales, true, true, stream);
+}
+
+DN_API dn_status rows_fp8(const void* x, int64_t M, int64_t K, int dtype, void* codes, float* scales, hipStream_t stream) {
+    return rows_call(x, nullptr, nullptr, M, K, 0.f, dtype, nullptr, codes, scales, true, false, stream);
+}
+
+// K < 2^23: 32-bit offsets in a tile's 256 rows; N < 2^24 likewise in the packed columns.
+static dn_status fp8_sizes(int64_t K, int64_t N, int gated) {
+    if (K < 1 || N < 1 || (gated != 0 && gated != 1)) return DN_ERR_INVALID_ARG;
+    return K % 16 || N % 8 || K >= (int64_t(1) << 23) || N >= (int64_t(1) << 24) ? DN_ERR_UNSUPPORTED : DN_OK;
+}
+
+DN_API size_t linear_fp8_packed_bytes(int64_t K, int64_t N, int gated) {
+    return fp8_sizes(K, N, gated) == DN_OK ? dn::fp8_layout(K, N, gated).total : 0;
+}
+
+DN_API dn_status linear_fp8_prepare(const void* W, const float* scales, const void* gamma, const float* bias,
+                                    const void* W_up, const float* up_scales, const float* up_bias, int64_t K, int64_t N,
+                                    int dtype, void* packed, size_t packed_bytes, linear_fp8_weights* w_out,
+                                    hipStream_t stream) {
+    const bool codes = dtype == DN_E4M3;
+    if (!W || !packed || !w_out || (!codes && !valid_dtype(dtype))) return DN_ERR_INVALID_ARG;
+    // codes come with their scales and have no gamma to fold; values are quantised here
+    if (codes ? (!scales || gamma || !W_up != !up_scales) : (scales || up_scales)) return DN_ERR_INVALID_ARG;
+    if (!W_up && (up_scales || up_bias)) return DN_ERR_INVALID_ARG;
+    const int gated = W_up != nullptr;
+    const dn_status st = fp8_sizes(K, N, gated);
+    if (st != DN_OK) return st;
+    const size_t need = dn::fp8_layout(K, N, gated).total, es = codes ? 1 : esize(dtype);
+    if (packed_bytes < need) return DN_ERR_INVALID_ARG;
+    const void* in16[7] = {W, scales, gamma, bias, W_up, up_scales, up_bias};
+    const size_t in_bytes[7] = {(size_t)K * N * es, (size_t)N * 4, (size_t)K * es, (size_t)N * 4,
+                                (size_t)K * N * es, (size_t)N * 4, (size_t)N * 4};
+    if (!aligned(packed, 256)) return DN_ERR_MISALIGNED;
+    for (int i = 0; i < 7; ++i)
+        if (!aligned(in16[i], 16)) return DN_ERR_MISALIGNED;
+    for (int i = 0; i < 7; ++i)
+        if (overlaps(packed, need, in16[i], in_bytes[i])) return DN_ERR_INVALID_ARG;
+    const dn_status done = from_hip(
+        dn::launch_linear_fp8_prepare(W, scales, gamma, bias, W_up, up_scales, up_bias, K, N, dtype, packed, stream));
+    if (done == DN_OK) *w_out = linear_fp8_weights{K, N, gated, DN_FP8_LAYOUT_VERSION, packed};
+    return done;
+}
+
+static dn_status fp8_weights_valid(const linear_fp8_weights* w) {
+    if (!w || !w->packed || w->layout_version != DN_FP8_LAYOUT_VERSION) return DN_ERR_INVALID_ARG;
+    return fp8_sizes(w->K, w->N, w->gated);
+}
+// Bytes of M x N results are counted with 8 bytes each: partial sums of gated weights have as many.
+static bool fp8_rows_valid(int64_t M, const linear_fp8_weights* w) {
+    size_t b;
+    return M >= 1 && bytes_of(M, std::max(w->K, w->N + 32), 8 * dn::kMaxSplits, &b);
+}
+
+DN_API size_t linear_fp8_workspace_bytes(int64_t M, const linear_fp8_weights* w) {
+    if (fp8_weights_valid(w) != DN_OK || !fp8_rows_valid(M, w)) return 0;
+    return dn::fp8_workspace(M, w->K, dn::fp8_layout(w->K, w->N, w->gated).blocks);
+}
+
+DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_fp8_weights* w, int64_t M, int activation,
+                            const void* residual, int out_dtype, void* workspace, size_t workspace_bytes, void* out,
+                            hipStream_t stream) {
+    if (!x || !x_scales || !out || activation < DN_ACT_NONE || activation > DN_ACT_GELU_TANH || !valid_dtype(out_dtype))
+        return DN_ERR_INVALID_ARG;
+    const dn_status st = fp8_weights_valid(w);
+    if (st != DN_OK) return st;
+    if (!fp8_rows_valid(M, w)) return DN_ERR_INVALID_ARG;
+    const int64_t K = w->K, N = w->N;
+    const dn::Fp8Layout l = dn::fp8_layout(K, N, w->gated);
+    if ((M + 15) / 16 * l.blocks > kMaxGridX || (M * (N / 8) + 255) / 256 > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    if (!aligned(x, 16) || !aligned(x_scales, 16) || !aligned(residual, 16) || !aligned(out, 16) ||
+        !aligned(w->packed, 256) || !aligned(workspace, 256))
+        return DN_ERR_MISALIGNED;
+    const size_t part = dn::fp8_partial_bytes(M, l.blocks);
+    const int64_t fit = workspace ? (int64_t)std::min<size_t>(workspace_bytes / part, dn::kMaxSplits) : 1;
+    const size_t used = fit > 1 ? std::min(workspace_bytes, dn::fp8_workspace(M, K, l.blocks)) : 0;
+    const size_t ob = (size_t)M * N * esize(out_dtype);
+    const Range in[4] = {{x, (size_t)M * K}, {x_scales, (size_t)M * 4}, {w->packed, l.total}, {residual, ob}};
+    const Range out_r{out, ob}, scratch{workspace, used};
+    if (any_overlap(out_r, in, 3) || any_overlap(scratch, in, 4) || any_overlap(scratch, &out_r, 1) ||
+        (residual != out && any_overlap(out_r, in + 3, 1)))
+        return DN_ERR_INVALID_ARG;
+    return from_hip(dn::launch_linear_fp8(x, x_scales, w->packed, M, K, N, w->gated, activation, residual, out_dtype,
+                                          workspace, fit, out, stream));
+}
+
+// ------------------------------------------------------------------------------- log probabilities
+static bool logprob_sizes(int64_t T, int64_t V, int64_t top) {
+    size_t b;
+    return T >= 1 && V >= 1 && V < (int64_t(1) << 31) && top >= 0 && top <= std::min(V, dn::kMaxTop) &&
+           bytes_of(T, V, 8, &b) && bytes_of(T, dn::kMaxSegments, 16 + 8 * dn::kMaxTop, &b);
+}
+
+DN_API size_t token_logprobs_workspace_bytes(int64_t T, int64_t V, int64_t top) {
+    return logprob_sizes(T, V, top) ? dn::logprob_workspace(T, V, top) : 0;
+}
+
+DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
+                                const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
+                                float* top_logprobs, int32_t* top_ids, void* workspace, size_t workspace_bytes,
+                                hipStream_t stream) {
+    if (!logits || !valid_dtype(dtype) || !logprob_sizes(T, V, top) || stride < V || n < 0) return DN_ERR_INVALID_ARG;
+    if (!isfinite(scale * 1.5f) || !(scale > 0.f)) return DN_ERR_INVALID_ARG;
+    if ((n > 0) != (targets != nullptr) || (n > 0) != (logprobs != nullptr) || (top > 0) != (top_logprobs != nullptr) ||
+        (top > 0) != (top_ids != nullptr) || (!n && !top && !entropy))
+        return DN_ERR_INVALID_ARG;
+    size_t lb, nb;
+    if (!bytes_of(T, stride, (int64_t)esize(dtype), &lb) || !bytes_of(T, std::max<int64_t>(n, 1), 4, &nb))
+        return DN_ERR_INVALID_ARG;
+    lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
+    const int64_t segments = dn::logprob_segments(T, V);
+    if (T * segments > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    if (!aligned(logits, esize(dtype)) || !aligned(targets, 16) || !aligned(logprobs, 16) || !aligned(entropy, 16) ||
+        !aligned(top_logprobs, 16) || !aligned(top_ids, 16) || !aligned(workspace, 256))
+        return DN_ERR_MISALIGNED;
+    const size_t need = dn::logprob_workspace(T, V, top);
+    if (need && (!workspace || workspace_bytes < need)) return DN_ERR_INVALID_ARG;
+    const Range in[2] = {{logits, lb}, {targets, n ? nb : 0}};
+    const Range outs[5] = {{logprobs, n ? nb : 0}, {entropy, (size_t)T * 4}, {top_logprobs, (size_t)T * top * 4},
+                           {top_ids, (size_t)T * top * 4}, {workspace, need}};
+    for (int i = 0; i < 5; ++i)
+        if (any_overlap(outs[i], in, 2) || any_overlap(outs[i], outs + i + 1, 4 - i)) return DN_ERR_INVALID_ARG;
+    return from_hip(dn::launch_token_logprobs(logits, stride, T, V, dtype, scale, targets, n, top, logprobs, entropy,
+                                              top_logprobs, top_ids, workspace, segments, stream));
 }
 
 }  // extern "C"

@@ -155,6 +155,24 @@ struct AttentionCacheCall {
 };
 hipError_t launch_attention_cache(const AttentionCacheCall& c, hipStream_t s);
 
+// RMSNorm of x + residual (residual, gamma null: none, ones): rows of dtype in y, or, with scales, e4m3 codes.
+hipError_t launch_residual_rmsnorm(const void* x, const void* residual, const void* gamma, int64_t M, int64_t K, float eps,
+                                   int dtype, void* sum, void* y, float* scales, hipStream_t s);
+hipError_t launch_rows_fp8(const void* x, int64_t M, int64_t K, int dtype, void* codes, float* scales, hipStream_t s);
+
+// Weights of the 8-bit products (W_up null: not gated) and the products.
+hipError_t launch_linear_fp8_prepare(const void* W, const float* scales, const void* gamma, const float* bias,
+                                     const void* W_up, const float* up_scales, const float* up_bias, int64_t K, int64_t N,
+                                     int dtype, void* packed, hipStream_t s);
+hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed, int64_t M, int64_t K, int64_t N, int gated,
+                             int act, const void* residual, int out_dtype, void* workspace, int64_t splits_that_fit,
+                             void* out, hipStream_t s);
+
+// Log probabilities, entropy and ranks of T rows; segments > 1 go through the workspace.
+hipError_t launch_token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
+                                 const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
+                                 float* top_logprobs, int32_t* top_ids, void* workspace, int64_t segments, hipStream_t s);
+
 // Largest K (elements per row) the row-wise unfused kernels keep in registers.
 constexpr int64_t kMaxRowElemsBf16 = 16384;
 constexpr int64_t kMaxRowElemsF32 = 8192;

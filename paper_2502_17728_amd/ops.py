@@ -11,6 +11,7 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
+import functools
 import math
 import os
 from typing import Optional
@@ -19,7 +20,7 @@ import torch
 
 _LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libdn.so")
 
-DN_F32, DN_BF16 = 0, 1
+DN_F32, DN_BF16, DN_E4M3 = 0, 1, 2
 DN_LN_LAYOUT_VERSION = 2
 DN_SWIGLU_LAYOUT_VERSION = 0x102
 STATUS = {0: "DN_OK", 1: "DN_ERR_INVALID_ARG", 2: "DN_ERR_UNSUPPORTED", 3: "DN_ERR_MISALIGNED", 4: "DN_ERR_HIP"}
@@ -31,10 +32,14 @@ SYMBOLS = ("dn_status_string", "dn_version", "ln_linear_packed_bytes", "ln_linea
            "attention_decode_deferred", "attention_decode_deferred_noalloc", "layernorm",
            "rmsnorm", "silu_mul", "softmax", "gemm", "rotary_table", "rotary_apply", "kv_cache_bytes",
            "kv_cache_describe", "kv_cache_append", "kv_cache_read", "attention_cache_workspace_bytes",
-           "attention_cache_deferred", "attention_shared_prefix_deferred")
+           "attention_cache_deferred", "attention_shared_prefix_deferred", "residual_rmsnorm", "residual_rmsnorm_fp8",
+           "rows_fp8", "linear_fp8_packed_bytes", "linear_fp8_prepare", "linear_fp8_workspace_bytes", "linear_fp8",
+           "token_logprobs_workspace_bytes", "token_logprobs")
 DN_KV_PAGE = 64
 DN_KV_LAYOUT_VERSION = 1
 KV_FORMATS = {"bf16": 1, "fp8": 2}  # DN_KV_BF16, DN_KV_FP8
+DN_FP8_LAYOUT_VERSION = 1
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3, "gelu_tanh": 4}  # dn_activation
 
 
 class DNError(RuntimeError):
@@ -53,6 +58,12 @@ class KVCacheDesc(ctypes.Structure):
     """Mirror of ``kv_cache`` in dn.h."""
     _fields_ = [("pages", ctypes.c_int64), ("heads", ctypes.c_int64), ("d", ctypes.c_int64),
                 ("format", ctypes.c_int32), ("layout_version", ctypes.c_int32), ("data", ctypes.c_void_p)]
+
+
+class LinearFp8Weights(ctypes.Structure):
+    """Mirror of ``linear_fp8_weights`` in dn.h."""
+    _fields_ = [("K", ctypes.c_int64), ("N", ctypes.c_int64), ("gated", ctypes.c_int32),
+                ("layout_version", ctypes.c_int32), ("packed", ctypes.c_void_p)]
 
 
 def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
@@ -100,6 +111,16 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
     lib.attention_cache_deferred.argtypes = [vp, i64, i64, i64, kv, vp, i64, vp, vp, i64, f32, i32, vp, sz, vp, vp]
     lib.attention_shared_prefix_deferred.argtypes = [vp, i64, i64, i64, kv, vp, i64, vp, i64, vp, vp, i64, f32, i32, vp,
                                                      sz, vp, vp]
+    fw = ctypes.POINTER(LinearFp8Weights)
+    lib.residual_rmsnorm.argtypes = [vp, vp, vp, i64, i64, f32, i32, vp, vp, vp]
+    lib.residual_rmsnorm_fp8.argtypes = [vp, vp, vp, i64, i64, f32, i32, vp, vp, vp, vp]
+    lib.rows_fp8.argtypes = [vp, i64, i64, i32, vp, vp, vp]
+    lib.linear_fp8_packed_bytes.argtypes, lib.linear_fp8_packed_bytes.restype = [i64, i64, i32], sz
+    lib.linear_fp8_prepare.argtypes = [vp] * 7 + [i64, i64, i32, vp, sz, fw, vp]
+    lib.linear_fp8_workspace_bytes.argtypes, lib.linear_fp8_workspace_bytes.restype = [i64, fw], sz
+    lib.linear_fp8.argtypes = [vp, vp, fw, i64, i32, vp, i32, vp, sz, vp, vp]
+    lib.token_logprobs_workspace_bytes.argtypes, lib.token_logprobs_workspace_bytes.restype = [i64] * 3, sz
+    lib.token_logprobs.argtypes = [vp, i64, i64, i64, i32, f32, vp, i64, i64, vp, vp, vp, vp, vp, sz, vp]
     for f in ("ln_linear_prepare", "ln_linear_deferred", "rms_linear_deferred", "ln_linear_prepare_centered",
               "ln_linear_serial", "ln_linear_norm_on_load", "ln_linear_deferred_post",
               "rms_linear_deferred_post", "swiglu_prepare", "rms_swiglu_deferred", "softmax_pv_deferred",
@@ -107,7 +128,8 @@ def load_library(path: str = _LIB_PATH) -> ctypes.CDLL:
               "attention_decode_deferred_noalloc", "layernorm", "rmsnorm",
               "silu_mul", "softmax",
               "gemm", "rotary_table", "rotary_apply", "kv_cache_describe", "kv_cache_append", "kv_cache_read",
-              "attention_cache_deferred", "attention_shared_prefix_deferred"):
+              "attention_cache_deferred", "attention_shared_prefix_deferred", "residual_rmsnorm", "residual_rmsnorm_fp8",
+              "rows_fp8", "linear_fp8_prepare", "linear_fp8", "token_logprobs"):
         getattr(lib, f).restype = i32
     return lib
 
@@ -894,4 +916,265 @@ def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_tab
     st = _lib.attention_shared_prefix_deferred(*head, pp, prefix_len, *tail, _stream_of(stream, Q))
     if st:
         raise DNError("attention_shared_prefix_deferred", st)
+    return out
+
+
+# ------------------------------------------------------------------------------- products in 8 bits
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+
+
+def _on_its_device(f):
+    """f, launched on the device of its first tensor where that is not the current one."""
+    @functools.wraps(f)
+    def call(x, *args, **kwargs):
+        if isinstance(x, torch.Tensor) and x.is_cuda and x.get_device() != _current_device():
+            with torch.cuda.device(x.get_device()):
+                return f(x, *args, **kwargs)
+        return f(x, *args, **kwargs)
+    return call
+
+
+def _ptr(t: Optional[torch.Tensor], name: str, shape, dtype, device: int):
+    """Pointer of a contiguous GPU tensor of this shape and type; None for None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.shape == shape and t.dtype is dtype and t.get_device() == device
+            and t.is_contiguous()):
+        _expect(t, name, shape, dtype, torch.device("cuda", device))
+        return _dev(t, name)
+    return t.data_ptr()
+
+
+def _rows_of(x: torch.Tensor):
+    """Pointer and sizes of x[M, K], and its device."""
+    if not isinstance(x, torch.Tensor) or x.dim() != 2:
+        raise ValueError(f"x has shape {list(x.shape)}, expected [M, K]")
+    M, K = x.shape
+    return _dev(x, "x"), M, K, x.get_device()
+
+
+def _sum_of(x, residual, total, M, K, dev, stream):
+    """Pointers of the residual and of the sum's tensor, which is made where it was not given."""
+    if residual is None:
+        if total is not None:
+            raise ValueError("there is no residual to sum")
+        return None, None, None
+    rp = _ptr(residual, "residual", (M, K), x.dtype, dev)
+    if total is None:
+        total = x.new_empty((M, K)) if stream is None else _empty(x, (M, K), stream)
+        return rp, total.data_ptr(), total
+    return rp, _ptr(total, "total", (M, K), x.dtype, dev), total
+
+
+@_on_its_device
+def residual_rmsnorm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
+                     eps: float = 1e-5, total: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+                     stream=None):
+    """(RMSNorm(x + residual) * gamma, x + residual) of x[M, K] and residual[M, K]; without a residual the
+    second is None.  total may be x or residual: the stream updated in place."""
+    xp, M, K, dev = _rows_of(x)
+    rp, sp, total = _sum_of(x, residual, total, M, K, dev, stream)
+    gp = _ptr(gamma, "gamma", (K,), x.dtype, dev)
+    if out is None:
+        out = x.new_empty((M, K)) if stream is None else _empty(x, (M, K), stream)
+        op = out.data_ptr()
+    else:
+        op = _ptr(out, "out", (M, K), x.dtype, dev)
+    st = _lib.residual_rmsnorm(xp, rp, gp, M, K, eps, _dt(x), sp, op, _stream_of(stream, x))
+    if st:
+        raise DNError("residual_rmsnorm", st)
+    return out, total
+
+
+def _codes_for(x, M, K, codes, scales, dev, stream):
+    if codes is None:
+        codes = _empty(x, (M, K), stream, torch.float8_e4m3fn)
+        cp = codes.data_ptr()
+    else:
+        cp = _ptr(codes, "codes", (M, K), torch.float8_e4m3fn, dev)
+    if scales is None:
+        scales = _empty(x, (M,), stream, torch.float32)
+        return cp, scales.data_ptr(), codes, scales
+    return cp, _ptr(scales, "scales", (M,), torch.float32, dev), codes, scales
+
+
+@_on_its_device
+def residual_rmsnorm_fp8(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
+                         eps: float = 1e-5, total: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
+                         scales: Optional[torch.Tensor] = None, stream=None):
+    """(codes, scales, x + residual): residual_rmsnorm with its rows as e4m3 codes [M, K] and one scale a row."""
+    xp, M, K, dev = _rows_of(x)
+    rp, sp, total = _sum_of(x, residual, total, M, K, dev, stream)
+    gp = _ptr(gamma, "gamma", (K,), x.dtype, dev)
+    cp, scp, codes, scales = _codes_for(x, M, K, codes, scales, dev, stream)
+    st = _lib.residual_rmsnorm_fp8(xp, rp, gp, M, K, eps, _dt(x), sp, cp, scp, _stream_of(stream, x))
+    if st:
+        raise DNError("residual_rmsnorm_fp8", st)
+    return codes, scales, total
+
+
+@_on_its_device
+def rows_fp8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
+    """(codes, scales): the rows of x[M, K] as e4m3 codes and one scale each, x = codes * scales[:, None]."""
+    xp, M, K, dev = _rows_of(x)
+    cp, scp, codes, scales = _codes_for(x, M, K, codes, scales, dev, stream)
+    st = _lib.rows_fp8(xp, M, K, _dt(x), cp, scp, _stream_of(stream, x))
+    if st:
+        raise DNError("rows_fp8", st)
+    return codes, scales
+
+
+@dataclasses.dataclass
+class PreparedFp8:
+    """Weights of linear_fp8: the packed device buffer and its descriptor."""
+    packed: torch.Tensor
+    desc: LinearFp8Weights
+
+    def __post_init__(self):
+        self.ref = ctypes.byref(self.desc)
+
+    @property
+    def K(self):
+        return self.desc.K
+
+    @property
+    def N(self):
+        return self.desc.N
+
+    @property
+    def gated(self):
+        return bool(self.desc.gated)
+
+
+def linear_fp8_packed_bytes(K: int, N: int, gated: bool = False) -> int:
+    return int(_lib.linear_fp8_packed_bytes(K, N, int(gated)))
+
+
+@_on_its_device
+def linear_fp8_prepare(W: torch.Tensor, scales: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
+                       bias: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
+                       up_scales: Optional[torch.Tensor] = None, up_bias: Optional[torch.Tensor] = None,
+                       stream=None) -> PreparedFp8:
+    """Weights of linear_fp8 from W[K, N]: float8_e4m3fn codes with one fp32 scale per column, or fp32 or
+    bf16 values that are quantised here (with gamma[K]: Diag(gamma) W).  bias[N] is fp32.  up[K, N], with its own
+    scales and bias, makes the weights gated: act(x W + bias) * (x up + up_bias)."""
+    if W.dim() != 2:
+        raise ValueError(f"W has shape {list(W.shape)}, expected [K, N]")
+    K, N = W.shape
+    dt = DN_E4M3 if W.dtype is torch.float8_e4m3fn else _dt(W)
+    _expect(gamma, "gamma", (K,), W.dtype, W.device)
+    _expect(up, "up", (K, N), W.dtype, W.device)
+    for name, t in (("scales", scales), ("bias", bias), ("up_scales", up_scales), ("up_bias", up_bias)):
+        _expect(t, name, (N,), torch.float32, W.device)
+    nbytes = linear_fp8_packed_bytes(K, N, up is not None)
+    if nbytes == 0:
+        raise DNError("linear_fp8_packed_bytes", 2)
+    packed = _empty(W, nbytes, stream, torch.uint8)
+    desc = LinearFp8Weights()
+    _check("linear_fp8_prepare", _lib.linear_fp8_prepare(
+        _dev(W, "W"), _dev(scales, "scales"), _dev(gamma, "gamma"), _dev(bias, "bias"), _dev(up, "up"),
+        _dev(up_scales, "up_scales"), _dev(up_bias, "up_bias"), K, N, dt, packed.data_ptr(), nbytes, ctypes.byref(desc),
+        _stream_of(stream, W)))
+    return PreparedFp8(packed, desc)
+
+
+def linear_fp8_workspace_bytes(M: int, w: PreparedFp8) -> int:
+    return int(_lib.linear_fp8_workspace_bytes(M, w.ref))
+
+
+def _scratch(x: torch.Tensor, workspace: Optional[torch.Tensor], need, stream):
+    """The workspace given, or one made of need() bytes (None for 0)."""
+    if workspace is None:
+        n = need()
+        return _empty(x, n, stream, torch.uint8) if n else None
+    if workspace.dtype is not torch.uint8 or workspace.get_device() != x.get_device() or not workspace.is_contiguous():
+        _expect(workspace, "workspace", None, torch.uint8, x.device)
+        _dev(workspace, "workspace")
+    return workspace
+
+
+@_on_its_device
+def linear_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: PreparedFp8, activation: str = "none",
+               residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               out_dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
+               stream=None) -> torch.Tensor:
+    """act(x W + bias) + residual of e4m3 rows x[M, K] with scales x_scales[M] (gated weights: times x up + up_bias
+    before the residual).  activation: "none", "relu", "silu", "gelu" or "gelu_tanh".  The result has out_dtype
+    (fp32 or bf16; by default out's or residual's type, else bf16); residual may be out."""
+    if not isinstance(w, PreparedFp8):
+        raise TypeError("w must come from linear_fp8_prepare")
+    act = ACTIVATIONS.get(activation)
+    if act is None:
+        raise ValueError(f"unknown activation {activation!r}")
+    desc = w.desc
+    K, N, dev = desc.K, desc.N, w.packed.get_device()
+    if x.dim() != 2:
+        raise ValueError(f"x has shape {list(x.shape)}, expected [M, {K}]")
+    M = x.shape[0]
+    xp = _ptr(x, "x", (M, K), torch.float8_e4m3fn, dev)
+    sp = _ptr(x_scales, "x_scales", (M,), torch.float32, dev)
+    if sp is None:
+        raise ValueError("x_scales is required")
+    if out_dtype is None:
+        like = out if out is not None else residual
+        out_dtype = torch.bfloat16 if like is None else like.dtype
+    rp = _ptr(residual, "residual", (M, N), out_dtype, dev)
+    if out is None:
+        out = _empty(x, (M, N), stream, out_dtype)
+        op = out.data_ptr()
+    else:
+        op = _ptr(out, "out", (M, N), out_dtype, dev)
+    held = _scratch(x, workspace, lambda: _lib.linear_fp8_workspace_bytes(M, w.ref), stream)
+    st = _lib.linear_fp8(xp, sp, w.ref, M, act, rp, _dt(out), None if held is None else held.data_ptr(),
+                         0 if held is None else held.numel(), op, _stream_of(stream, x))
+    if st:
+        raise DNError("linear_fp8", st)
+    return out
+
+
+# ------------------------------------------------------------------------------- log probabilities
+def token_logprobs_workspace_bytes(T: int, V: int, top: int = 0) -> int:
+    return int(_lib.token_logprobs_workspace_bytes(T, V, top))
+
+
+@_on_its_device
+def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, scale: float = 1.0,
+                   entropy: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
+    """{"logprobs", "entropy", "top_logprobs", "top_ids"} of softmax(scale * logits) for logits[T, V] (rows may be
+    strided, V and the stride odd): ln p of targets[T, n] (int32; 0 for a negative one), the entropy [T], and the
+    `top` likeliest tokens (the lowest id first among equals) with their ln p.  What was not asked for is None."""
+    if logits.dim() != 2:
+        raise ValueError(f"logits has shape {list(logits.shape)}, expected [T, V]")
+    if not logits.is_cuda:
+        raise ValueError("logits must be a GPU tensor")
+    T, V = logits.shape
+    if logits.stride(1) != 1 and V != 1:
+        raise ValueError("logits must be contiguous within a row")
+    stride = logits.stride(0) if T != 1 else V
+    n, tp, lp, given = 0, None, None, None
+    if targets is not None:
+        if targets.dim() != 2:
+            raise ValueError(f"targets has shape {list(targets.shape)}, expected [T, n]")
+        n = targets.shape[1]
+        tp = _int32(targets, "targets", (T, n), logits)
+        if n:
+            given = _empty(logits, (T, n), stream, torch.float32)
+            lp = given.data_ptr()
+        else:
+            tp = None
+    out = {"logprobs": given, "entropy": None, "top_logprobs": None, "top_ids": None}
+    ep = kp = ip = None
+    if entropy:
+        out["entropy"] = _empty(logits, (T,), stream, torch.float32)
+        ep = out["entropy"].data_ptr()
+    if top > 0:
+        out["top_logprobs"] = _empty(logits, (T, top), stream, torch.float32)
+        out["top_ids"] = _empty(logits, (T, top), stream, torch.int32)
+        kp, ip = out["top_logprobs"].data_ptr(), out["top_ids"].data_ptr()
+    held = _scratch(logits, workspace, lambda: _lib.token_logprobs_workspace_bytes(T, V, top), stream)
+    st = _lib.token_logprobs(logits.data_ptr(), stride, T, V, _dt(logits), scale, tp, n, top, lp, ep, kp, ip,
+                             None if held is None else held.data_ptr(), 0 if held is None else held.numel(),
+                             _stream_of(stream, logits))
+    if st:
+        raise DNError("token_logprobs", st)
     return out
