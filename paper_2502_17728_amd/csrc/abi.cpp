@@ -739,7 +739,7 @@ static bool fp8_rows_valid(int64_t M, const linear_fp8_weights* w) {
 
 DN_API size_t linear_fp8_workspace_bytes(int64_t M, const linear_fp8_weights* w) {
     if (fp8_weights_valid(w) != DN_OK || !fp8_rows_valid(M, w)) return 0;
-    return dn::fp8_workspace(M, w->K, dn::fp8_layout(w->K, w->N, w->gated).blocks);
+    return dn::fp8_workspace(M, w->K, dn::fp8_layout(w->K, w->N, w->gated).blocks, w->gated);
 }
 
 DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_fp8_weights* w, int64_t M, int activation,
@@ -757,8 +757,8 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
         !aligned(w->packed, 256) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;
     const size_t part = dn::fp8_partial_bytes(M, l.blocks);
-    const int64_t fit = workspace ? (int64_t)std::min<size_t>(workspace_bytes / part, dn::kMaxSplits) : 1;
-    const size_t used = fit > 1 ? std::min(workspace_bytes, dn::fp8_workspace(M, K, l.blocks)) : 0;
+    const int64_t fit = workspace ? std::max<int64_t>(1, (int64_t)std::min<size_t>(workspace_bytes / part, dn::kMaxSplits)) : 1;
+    const size_t used = fit > 1 ? std::min(workspace_bytes, dn::fp8_workspace(M, K, l.blocks, w->gated)) : 0;
     const size_t ob = (size_t)M * N * esize(out_dtype);
     const Range in[4] = {{x, (size_t)M * K}, {x_scales, (size_t)M * 4}, {w->packed, l.total}, {residual, ob}};
     const Range out_r{out, ob}, scratch{workspace, used};

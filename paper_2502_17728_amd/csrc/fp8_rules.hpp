@@ -39,25 +39,74 @@ inline Fp8Layout fp8_layout(int64_t K, int64_t N, int gated) {
 }
 
 // ------------------------------------------------------------------------------- products
-enum class Fp8Kernel { kRing };
-struct Fp8Plan {
-    Fp8Kernel kernel;
-    int bm, bn;      // tile
-    int64_t splits;  // of K
+// Which kernel takes a call, by estimated time: rounds of workgroups (256 CUs, `per_cu` of them on each), each a
+// fixed 1.5 us (first copies, epilogue) and its stages of 128 codes at `stage_us`; never less than W from HBM at 6.2 TB/s.
+// Stage times were fitted to calls of one round, us: 64 x 64 tiles 0.235 (two on a CU 0.36 the pair), 64 x 128 0.315,
+// 128 x 128 0.46, 256 x 128 0.80, 256 x 256 1.42.  Measured, us, best first:
+//   64 rows 4096 -> 12288    64 x 64 11.4, 64 x 128 12.9, streamed 14.9, 128 x 128 17
+//   128 rows 4096 -> 12288   64 x 128 13.2, 64 x 64 14.3, 128 x 128 16.9
+//   256 rows 4096 -> 12288   128 x 128 18.2, 64 x 128 24.3
+//   512 rows 4096 -> 12288   256 x 128 28.8, 128 x 128 35.5, 256 x 256 42.4
+//   1024 rows 4096 -> 12288  256 x 256 48.9, 256 x 128 56.6, 128 x 128 59.8
+//   2048 rows 14336 -> 4096  256 x 128 101, 128 x 128 124, 256 x 256 (128 tiles) 128
+// K is split where that fills the chip: 32 rows 14336 -> 4096 15.7 us with 4 splits of 64 x 128, 43 without;
+// the join costs a launch and the traffic of the fp32 sums.
+constexpr int kFp8Tiles = 5;
+struct Fp8Tile {
+    int bm, bn, per_cu;
+    double stage_us, pair_us;  // one workgroup on a CU, all of per_cu
 };
+constexpr Fp8Tile kFp8Tile[kFp8Tiles] = {{64, 64, 2, 0.235, 0.36},  {64, 128, 1, 0.315, 0.315}, {128, 128, 1, 0.46, 0.46},
+                                         {256, 128, 1, 0.80, 0.80}, {256, 256, 1, 1.42, 1.42}};
 constexpr int64_t kMaxSplits = 16;
 
-inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int64_t splits_that_fit) {
-    Fp8Plan p{Fp8Kernel::kRing, 64, 64, 1};
-    const int64_t tiles = (M + 63) / 64 * ((blocks + 3) / 4), stages = (K + 127) / 128;
-    p.splits = std::max<int64_t>(1, std::min({256 / tiles, stages / 8, kMaxSplits, splits_that_fit}));
-    return p;
-}
+// tile >= 0: that tile, K in `splits` parts.  tile < 0: the streamed kernel, rf row fragments x nc column blocks.
+struct Fp8Plan {
+    int tile, rf, nc;
+    int64_t splits;
+    double us;
+};
+
 // fp32 partial sums of one split
 inline size_t fp8_partial_bytes(int64_t M, int64_t blocks) { return (size_t)M * blocks * 64; }
-inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks) {
-    const Fp8Plan p = plan_fp8(M, K, blocks, kMaxSplits);
-    return p.splits > 1 ? p.splits * fp8_partial_bytes(M, blocks) : 0;
+
+// f32: codes widened to bf16, whose products take twice as long; the largest tile has no registers for it.
+inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32, int64_t splits_that_fit) {
+    const int64_t stages = (K + 127) / 128;
+    const double w_us = (double)blocks * 16 * (double)K / 6.2e6, slow = f32 ? 1.8 : 1.0;
+    Fp8Plan best{-1, 0, 0, 1, 0};
+    // Streamed: W straight into registers, up to 64 rows.  Per step of 128 codes 0.02 us and 0.072 us per column block
+    // with 16 rows to a workgroup, 0.07 and 0.067 with 32.  16 rows 4096 -> 4096 5.7 us, 64 x 64 tiles 10.7.
+    for (int rf = 1; rf <= 2 && M <= 64; ++rf) {
+        const int64_t rows = (M + 16 * rf - 1) / (16 * rf);
+        static constexpr int kNc[6] = {1, 2, 3, 4, 6, 8};
+        for (int nc : kNc) {
+            if ((gated && nc % 2) || (rf == 2 && nc > 4)) continue;
+            const int64_t wgs = rows * ((blocks + nc - 1) / nc);
+            const double step = rf == 1 ? 0.02 + 0.072 * nc : 0.07 + 0.067 * nc;
+            const double us = 2.7 + std::max(w_us, (double)((wgs + 255) / 256) * (double)stages * step * slow);
+            if (best.rf == 0 || us < best.us) best = Fp8Plan{-1, rf, nc, 1, us};
+        }
+    }
+    if (M <= 16) return best;
+    for (int i = 0; i < (f32 ? kFp8Tiles - 1 : kFp8Tiles); ++i) {
+        const Fp8Tile& t = kFp8Tile[i];
+        const int64_t tiles = (M + t.bm - 1) / t.bm * ((blocks * 16 + t.bn - 1) / t.bn);
+        for (int64_t splits = 1; splits <= std::min(kMaxSplits, splits_that_fit); splits *= 2) {
+            if (splits > 1 && (tiles * splits > 512 || stages / splits < 8)) break;
+            const int64_t wgs = tiles * splits, per_round = 256 * t.per_cu;
+            const double stage = (wgs <= 256 ? t.stage_us : t.pair_us) * slow;
+            const int64_t each = (stages + splits - 1) / splits;
+            double us = 3.0 + std::max(w_us, (double)((wgs + per_round - 1) / per_round) * (1.5 + (double)each * stage));
+            if (splits > 1) us += 2.5 + (double)splits * (double)fp8_partial_bytes(M, blocks) * 2.0 / 6e6;
+            if (best.us == 0 || us < best.us) best = Fp8Plan{i, 0, 0, splits, us};
+        }
+    }
+    return best;
+}
+inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
+    const int64_t splits = std::max(plan_fp8(M, K, blocks, gated, 0, kMaxSplits).splits, plan_fp8(M, K, blocks, gated, 1, kMaxSplits).splits);
+    return splits > 1 ? splits * fp8_partial_bytes(M, blocks) : 0;
 }
 
 // ------------------------------------------------------------------------------- log probabilities

@@ -11,6 +11,7 @@
 // 16 (l >> 4) .. of the first and of the second 64-byte half, which is what two packed chunks
 // (and two 16-byte pieces of a 128-byte stretch of an x row) give it.
 #include <type_traits>
+#include <utility>
 
 #include "dn_device.hpp"
 #include "dn_launch.hpp"
@@ -63,58 +64,111 @@ __device__ __forceinline__ f32x4 mfma_codes(const u32x4& a0, const u32x4& a1, co
 // z / (1 + e^-t)
 __device__ __forceinline__ float gate(float z, float t) { return z / (1.f + __builtin_amdgcn_exp2f(-t * kLog2eF)); }
 
-__device__ __forceinline__ float activation(float z, int act) {
-    switch (act) {
-        case 1: return z < 0.f ? 0.f : z;
-        case 2: return gate(z, z);
-        case 3: return 0.5f * z * (1.f + erff(z * 0.70710678118654752f));
-        // (1 + tanh a) / 2 = 1 / (1 + e^-2a), 2a = sqrt(8 / pi) (z + 0.044715 z^3)
-        case 4: return gate(z, z * __builtin_fmaf(0.0713548162726f * z, z, 1.5957691216057308f));
-        default: return z;
+// z Phi(z) by Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^-x^2, t = 1 / (1 + p x), x >= 0, off
+// by 1.5e-7 at most; the tail q = erfc(|z| / sqrt 2) / 2 is taken as it is, so nothing cancels at negative z.
+// About half of erff's instructions: the GELU of 8192 x 28672 outputs cost 216 us of 1740 with it.
+__device__ __forceinline__ float gelu(float z) {
+    const float x = __builtin_fabsf(z) * 0.70710678118654752f;
+    const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f, x, 1.f));
+    float q = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
+    q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
+    q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
+    q = __builtin_fmaf(q, t, 0.5f * 0.254829592f);
+    q *= t * __builtin_amdgcn_exp2f(-kLog2eF * x * x);
+    return z * (z < 0.f ? q : 1.f - q);
+}
+
+__device__ __forceinline__ void activate8(float* v, int act) {
+    switch (act) {  // uniform: outside the loops over values
+        case 0: break;
+        case 1:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = v[e] < 0.f ? 0.f : v[e];
+            break;
+        case 2:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gate(v[e], v[e]);
+            break;
+        case 3:
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gelu(v[e]);
+            break;
+        default:  // (1 + tanh a) / 2 = 1 / (1 + e^-2a), 2a = sqrt(8 / pi) (z + 0.044715 z^3)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = gate(v[e], v[e] * __builtin_fmaf(0.0713548162726f * v[e], v[e], 1.5957691216057308f));
+    }
+}
+
+// Scales and biases of 8 columns.
+struct Cols8 {
+    f32x4 s[2], b[2];
+    __device__ __forceinline__ void load(const float* ws, const float* bias) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            s[i] = *reinterpret_cast<const f32x4*>(ws + 4 * i);
+            b[i] = *reinterpret_cast<const f32x4*>(bias + 4 * i);
+        }
+    }
+    __device__ __forceinline__ float z(float sum, float sx, int e) const {
+        return __builtin_fmaf(sum * sx, s[e >> 2][e & 3], b[e >> 2][e & 3]);
+    }
+};
+
+// 8 values of the residual
+struct Residual8 {
+    u32x4 w[2];
+    __device__ __forceinline__ void load(const Fp8Args& p, int64_t at) {
+        if (p.out_f32) {
+            w[0] = ld16(reinterpret_cast<const float*>(p.residual) + at);
+            w[1] = ld16(reinterpret_cast<const float*>(p.residual) + at + 4);
+        } else {
+            w[0] = ld16(reinterpret_cast<const __bf16*>(p.residual) + at);
+        }
+    }
+    __device__ __forceinline__ void add(const Fp8Args& p, float* v) const {
+        const uint32_t a[8] = {w[0].x, w[0].y, w[0].z, w[0].w, w[1].x, w[1].y, w[1].z, w[1].w};
+        if (p.out_f32) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] += __uint_as_float(a[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                v[2 * e] += bf_lo(a[e]);
+                v[2 * e + 1] += bf_hi(a[e]);
+            }
+        }
+    }
+};
+__device__ __forceinline__ void store8(const Fp8Args& p, int64_t at, const float* v) {
+    if (p.out_f32) {
+        float* o = reinterpret_cast<float*>(p.out) + at;
+        *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
+        *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+    } else {
+        *reinterpret_cast<u32x4*>(reinterpret_cast<__bf16*>(p.out) + at) =
+            u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
     }
 }
 
 // 8 output columns n .. of one row from their sums g (packed columns c ..) and, gated, u (c + 16 ..).
 __device__ __forceinline__ void finish8(const Fp8Args& p, const float* g, const float* u, int64_t row, int64_t c, int64_t n) {
-    float v[8];
-    const float sx = p.xs[row];
-    const f32x4 s0 = *reinterpret_cast<const f32x4*>(p.ws + c), s1 = *reinterpret_cast<const f32x4*>(p.ws + c + 4);
-    const f32x4 b0 = *reinterpret_cast<const f32x4*>(p.bias + c), b1 = *reinterpret_cast<const f32x4*>(p.bias + c + 4);
-#pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = __builtin_fmaf(g[e] * sx, e < 4 ? s0[e & 3] : s1[e & 3], e < 4 ? b0[e & 3] : b1[e & 3]);
-    if (p.act)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = activation(v[e], p.act);
-    if (p.gated) {
-        const f32x4 t0 = *reinterpret_cast<const f32x4*>(p.ws + c + 16), t1 = *reinterpret_cast<const f32x4*>(p.ws + c + 20);
-        const f32x4 d0 = *reinterpret_cast<const f32x4*>(p.bias + c + 16), d1 = *reinterpret_cast<const f32x4*>(p.bias + c + 20);
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            v[e] *= __builtin_fmaf(u[e] * sx, e < 4 ? t0[e & 3] : t1[e & 3], e < 4 ? d0[e & 3] : d1[e & 3]);
-    }
     const int64_t at = row * p.N + n;
-    if (p.out_f32) {
-        float* o = reinterpret_cast<float*>(p.out) + at;
-        if (p.residual) {
-            const float* r = reinterpret_cast<const float*>(p.residual) + at;
+    const float sx = p.xs[row];
+    Cols8 k;
+    k.load(p.ws + c, p.bias + c);
+    Residual8 r;
+    if (p.residual) r.load(p, at);
+    float v[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] += r[e];
-        }
-        *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
-    } else {
-        __bf16* o = reinterpret_cast<__bf16*>(p.out) + at;
-        if (p.residual) {
-            const u32x4 r = ld16(reinterpret_cast<const __bf16*>(p.residual) + at);
+    for (int e = 0; e < 8; ++e) v[e] = k.z(g[e], sx, e);
+    activate8(v, p.act);
+    if (p.gated) {
+        k.load(p.ws + c + 16, p.bias + c + 16);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                v[2 * e] += bf_lo(r[e]);
-                v[2 * e + 1] += bf_hi(r[e]);
-            }
-        }
-        *reinterpret_cast<u32x4*>(o) =
-            u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        for (int e = 0; e < 8; ++e) v[e] *= k.z(u[e], sx, e);
     }
+    if (p.residual) r.add(p, v);
+    store8(p, at, v);
 }
 
 // Columns c .. c + 7 of `cols` packed columns from column c0 on: which output they are.  Gated: c walks the
@@ -135,34 +189,6 @@ __device__ __forceinline__ void lds_in_order() {
     __builtin_amdgcn_wave_barrier();
 }
 
-// A wave's ROWS x COLS sums lie in LDS, LDR floats to a row: eight columns to a lane at a time.
-template <int ROWS, int COLS, int LDR>
-__device__ __forceinline__ void finish_region(const Fp8Args& p, const float* sums, int64_t row0, int64_t c0, int lane, int split) {
-    const int per_row = p.part ? COLS / 8 : p.gated ? COLS / 16 : COLS / 8;
-    for (int i = lane; i < ROWS * per_row; i += kWave) {
-        const int r = i / per_row, c = i % per_row * 8;
-        const int64_t row = row0 + r;
-        if (row >= p.M) continue;
-        if (p.part) {
-            if (c0 + c >= p.blocks * 16) continue;
-            float* o = p.part + ((int64_t)split * p.M + row) * (p.blocks * 16) + c0 + c;
-            const f32x4* in = reinterpret_cast<const f32x4*>(sums + r * LDR + c);
-            *reinterpret_cast<f32x4*>(o) = in[0];
-            *reinterpret_cast<f32x4*>(o + 4) = in[1];
-            continue;
-        }
-        const Column k = column_of(c0, c, p.gated);
-        if (k.out >= p.N) continue;
-        const float* g = sums + r * LDR + (k.packed - c0);
-        float gv[8], uv[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) gv[e] = g[e];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) uv[e] = p.gated ? g[16 + e] : 0.f;
-        finish8(p, gv, uv, row, k.packed, k.out);
-    }
-}
-
 // Joins the splits' partial sums in order: one thread to 8 output columns of a row.
 __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args p) {
     const int64_t per_row = p.N / 8, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
@@ -181,101 +207,318 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args p) {
     finish8(p, g, u, row, k.packed, k.out);
 }
 
-// ------------------------------------------------------------------------------- ring kernel
-// BM x BN tiles (packed columns) of WM x WN waves.  A stage is 128 codes of K: x rows as whole
-// 128-byte lines, 8 rows to a copy, 16-byte pieces swizzled as in LayerNorm's large tiles; W as 1 KiB
-// chunks.  NST stages in LDS, copies NST - 1 ahead, one barrier to a stage.
-template <int BM, int BN, int WM, int WN, int NST, bool F32>
-__global__ __launch_bounds__(WM* WN* kWave) void fp8_ring_kernel(Fp8Args p) {
-    constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 16, FN = WTN / 16;
+// ------------------------------------------------------------------------------- few rows
+// 16 RF rows x 16 NC packed columns to a workgroup, whose KS waves take every KS-th step of 128 codes of K: W comes
+// straight from HBM into operand registers, 1 KiB to an instruction and read once; x, which every
+// workgroup reads, from L2.  No barrier until the waves' sums meet in LDS.  U steps' loads are issued together.
+template <int RF, int NC, int KS, int U, bool F32>
+__global__ __launch_bounds__(KS* kWave) void fp8_stream_kernel(Fp8Args p) {
+    constexpr int LDR = NC * 16 + 4;
+    __shared__ __attribute__((aligned(16))) float sums[KS * RF * 16 * LDR];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tiles_m = (int)((p.M + RF * 16 - 1) / (RF * 16));
+    const int t = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t m0 = (int64_t)(t % tiles_m) * RF * 16, nb0 = (int64_t)(t / tiles_m) * NC;
+    const int nst = (int)(p.kchunks / 2);
+
+    const char* xr[RF];
+    const int at = (lane >> 4) * 16;
+#pragma unroll
+    for (int r = 0; r < RF; ++r) xr[r] = p.x + min(m0 + r * 16 + (lane & 15), p.M - 1) * p.K;
+    const char* wc[NC];
+#pragma unroll
+    for (int c = 0; c < NC; ++c) wc[c] = p.w + packed_chunk(min(nb0 + c, p.blocks - 1), 0, p.kchunks, lane);
+
+    f32x4 acc[RF][NC];
+#pragma unroll
+    for (int r = 0; r < RF; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int s = wave; s < nst; s += KS * U) {
+        u32x4 a[U][RF][2], b[U][NC][2];
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u == 0 || s + u * KS < nst) {
+                const int64_t st = s + u * KS;
+#pragma unroll
+                for (int c = 0; c < NC; ++c)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) b[u][c][h] = ld16_stream(wc[c] + (st * 2 + h) * kChunkBytes);
+#pragma unroll
+                for (int r = 0; r < RF; ++r)
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)  // pieces past K: the row's last one, against weights that are zero there
+                        a[u][r][h] = ld16(xr[r] + min(st * 128 + h * 64 + at, p.K - 16));
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+            if (u == 0 || s + u * KS < nst) {
+#pragma unroll
+                for (int r = 0; r < RF; ++r)
+#pragma unroll
+                    for (int c = 0; c < NC; ++c)
+                        acc[r][c] = mfma_codes<F32>(a[u][r][0], a[u][r][1], b[u][c][0], b[u][c][1], acc[r][c]);
+            }
+    }
+    float* mine = sums + wave * RF * 16 * LDR;
+#pragma unroll
+    for (int r = 0; r < RF; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) mine[(r * 16 + 4 * (lane >> 4) + i) * LDR + c * 16 + (lane & 15)] = acc[r][c][i];
+    __syncthreads();
+    const int per_row = p.gated ? NC : NC * 2, rows = (int)min((int64_t)RF * 16, p.M - m0);
+    for (int i = threadIdx.x; i < rows * per_row; i += KS * kWave) {
+        const int r = i / per_row;
+        const Column k = column_of(nb0 * 16, i % per_row * 8, p.gated);
+        if (k.out >= p.N) continue;
+        const float* in = sums + r * LDR + (k.packed - nb0 * 16);
+        float g[8] = {}, v[8] = {};
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] += in[w * RF * 16 * LDR + e];
+            if (p.gated)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] += in[w * RF * 16 * LDR + 16 + e];
+        }
+        finish8(p, g, v, m0 + r, k.packed, k.out);
+    }
+}
+
+// f(0) .. f(N - 1) with constants: loops whose bodies the compiler would not unroll
+template <class F, int... I>
+__device__ __forceinline__ void unrolled_(F&& f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void unrolled(F&& f) {
+    unrolled_(f, std::make_integer_sequence<int, N>{});
+}
+
+// ------------------------------------------------------------------------------- large tiles
+// BM x BN tiles (packed columns), WM x WN waves, v_mfma_f32_32x32x64: a stage is 128 codes of K in two halves of 64.
+// NST stages in LDS; the products of one half run while the fragments of the next are read, and the copies of
+// stage s + NST are issued after the barrier in the middle of stage s, when every wave has read all of it.
+// Lane l holds row (or column) l & 31 and, of a half's 64 codes, pieces 2 (l >> 5) and the next; its
+// 16 sums are rows 8 (i / 4) + 4 (l >> 5) + i % 4 of column l & 31.
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct Piece2 {
+    u32x4 a, b;
+};
+// Of n things done by the first by/8 of m steps: how many are done before step i.
+constexpr int cut(int n, int by, int m, int i) { return n * i * 8 / (by * m) < n ? n * i * 8 / (by * m) : n; }
+// Reads are done by the middle of a half's products, copies by three quarters (measured, 8192 x 8192 -> 28672: 1352 us;
+// reads to the end 1387, both by the middle 1405).
+constexpr int kReadsBy = 4, kCopiesBy = 6;
+
+template <bool F32>
+__device__ __forceinline__ f32x16 mfma_32(const Piece2& x, const Piece2& w, f32x16 acc) {
+    if constexpr (!F32) {
+        const i32x8 a = {(int)x.a.x, (int)x.a.y, (int)x.a.z, (int)x.a.w, (int)x.b.x, (int)x.b.y, (int)x.b.z, (int)x.b.w};
+        const i32x8 b = {(int)w.a.x, (int)w.a.y, (int)w.a.z, (int)w.a.w, (int)w.b.x, (int)w.b.y, (int)w.b.z, (int)w.b.w};
+        return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, b, acc, 0, 0, 0, 0, 0, 0);
+    } else {
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(x.a.x, x.a.y), widen8(w.a.x, w.a.y), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(x.a.z, x.a.w), widen8(w.a.z, w.a.w), acc, 0, 0, 0);
+        acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(x.b.x, x.b.y), widen8(w.b.x, w.b.y), acc, 0, 0, 0);
+        return __builtin_amdgcn_mfma_f32_32x32x16_bf16(widen8(x.b.z, x.b.w), widen8(w.b.z, w.b.w), acc, 0, 0, 0);
+    }
+}
+
+template <int BM, int BN, int WM, int WN, int NST, bool GATED, bool F32>
+__global__ __launch_bounds__(WM* WN* kWave) void fp8_tile_kernel(Fp8Args p) {
+    constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 32, FN = WTN / 32;
     constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
-    constexpr int PER = (BM + BN) / 8 / NW;
-    constexpr int LDR = WTN + 4;
-    static_assert((BM + BN) / 8 % NW == 0, "every wave issues the same number of copies");
-    static_assert(NST * STAGE >= NW * WTM * LDR * 4, "the epilogue's sums fit the ring");
+    constexpr int A_INS = BM / 8 / NW, B_INS = BN / 8 / NW, PER = A_INS + B_INS;
+    constexpr int NMF = FM * FN, NRD = 2 * (FM + FN), LDR = 68;
+    static_assert(FN % 2 == 0, "the epilogue takes 32 x 64 sums at a time");
+    static_assert(NST * STAGE >= NW * 32 * LDR * 4, "the epilogue's sums fit the stages");
     __shared__ __attribute__((aligned(1024))) char smem[NST * STAGE];
+    __shared__ float row_s[BM], col_s[BN], col_b[BN];
 
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave / WN, wn = wave % WN;
+    // tiles: XCD-contiguous, then blocks of GM row blocks x all column tiles
     const int tiles_m = (int)((p.M + BM - 1) / BM), tiles_n = (int)((p.blocks * 16 + BN - 1) / BN);
-    const int t = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int pm = t % tiles_m, pn = t / tiles_m % tiles_n, split = t / (tiles_m * tiles_n);
+    const int tiles = tiles_m * tiles_n, tt = xcd_contiguous(blockIdx.x, gridDim.x), t = tt % tiles, split = tt / tiles;
+    constexpr int GM = 4;
+    const int span = GM * tiles_n, first = t / span * GM, gsz = min(tiles_m - first, GM);
+    const int pm = first + t % span % gsz, pn = t % span / gsz;
     const int64_t m0 = (int64_t)pm * BM, c0 = (int64_t)pn * BN, nb0 = c0 / 16;
     const int all = (int)(p.kchunks / 2), s0 = (int)((int64_t)all * split / p.splits),
-              s1 = (int)((int64_t)all * (split + 1) / p.splits);
+              nst = (int)((int64_t)all * (split + 1) / p.splits) - s0;  // stages of this split
+    for (int i = tid; i < BM; i += NW * kWave) row_s[i] = p.xs[min(m0 + i, p.M - 1)];
+    for (int i = tid; i < BN; i += NW * kWave) {
+        const int64_t c = min(c0 + i, p.blocks * 16 - 1);
+        col_s[i] = p.ws[c];
+        col_b[i] = p.bias[c];
+    }
 
+    uint32_t a_off[A_INS], b_off[B_INS];
+    uint32_t a_piece[A_INS];
+#pragma unroll
+    for (int j = 0; j < A_INS; ++j) {
+        const int r = (wave + j * NW) * 8 + (lane >> 3);
+        a_off[j] = (uint32_t)((min(m0 + r, p.M - 1) - m0) * p.K);
+        a_piece[j] = (uint32_t)(((lane & 7) ^ a_swz(r)) * 16);
+    }
+#pragma unroll
+    for (int j = 0; j < B_INS; ++j) {
+        const int c = wave + j * NW;
+        b_off[j] = (uint32_t)packed_chunk(min(nb0 + (c >> 1), p.blocks - 1) - nb0, c & 1, p.kchunks, lane);
+    }
     const uint64_t a_base = uniform_u64(p.x + m0 * p.K);
     const uint64_t b_base = uniform_u64(p.w + nb0 * p.kchunks * kChunkBytes);
     const uint32_t smem_addr = lds_addr32(smem), last = (uint32_t)(p.K - 16);
-    uint32_t off[PER], piece16[PER];
+    // copy k of stage s's PER (this wave's), into slot s % NST
+    auto issue = [&](int s, auto kc) {
+        constexpr int k = decltype(kc)::value;
+        const uint32_t base = smem_addr + (uint32_t)(s % NST * STAGE);
+        if constexpr (k < A_INS)  // pieces past K: the row's last one, against weights that are zero there
+            g2lds16_async_sb(a_base, a_off[k] + min((uint32_t)(s0 + s) * 128 + a_piece[k], last),
+                             base + (uint32_t)((wave + k * NW) * kChunkBytes));
+        else
+            g2lds16_async_sb(b_base + (uint64_t)(s0 + s) * (2 * kChunkBytes), b_off[k - A_INS],
+                             base + (uint32_t)(A_BYTES + (wave + (k - A_INS) * NW) * kChunkBytes));
+    };
+    const int g = lane >> 5;
+    // reads k of a half's NRD: the pieces of row fragments, then of column fragments
+    uint32_t a_at[FM][2];
 #pragma unroll
-    for (int j = 0; j < PER; ++j) {
-        const int c = wave + j * NW;
-        if (c < BM / 8) {
-            const int r = c * 8 + (lane >> 3);
-            off[j] = (uint32_t)((min(m0 + r, p.M - 1) - m0) * p.K);
-            piece16[j] = (uint32_t)(((lane & 7) ^ a_swz(r)) * 16);
-        } else {
-            const int b = c - BM / 8;
-            off[j] = (uint32_t)(packed_chunk(min(nb0 + (b >> 1), p.blocks - 1) - nb0, b & 1, p.kchunks, lane));
-            piece16[j] = 0;
-        }
+    for (int fm = 0; fm < FM; ++fm) {
+        const int r = wm * WTM + fm * 32 + (lane & 31);
+        a_at[fm][0] = (uint32_t)(r * 128 + (((2 * g) ^ a_swz(r)) << 4));
+        a_at[fm][1] = (uint32_t)(r * 128 + (((2 * g + 1) ^ a_swz(r)) << 4));
     }
-    auto issue = [&](int s) {
-        const uint32_t base = smem_addr + (uint32_t)((s - s0) % NST * STAGE);
-#pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            const int c = wave + j * NW;
-            if (c < BM / 8)  // pieces past K: the row's last one, against weights that are zero there
-                g2lds16_async_sb(a_base, off[j] + min((uint32_t)s * 128 + piece16[j], last), base + c * kChunkBytes);
-            else
-                g2lds16_async_sb(b_base + (uint64_t)s * (2 * kChunkBytes), off[j], base + c * kChunkBytes);
+    const uint32_t b_at = (uint32_t)(A_BYTES + (wn * WTN / 16 + ((lane >> 4) & 1)) * 2 * kChunkBytes + (lane & 15) * 16 + g * 512);
+    auto read = [&](int s, int h, auto kc, Piece2(&fa)[FM], Piece2(&fb)[FN]) {
+        constexpr int k = decltype(kc)::value;
+        char* base = smem + s % NST * STAGE;
+        u32x4 v;
+        if constexpr (k < 2 * FM) {
+            v = lds_ld16(lds_ptr(base + (a_at[k / 2][k & 1] ^ (h * 64))));
+            (k & 1 ? fa[k / 2].b : fa[k / 2].a) = v;
+        } else {
+            constexpr int f = (k - 2 * FM) / 2;
+            v = lds_ld16(lds_ptr(base + b_at + f * 4 * kChunkBytes + h * kChunkBytes + (k & 1) * 256));
+            (k & 1 ? fb[f].b : fb[f].a) = v;
         }
     };
-
-    f32x4 acc[FM][FN];
+    f32x16 acc[FM][FN];
 #pragma unroll
     for (int i = 0; i < FM; ++i)
 #pragma unroll
-        for (int j = 0; j < FN; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int j = 0; j < NST - 1 && s0 + j < s1; ++j) issue(s0 + j);
-    for (int s = s0; s < s1; ++s) {
-        if (s + NST - 2 < s1)
-            wait_vmcnt<(NST - 2) * PER>();  // this wave's copies of stage s
+        for (int j = 0; j < FN; ++j)
+#pragma unroll
+            for (int e = 0; e < 16; ++e) acc[i][j][e] = 0.f;
+    // The products of one half (fa, fb), and between them the reads of the next half (na, nb) from stage rs
+    // and, with COPY, the copies of stage cs.
+    auto compute = [&](Piece2(&fa)[FM], Piece2(&fb)[FN], int rs, int rh, Piece2(&na)[FM], Piece2(&nb)[FN], auto copies, int cs) {
+        constexpr bool COPY = decltype(copies)::value;
+        const bool copy = COPY && cs < nst;
+        unrolled<NMF>([&](auto ic) {
+            constexpr int i = decltype(ic)::value, fm = i / FN, fn = i % FN;
+            constexpr int r0 = cut(NRD, kReadsBy, NMF, i), r1 = cut(NRD, kReadsBy, NMF, i + 1), k0 = cut(PER, kCopiesBy, NMF, i), k1 = cut(PER, kCopiesBy, NMF, i + 1);
+            unrolled<r1 - r0>([&](auto k) { read(rs, rh, std::integral_constant<int, r0 + decltype(k)::value>{}, na, nb); });
+            if constexpr (COPY && k1 > k0) {
+                if (copy) unrolled<k1 - k0>([&](auto k) { issue(cs, std::integral_constant<int, k0 + decltype(k)::value>{}); });
+            }
+            acc[fm][fn] = mfma_32<F32>(fa[fm], fb[fn], acc[fm][fn]);
+            __builtin_amdgcn_sched_barrier(0);
+        });
+    };
+
+    for (int s = 0; s < NST && s < nst; ++s) unrolled<PER>([&](auto k) { issue(s, k); });
+    if (nst >= NST)
+        wait_vmcnt<(NST - 1) * PER>();  // stage 0
+    else
+        wait_vmcnt<0>();
+    block_barrier();
+    Piece2 fa0[FM], fb0[FN], fa1[FM], fb1[FN];
+    unrolled<NRD>([&](auto k) { read(0, 0, k, fa0, fb0); });
+    for (int s = 0; s < nst; ++s) {
+        compute(fa0, fb0, s, 1, fa1, fb1, std::false_type{}, 0);
+        // this wave's copies of stage s + 1 have landed (those of s + 2 .. s + NST - 1 may be on their way)
+        if (NST > 2 && s + NST - 1 < nst)
+            wait_vmcnt<(NST - 2) * PER>();
         else
             wait_vmcnt<0>();
-        block_barrier();  // every wave's, and every wave is done with the slot that is filled next
-        if (s + NST - 1 < s1) issue(s + NST - 1);
-        const char* base = smem + (s - s0) % NST * STAGE;
-        u32x4 fa[FM][2], fb[FN][2];
+        wait_lgkm0();  // this wave's reads of stage s are complete
+        block_barrier();
+        // past the end this reads stale data that is never used
+        compute(fa1, fb1, s + 1, 0, fa0, fb0, std::true_type{}, s + NST);
+    }
+    if (p.part) {
+        const int64_t ld = p.blocks * 16;
+        unrolled<FM * FN>([&](auto ic) {
+            constexpr int fm = decltype(ic)::value / FN, fn = decltype(ic)::value % FN;
+            const int64_t c = c0 + wn * WTN + fn * 32 + (lane & 31);
 #pragma unroll
-        for (int fm = 0; fm < FM; ++fm)
+            for (int i = 0; i < 16; ++i) {
+                const int64_t row = m0 + wm * WTM + fm * 32 + 8 * (i / 4) + 4 * g + i % 4;
+                if (row < p.M && c < ld) p.part[((int64_t)split * p.M + row) * ld + c] = acc[fm][fn][i];
+            }
+        });
+        wait_lgkm0();
+        return;
+    }
+    wait_lgkm0();
+    __syncthreads();
+    // 32 x 64 sums of a wave at a time through LDS: eight columns to a lane, whole 128-byte lines to a store.  Rows'
+    // and columns' scales come from LDS, so that no step waits for memory.
+    float* sums = reinterpret_cast<float*>(smem) + wave * 32 * LDR;
+    constexpr int IT = GATED ? 2 : 4, PER_ROW = 64 / 8 / (GATED ? 2 : 1);
+    const int col = GATED ? (lane % PER_ROW / 2) * 32 + (lane & 1) * 8 : lane % PER_ROW * 8;  // of the gate, packed
+    unrolled<FN / 2>([&](auto fpc) {
+        constexpr int fp = decltype(fpc)::value;
+        const int pc = wn * WTN + fp * 64;  // the region's first packed column in the tile
+        const int64_t n = GATED ? (c0 + pc) / 2 + lane % PER_ROW * 8 : c0 + pc + col;
+        Cols8 k, ku;
+        k.load(col_s + pc + col, col_b + pc + col);
+        if (GATED) ku.load(col_s + pc + col + 16, col_b + pc + col + 16);
+        unrolled<FM>([&](auto fmc) {
+            constexpr int fm = decltype(fmc)::value;
+            const int r0 = wm * WTM + fm * 32 + lane / PER_ROW;
+            Residual8 res[IT];
+            if (p.residual) {
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const int r = wm * WTM + fm * 16 + (lane & 15);
-                fa[fm][h] = lds_ld16(lds_ptr((char*)base + r * 128 + (((h * 4 + (lane >> 4)) ^ a_swz(r)) << 4)));
+                for (int it = 0; it < IT; ++it) {
+                    const int64_t row = m0 + r0 + it * (64 / PER_ROW);
+                    if (row < p.M && n < p.N) res[it].load(p, row * p.N + n);
+                }
             }
 #pragma unroll
-        for (int fn = 0; fn < FN; ++fn)
+            for (int f = 0; f < 2; ++f)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-                fb[fn][h] = lds_ld16(lds_ptr((char*)base + A_BYTES + ((wn * FN + fn) * 2 + h) * kChunkBytes + lane * 16));
+                for (int i = 0; i < 16; ++i)
+                    sums[(8 * (i / 4) + 4 * g + i % 4) * LDR + f * 32 + (lane & 31)] = acc[fm][fp * 2 + f][i];
+            lds_in_order();
 #pragma unroll
-        for (int fm = 0; fm < FM; ++fm)
+            for (int it = 0; it < IT; ++it) {
+                const int r = it * (64 / PER_ROW);
+                const int64_t row = m0 + r0 + r;
+                const float* at = sums + (lane / PER_ROW + r) * LDR + col;
+                const f32x4 a0 = *reinterpret_cast<const f32x4*>(at), a1 = *reinterpret_cast<const f32x4*>(at + 4);
+                const float sx = row_s[r0 + r];
+                float v[8];
 #pragma unroll
-            for (int fn = 0; fn < FN; ++fn) acc[fm][fn] = mfma_codes<F32>(fa[fm][0], fa[fm][1], fb[fn][0], fb[fn][1], acc[fm][fn]);
-    }
-    __syncthreads();
-    float* sums = reinterpret_cast<float*>(smem) + wave * WTM * LDR;
+                for (int e = 0; e < 8; ++e) v[e] = k.z(e < 4 ? a0[e & 3] : a1[e & 3], sx, e);
+                activate8(v, p.act);
+                if (GATED) {
+                    const f32x4 u0 = *reinterpret_cast<const f32x4*>(at + 16), u1 = *reinterpret_cast<const f32x4*>(at + 20);
 #pragma unroll
-    for (int fm = 0; fm < FM; ++fm)
-#pragma unroll
-        for (int fn = 0; fn < FN; ++fn)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) sums[(fm * 16 + 4 * (lane >> 4) + i) * LDR + fn * 16 + (lane & 15)] = acc[fm][fn][i];
-    lds_in_order();
-    finish_region<WTM, WTN, LDR>(p, sums, m0 + wm * WTM, c0 + wn * WTN, lane, split);
+                    for (int e = 0; e < 8; ++e) v[e] *= ku.z(e < 4 ? u0[e & 3] : u1[e & 3], sx, e);
+                }
+                if (p.residual) res[it].add(p, v);
+                if (row < p.M && n < p.N) store8(p, row * p.N + n, v);
+            }
+            lds_in_order();
+        });
+    });
 }
 
 // ------------------------------------------------------------------------------- weights
@@ -384,22 +627,67 @@ hipError_t launch_linear_fp8_prepare(const void* W, const float* scales, const v
     return hipSuccess;
 }
 
+template <bool GATED, bool F32>
+static void launch_tile_(const Fp8Args& p, int tile, dim3 grid, hipStream_t s) {
+    switch (tile) {
+        case 0: fp8_tile_kernel<64, 64, 2, 1, 4, GATED, F32><<<grid, 128, 0, s>>>(p); break;
+        case 1: fp8_tile_kernel<64, 128, 2, 2, 4, GATED, F32><<<grid, 256, 0, s>>>(p); break;
+        case 2: fp8_tile_kernel<128, 128, 2, 2, 4, GATED, F32><<<grid, 256, 0, s>>>(p); break;
+        case 3: fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32><<<grid, 512, 0, s>>>(p); break;
+        default:
+            if constexpr (!F32) fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32><<<grid, 512, 0, s>>>(p);
+    }
+}
+static void launch_tile(const Fp8Args& p, int tile, dim3 grid, hipStream_t s) {
+    if (p.gated)
+        p.out_f32 ? launch_tile_<true, true>(p, tile, grid, s) : launch_tile_<true, false>(p, tile, grid, s);
+    else
+        p.out_f32 ? launch_tile_<false, true>(p, tile, grid, s) : launch_tile_<false, false>(p, tile, grid, s);
+}
+
+template <int RF, int NC>
+static void launch_stream_(const Fp8Args& p, dim3 grid, hipStream_t s) {
+    // 2 steps' loads at a time while the registers hold them
+    constexpr int U = RF + NC <= 3 ? 2 : 1;
+    if (p.out_f32)
+        fp8_stream_kernel<RF, NC, 8, U, true><<<grid, 512, 0, s>>>(p);
+    else
+        fp8_stream_kernel<RF, NC, 8, U, false><<<grid, 512, 0, s>>>(p);
+}
+static void launch_stream(const Fp8Args& p, int rf, int nc, dim3 grid, hipStream_t s) {
+    switch (rf * 16 + nc) {
+        case 17: launch_stream_<1, 1>(p, grid, s); break;
+        case 18: launch_stream_<1, 2>(p, grid, s); break;
+        case 19: launch_stream_<1, 3>(p, grid, s); break;
+        case 20: launch_stream_<1, 4>(p, grid, s); break;
+        case 22: launch_stream_<1, 6>(p, grid, s); break;
+        case 24: launch_stream_<1, 8>(p, grid, s); break;
+        case 33: launch_stream_<2, 1>(p, grid, s); break;
+        case 34: launch_stream_<2, 2>(p, grid, s); break;
+        case 35: launch_stream_<2, 3>(p, grid, s); break;
+        default: launch_stream_<2, 4>(p, grid, s);
+    }
+}
+
 hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed, int64_t M, int64_t K, int64_t N, int gated,
                              int act, const void* residual, int out_dtype, void* workspace, int64_t splits_that_fit,
                              void* out, hipStream_t s) {
     const Fp8Layout l = fp8_layout(K, N, gated);
     const char* base = reinterpret_cast<const char*>(packed);
-    const Fp8Plan plan = plan_fp8(M, K, l.blocks, splits_that_fit);
-    Fp8Args p{reinterpret_cast<const char*>(x), xs, base, reinterpret_cast<const float*>(base + l.scales),
-              reinterpret_cast<const float*>(base + l.bias), residual, out,
-              plan.splits > 1 ? reinterpret_cast<float*>(workspace) : nullptr, M, K, N, l.kchunks, l.blocks, act, gated,
-              out_dtype == 0, (int)plan.splits};
-    const int64_t tiles = (M + plan.bm - 1) / plan.bm * ((l.blocks * 16 + plan.bn - 1) / plan.bn);
-    const dim3 grid((unsigned)(tiles * plan.splits));
-    if (p.out_f32)
-        fp8_ring_kernel<64, 64, 2, 2, 4, true><<<grid, 256, 0, s>>>(p);
-    else
-        fp8_ring_kernel<64, 64, 2, 2, 4, false><<<grid, 256, 0, s>>>(p);
+    const int f32 = out_dtype == 0;
+    const Fp8Plan plan = plan_fp8(M, K, l.blocks, gated, f32, splits_that_fit);
+    const Fp8Args p{reinterpret_cast<const char*>(x), xs, base, reinterpret_cast<const float*>(base + l.scales),
+                    reinterpret_cast<const float*>(base + l.bias), residual, out,
+                    plan.splits > 1 ? reinterpret_cast<float*>(workspace) : nullptr, M, K, N, l.kchunks, l.blocks, act, gated,
+                    f32, (int)plan.splits};
+    if (plan.tile >= 0) {
+        const Fp8Tile& t = kFp8Tile[plan.tile];
+        const int64_t tiles = (M + t.bm - 1) / t.bm * ((l.blocks * 16 + t.bn - 1) / t.bn);
+        launch_tile(p, plan.tile, dim3((unsigned)(tiles * plan.splits)), s);
+    } else {
+        const int64_t rows = (M + plan.rf * 16 - 1) / (plan.rf * 16);
+        launch_stream(p, plan.rf, plan.nc, dim3((unsigned)(rows * ((l.blocks + plan.nc - 1) / plan.nc))), s);
+    }
     if (plan.splits > 1) fp8_join_kernel<<<dim3((unsigned)((M * (N / 8) + 255) / 256)), 256, 0, s>>>(p);
     return hipGetLastError();
 }
