@@ -772,7 +772,7 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
 // ------------------------------------------------------------------------------- log probabilities
 static bool logprob_sizes(int64_t T, int64_t V, int64_t top) {
     size_t b;
-    return T >= 1 && V >= 1 && V < (int64_t(1) << 31) && top >= 0 && top <= std::min(V, dn::kMaxTop) &&
+    return T >= 1 && V >= 1 && V < (int64_t(1) << 30) && top >= 0 && top <= std::min(V, dn::kMaxTop) &&
            bytes_of(T, V, 8, &b) && bytes_of(T, dn::kMaxSegments, 16 + 8 * dn::kMaxTop, &b);
 }
 
@@ -793,7 +793,7 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
     if (!bytes_of(T, stride, (int64_t)esize(dtype), &lb) || !bytes_of(T, std::max<int64_t>(n, 1), 4, &nb))
         return DN_ERR_INVALID_ARG;
     lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
-    const int64_t segments = dn::logprob_segments(T, V);
+    const int64_t segments = dn::plan_logprobs(T, V).segments;
     if (T * segments > kMaxGridX) return DN_ERR_UNSUPPORTED;
     if (!aligned(logits, esize(dtype)) || !aligned(targets, 16) || !aligned(logprobs, 16) || !aligned(entropy, 16) ||
         !aligned(top_logprobs, 16) || !aligned(top_ids, 16) || !aligned(workspace, 256))
@@ -806,7 +806,7 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
     for (int i = 0; i < 5; ++i)
         if (any_overlap(outs[i], in, 2) || any_overlap(outs[i], outs + i + 1, 4 - i)) return DN_ERR_INVALID_ARG;
     return from_hip(dn::launch_token_logprobs(logits, stride, T, V, dtype, scale, targets, n, top, logprobs, entropy,
-                                              top_logprobs, top_ids, workspace, segments, stream));
+                                              top_logprobs, top_ids, workspace, stream));
 }
 
 }  // extern "C"

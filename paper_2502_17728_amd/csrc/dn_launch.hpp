@@ -168,10 +168,10 @@ hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed,
                              int act, const void* residual, int out_dtype, void* workspace, int64_t splits_that_fit,
                              void* out, hipStream_t s);
 
-// Log probabilities, entropy and ranks of T rows; segments > 1 go through the workspace.
+// Log probabilities, entropy and ranks of T rows.
 hipError_t launch_token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
                                  const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
-                                 float* top_logprobs, int32_t* top_ids, void* workspace, int64_t segments, hipStream_t s);
+                                 float* top_logprobs, int32_t* top_ids, void* workspace, hipStream_t s);
 
 // Largest K (elements per row) the row-wise unfused kernels keep in registers.
 constexpr int64_t kMaxRowElemsBf16 = 16384;

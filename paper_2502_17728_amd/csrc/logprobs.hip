@@ -7,9 +7,13 @@
 // asked for alone, after the pass.  Each lane keeps its own (m, l, s); on a larger m' they become
 // f l and f (s + d' l) with d' = scale (m - m'), f = e^d'.  Exponents are to base 2 inside.
 //
-// The likeliest tokens are a sorted list per wave, one entry to a lane, as 64-bit keys: the logit's
-// bits in an order that integers share, then the complement of the token's id, so that the larger
-// key is the likelier token and, among equals, the lower id.
+// The likeliest tokens are 64-bit keys: the logit's bits in an order that integers share, then the
+// complement of the token's id, so that the larger key is the likelier token and, among equals, the
+// lower id.  A wave puts the groups of 8 tokens whose largest may belong to the likeliest aside, in
+// LDS; every few dozen groups their tokens are filtered, and a search by bits over the keys (one
+// ballot a bit) finds a bound that `top` of them reach and drops the rest.  The first bound comes so from the
+// lanes' maxima of the first 512 tokens; a row of random order is searched about five times.  The waves'
+// keys are then cut together, and only what is left, about `top` keys, is put in order.
 //
 // Bound by HBM for long inputs (one read of the logits), by launches and the serial ranking for short.
 #include "dn_device.hpp"
@@ -21,7 +25,8 @@ namespace dn {
 constexpr float kLowest = -3.402823466e38f;
 constexpr float kLeastExponent = -200.f;  // 2^-200 is 0 in fp32; keeps 0 * -inf out of the sums
 constexpr float kLn2 = 0.6931471805599453f;
-constexpr int kLpThreads = 256, kLpWaves = kLpThreads / kWave;
+constexpr int kBuffer = 128;                 // keys of a wave's list: `top` (at most 64) and 64 more always fit
+constexpr int kFlush = 32, kGroups = kFlush + 64;  // groups put aside: looked at past kFlush, and 64 more fit
 
 struct LpArgs {
     const void* logits;
@@ -55,18 +60,46 @@ __device__ __forceinline__ void join(Sums& a, Sums b, float c) {
     a.l += b.l;
     a.s += b.s;
 }
+// Reductions over the wave's 64 lanes without LDS: pairs, quads, halves of a row of 16, then rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp(uint32_t v) {
+    return (uint32_t)__builtin_amdgcn_update_dpp((int)v, (int)v, CTRL, 0xf, 0xf, false);
+}
+template <class F>
+__device__ __forceinline__ uint32_t wave_reduce(uint32_t v, F f) {
+    v = f(v, dpp<0xB1>(v));   // lane ^ 1
+    v = f(v, dpp<0x4E>(v));   // lane ^ 2
+    v = f(v, dpp<0x141>(v));  // the row's halves mirrored
+    v = f(v, dpp<0x140>(v));  // the row mirrored
+    const auto p = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = f(p[0], p[1]);
+    const auto q = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return f(q[0], q[1]);
+}
+__device__ __forceinline__ uint32_t wave_max(uint32_t v) {
+    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a > b ? a : b; });
+}
+__device__ __forceinline__ float wave_maxf(float v) {
+    return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__builtin_fmaxf(__uint_as_float(a), __uint_as_float(b)));
+    }));
+}
+__device__ __forceinline__ float wave_addf(float v) {
+    return __uint_as_float(wave_reduce(__float_as_uint(v), [](uint32_t a, uint32_t b) {
+        return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+    }));
+}
 __device__ __forceinline__ Sums wave_join(Sums a, float c) {
-#pragma unroll
-    for (int o = 32; o >= 1; o >>= 1)
-        join(a, Sums{__shfl_xor(a.m, o), __shfl_xor(a.l, o), __shfl_xor(a.s, o)}, c);
+    raise(a, wave_maxf(a.m), c);
+    a.l = wave_addf(a.l);
+    a.s = wave_addf(a.s);
     return a;
 }
 
 // ------------------------------------------------------------------------------- ranks
-__device__ __forceinline__ unsigned long long key_of(float x, uint32_t id) {
+__device__ __forceinline__ uint32_t order_of(float x) {
     const uint32_t u = __float_as_uint(x + 0.f);  // -0 ranks as +0
-    const uint32_t o = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
-    return ((unsigned long long)o << 32) | (uint32_t)~id;
+    return u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
 }
 __device__ __forceinline__ float value_of(unsigned long long key) {
     const uint32_t o = (uint32_t)(key >> 32);
@@ -74,70 +107,228 @@ __device__ __forceinline__ float value_of(unsigned long long key) {
 }
 __device__ __forceinline__ uint32_t id_of(unsigned long long key) { return ~(uint32_t)key; }
 
-__device__ __forceinline__ unsigned long long lane_key(unsigned long long k, int lane) {
-    return ((unsigned long long)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), lane) << 32) |
-           (uint32_t)__builtin_amdgcn_readlane((int)k, lane);
+__device__ __forceinline__ void lds_in_order() { asm volatile("" ::: "memory"); }  // a wave's LDS instructions are served in order
+
+__device__ __forceinline__ int lanes_below(unsigned long long mask) {
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0));
 }
 
-// A wave's ranked list: lane i holds the i-th largest key so far, 0 where there is none yet.
-struct Ranked {
-    unsigned long long key;
-    float last;        // the value and id that a token has to beat
-    uint32_t last_id;
-    __device__ __forceinline__ void clear() {
-        key = 0;
-        last = -__builtin_inff();
-        last_id = 0xffffffffu;
-    }
-    __device__ __forceinline__ bool beats(float x, uint32_t id) const { return x > last || (x == last && id < last_id); }
-    __device__ __forceinline__ void insert(unsigned long long k, int lane, int top) {
-        const int pos = __popcll(__ballot(key > k));
-        const unsigned long long up = __shfl_up(key, 1);
-        key = lane < pos ? key : lane == pos ? k : up;
-        const unsigned long long e = lane_key(key, top - 1);
-        if (e != 0) {
-            last = value_of(e);
-            last_id = id_of(e);
+__device__ __forceinline__ uint32_t wave_min(uint32_t v) {
+    return wave_reduce(v, [](uint32_t a, uint32_t b) { return a < b ? a : b; });
+}
+
+// A t of which count(t) >= top, where count(lo) >= top and no value is above hi: the largest whose bits below `least` are
+// zero, or a smaller one with count(t) <= enough.
+template <class F>
+__device__ __forceinline__ uint32_t search(uint32_t lo, uint32_t hi, int least, int top, int enough, F count) {
+    if (lo >= hi) return lo;
+    int bit = 31 - __builtin_clz(lo ^ hi);
+    uint32_t t = lo & ~((2u << bit) - 1);  // what lo and hi share
+    for (; bit >= least; --bit) {
+        const uint32_t next = t | (1u << bit);
+        const int n = count(next);
+        if (n >= top) {
+            t = next;
+            if (n <= enough) break;
         }
+    }
+    return t > lo ? t : lo;
+}
+
+// A wave's part of LDS
+struct WaveRanks {
+    unsigned long long keys[kBuffer];
+    float values[kGroups * 8];
+    uint32_t first[kGroups];
+};
+
+// A wave's likeliest tokens so far: n keys, none below `floor`, and groups of 8 tokens that have not been looked at.
+// A further token counts if the order of its logit is `bar` or more.
+struct Ranked {
+    DN_LDS WaveRanks* m;
+    int n, groups, top;
+    uint32_t floor, bar;
+
+    // From the lanes' maxima of the first tokens (order 0 where a lane has none): at least `top` tokens are not below
+    // what `top` of these reach, and the rest need not be kept.
+    __device__ __forceinline__ void start(float most, bool there) {
+        const uint32_t o = there && most == most ? order_of(most) : 0;
+        bar = floor = search(wave_min(o), wave_max(o), 16, top, top + 1, [&](uint32_t t) { return __popcll(__ballot(o >= t)); });
+    }
+
+    // Sorts the keys and cuts them to `top`, by counting the larger ones.
+    __device__ __forceinline__ void rank(int lane) {
+        lds_in_order();
+        DN_LDS unsigned long long* k = m->keys;
+        const unsigned long long a = lane < n ? k[lane] : 0, b = 64 + lane < n ? k[64 + lane] : 0;
+        if (lane >= n && lane < n + 8) k[lane] = 0;  // whole groups of 8 below
+        if (64 + lane >= n && 64 + lane < n + 8) k[64 + lane] = 0;
+        lds_in_order();
+        typedef unsigned long long u64x2 __attribute__((ext_vector_type(2)));
+        int ra = 0, rb = 0;
+        for (int i = 0; i < n; i += 8) {
+            u64x2 o[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) o[j] = *reinterpret_cast<DN_LDS u64x2*>(k + i + 2 * j);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) ra += o[j / 2][j & 1] > a;
+            if (n > 64) {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) rb += o[j / 2][j & 1] > b;
+            }
+        }
+        lds_in_order();
+        if (lane < n && ra < top) k[ra] = a;
+        if (64 + lane < n && rb < top) k[rb] = b;
+        lds_in_order();
+        if (n >= top) {
+            n = top;
+            bar = floor = (uint32_t)__builtin_amdgcn_readfirstlane((int)(k[top - 1] >> 32));
+        }
+    }
+
+    // Drops keys that `top` others are above; what is left is at most 64.
+    __device__ __forceinline__ void cut(int lane) {
+        lds_in_order();
+        const unsigned long long a = lane < n ? m->keys[lane] : 0, b = 64 + lane < n ? m->keys[64 + lane] : 0;
+        const uint32_t ha = (uint32_t)(a >> 32), hb = (uint32_t)(b >> 32);
+        floor = search(floor, wave_max(ha > hb ? ha : hb), 8, top, top + 8,
+                       [&](uint32_t t) { return __popcll(__ballot(ha >= t)) + __popcll(__ballot(hb >= t)); });
+        const bool ka = a != 0 && ha >= floor, kb = b != 0 && hb >= floor;
+        const unsigned long long ma = __ballot(ka), mb = __ballot(kb);
+        if (ka) m->keys[lanes_below(ma)] = a;
+        if (kb) m->keys[__popcll(ma) + lanes_below(mb)] = b;
+        n = __popcll(ma) + __popcll(mb);
+        lds_in_order();
+        bar = floor;
+        if (n > 64) rank(lane);  // many equals
+    }
+
+    // The tokens of the groups put aside.  Later groups hold higher ids: of those, a logit that only equals the last
+    // of `top` keys does not count.
+    __device__ __forceinline__ void flush(int V, int lane) {
+        lds_in_order();
+        for (int i = 0; i < groups * 8; i += kWave) {
+            const int at = i + lane, g = at >> 3;
+            const bool there = at < groups * 8;
+            const float x = there ? m->values[at] : 0.f;
+            const uint32_t id = there ? m->first[g] + (at & 7) : 0, o = order_of(x);
+            bool keep = there && x == x && (int)id >= 0 && (int)id < V && o >= bar;
+            unsigned long long mask = __ballot(keep);
+            if (n + __popcll(mask) > kBuffer) {
+                rank(lane);
+                keep = keep && o >= bar;
+                mask = __ballot(keep);
+            }
+            if (keep) m->keys[n + lanes_below(mask)] = ((unsigned long long)o << 32) | (uint32_t)~id;
+            n += __popcll(mask);
+        }
+        groups = 0;
+        if (n >= top) {
+            cut(lane);
+            if (floor != 0xffffffffu) bar = floor + 1;
+        }
+    }
+
+    // f[0 .. 7] are tokens at, at + 1, .., `most` the largest of them; `there`: the lane has some.
+    __device__ __forceinline__ void add(const float* f, float most, bool there, int at, int V, int lane) {
+        const bool keep = there && order_of(most) >= bar;
+        const unsigned long long mask = __ballot(keep);
+        if (!mask) return;
+        if (keep) {
+            const int g = groups + lanes_below(mask);
+            *reinterpret_cast<DN_LDS f32x4*>(&m->values[g * 8]) = f32x4{f[0], f[1], f[2], f[3]};
+            *reinterpret_cast<DN_LDS f32x4*>(&m->values[g * 8 + 4]) = f32x4{f[4], f[5], f[6], f[7]};
+            m->first[g] = (uint32_t)at;
+        }
+        groups += __popcll(mask);
+        if (groups > kFlush) flush(V, lane);
     }
 };
 
-// Joins `lists` (at most 64) sorted lists of `top` keys: lane i of the calling wave gets the i-th key.
-__device__ __forceinline__ unsigned long long join_lists(const unsigned long long* keys, int lists, int top, int lane) {
-    int at = 0;
-    unsigned long long head = lane < lists ? keys[(int64_t)lane * top] : 0, mine = 0;
-    for (int r = 0; r < top; ++r) {
-        unsigned long long best = head;
+// The `top` largest of `total` keys (at most 64 CHUNKS; zeros are none) in order, by one wave: lane i gets the i-th,
+// 0 where there are fewer.  At least `top` keys have order `lo` or more, if that is not 1.  `m` is scratch.
+template <int CHUNKS>
+__device__ __forceinline__ unsigned long long top_of_(const DN_LDS unsigned long long* keys, int total, int top, uint32_t lo_bound,
+                                                      DN_LDS WaveRanks* m, int lane) {
+    uint32_t hi[CHUNKS], lo[CHUNKS], most = 0;
 #pragma unroll
-        for (int o = 32; o >= 1; o >>= 1) {
-            const unsigned long long other = __shfl_xor(best, o);
-            best = other > best ? other : best;
-        }
-        if (lane == r) mine = best;
-        if (best == 0) break;
-        if (head == best) {
-            ++at;
-            head = at < top ? keys[(int64_t)lane * top + at] : 0;
-        }
+    for (int c = 0; c < CHUNKS; ++c) {
+        const unsigned long long k = c * 64 + lane < total ? keys[c * 64 + lane] : 0;
+        hi[c] = (uint32_t)(k >> 32);
+        lo[c] = (uint32_t)k;
+        most = hi[c] > most ? hi[c] : most;
     }
-    return mine;
+    auto count = [&](uint32_t t) {
+        int n = 0;
+#pragma unroll
+        for (int c = 0; c < CHUNKS; ++c) n += __popcll(__ballot(hi[c] >= t));
+        return n;
+    };
+    uint32_t t = lo_bound;
+    const int all = count(t);
+    int left = all;
+    if (all > 64) {  // then at least `top` (at most 64)
+        t = search(t, wave_max(most), 0, top, 64, count);
+        left = count(t);
+    }
+    uint32_t last = 0;  // of the keys with order t, those whose lower half is `last` or more
+    if (left > kBuffer) {
+        const int above = t == 0xffffffffu ? 0 : count(t + 1);
+        last = search(0, 0xffffffffu, 0, top - above, top - above, [&](uint32_t l) {
+            int n = 0;
+#pragma unroll
+            for (int c = 0; c < CHUNKS; ++c) n += __popcll(__ballot(hi[c] == t && lo[c] >= l));
+            return n;
+        });
+    }
+    Ranked r{m, 0, 0, top, 0, 0};
+    lds_in_order();
+#pragma unroll
+    for (int c = 0; c < CHUNKS; ++c) {
+        const bool keep = hi[c] > t || (hi[c] == t && lo[c] >= last);
+        const unsigned long long mask = __ballot(keep);
+        if (keep) m->keys[r.n + lanes_below(mask)] = ((unsigned long long)hi[c] << 32) | lo[c];
+        r.n += __popcll(mask);
+    }
+    r.rank(lane);
+    return lane < r.n ? m->keys[lane] : 0;
+}
+__device__ __forceinline__ unsigned long long top_of(const DN_LDS unsigned long long* keys, int total, int top, uint32_t lo,
+                                                     DN_LDS WaveRanks* m, int lane) {
+    if (total <= 128) return top_of_<2>(keys, total, top, lo, m, lane);
+    if (total <= 256) return top_of_<4>(keys, total, top, lo, m, lane);
+    if (total <= 512) return top_of_<8>(keys, total, top, lo, m, lane);
+    return top_of_<16>(keys, total, top, lo, m, lane);
 }
 
 // ------------------------------------------------------------------------------- results
+// A lane's first given token and its logit, read before the pass over the row.
+struct Given {
+    int32_t t;
+    float x;
+    template <class T>
+    __device__ __forceinline__ void load(const LpArgs& p, int64_t row, const T* logits, int64_t i) {
+        t = i < p.n ? p.targets[row * p.n + i] : -1;
+        x = t >= 0 && t < p.V ? to_f32<T>(logits[t]) : 0.f;
+    }
+    __device__ __forceinline__ float logprob(const LpArgs& p, const Sums& a, float log_l) const {
+        return t < 0 ? 0.f : t < p.V ? (x - a.m) * p.scale - log_l : __builtin_nanf("");
+    }
+};
+
 template <class T>
 __device__ __forceinline__ void finish(const LpArgs& p, int64_t row, const T* x, const Sums& a, unsigned long long key,
-                                       int thread, int threads) {
+                                       Given given, int lane) {
     const float log_l = kLn2 * __builtin_amdgcn_logf(a.l);
-    for (int64_t i = thread; i < p.n; i += threads) {
-        const int32_t t = p.targets[row * p.n + i];
-        float v = 0.f;
-        if (t >= 0) v = t < p.V ? (to_f32<T>(x[t]) - a.m) * p.scale - log_l : __builtin_nanf("");
-        p.logprobs[row * p.n + i] = v;
+    for (int64_t i = lane; i < p.n; i += kWave) {
+        if (i >= kWave) given.load(p, row, x, i);
+        p.logprobs[row * p.n + i] = given.logprob(p, a, log_l);
     }
-    if (p.entropy && thread == 0) p.entropy[row] = log_l - kLn2 * (a.s / a.l);
-    if (thread < p.top) {
-        p.top_logprobs[row * p.top + thread] = key ? (value_of(key) - a.m) * p.scale - log_l : __builtin_nanf("");
-        p.top_ids[row * p.top + thread] = key ? (int32_t)id_of(key) : -1;
+    if (p.entropy && lane == 0) p.entropy[row] = log_l - kLn2 * (a.s / a.l);
+    if (lane < p.top) {
+        p.top_logprobs[row * p.top + lane] = key ? (value_of(key) - a.m) * p.scale - log_l : __builtin_nanf("");
+        p.top_ids[row * p.top + lane] = key ? (int32_t)id_of(key) : -1;
     }
 }
 
@@ -173,27 +364,37 @@ __device__ __forceinline__ void load8<float>(const float* x, int64_t at, int64_t
     }
 }
 
-template <class T, bool TOP>
-__global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs p) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int64_t row = blockIdx.x / p.segments;
-    const int seg = (int)(blockIdx.x % p.segments);
+// A workgroup of NT threads takes a row, or one of its segments; loads run one step of 8 NT tokens ahead.
+template <class T, bool TOP, int NT>
+__global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
+    constexpr int NW = NT / kWave;
+    __shared__ float sums[NW][3];
+    __shared__ int counts[NW];
+    __shared__ uint32_t floors[NW];
+    __shared__ unsigned long long pool[TOP ? NW * 64 : 1];
+    __shared__ __attribute__((aligned(16))) WaveRanks ranks[TOP ? NW : 1];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int64_t row = blockIdx.x / (unsigned)p.segments;
+    const int seg = (int)(blockIdx.x % (unsigned)p.segments);
     const T* x = reinterpret_cast<const T*>(p.logits) + row * p.stride;
-    const int64_t V = p.V;
+    const int V = (int)p.V;
     const float c = p.scale * kLog2eF;
     // the row in pieces of 8 values that start at aligned addresses: the first piece may begin before it
     const int shift = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
-    const int64_t pieces = (V + shift + 7) / 8, per = (pieces + p.segments - 1) / p.segments;
-    const int64_t end = min(pieces, (seg + 1) * per);
+    const int pieces = (int)((p.V + shift + 7) / 8), per = (pieces + p.segments - 1) / p.segments;
+    const int end = min(pieces, (seg + 1) * per);
 
     Sums a{kLowest, 0.f, 0.f};
-    Ranked ranked;
-    ranked.clear();
-    for (int64_t v0 = seg * per + wave * kWave; v0 < end; v0 += kLpThreads) {
-        const int64_t at = (v0 + lane) * 8 - shift;
-        const int64_t limit = v0 + lane < end ? V : 0;  // past the segment: nothing
-        float f[8];
-        load8<T>(x, at, limit, f);
+    Ranked ranked{(DN_LDS WaveRanks*)&ranks[TOP ? wave : 0], 0, 0, p.top, 0, 0};
+    int v0 = seg * per + wave * kWave;
+    Given given{-1, 0.f};
+    if (wave == 0 && p.segments == 1 && p.n) given.load(p, row, x, lane);
+    float f[8], g[8];
+    bool first = true;
+    if (v0 < end) load8<T>(x, (int64_t)(v0 + lane) * 8 - shift, v0 + lane < end ? V : 0, f);
+    for (; v0 < end; v0 += NT) {
+        const int v = v0 + lane;
+        if (v0 + NT < end) load8<T>(x, (int64_t)(v + NT) * 8 - shift, v + NT < end ? V : 0, g);
         const float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(f[0], f[1]), __builtin_fmaxf(f[2], f[3])),
                                            __builtin_fmaxf(__builtin_fmaxf(f[4], f[5]), __builtin_fmaxf(f[6], f[7])));
         if (__any(most > a.m)) raise(a, __builtin_fmaxf(a.m, most), c);
@@ -204,83 +405,95 @@ __global__ __launch_bounds__(kLpThreads) void logprobs_kernel(LpArgs p) {
             a.s = __builtin_fmaf(w, __builtin_fmaxf(d, kLeastExponent), a.s);
         }
         if constexpr (TOP) {
-            const uint32_t first = (uint32_t)max(at, (int64_t)0);
-            if (__any(at < limit && ranked.beats(most, first))) {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const int64_t id = at + e;
-                    unsigned long long left = __ballot(id >= 0 && id < limit && ranked.beats(f[e], (uint32_t)id));
-                    while (left) {
-                        const int b = __builtin_ctzll(left);
-                        const float xv = __uint_as_float(__builtin_amdgcn_readlane((int)__float_as_uint(f[e]), b));
-                        const uint32_t xi = (uint32_t)__builtin_amdgcn_readlane((int)id, b);
-                        ranked.insert(key_of(xv, xi), lane, p.top);
-                        left &= left - 1;
-                        left &= __ballot(ranked.beats(f[e], (uint32_t)id));
-                    }
-                }
-            }
+            if (first) ranked.start(most, v < end);
+            first = false;
+            ranked.add(f, most, v < end, v * 8 - shift, V, lane);  // v * 8 - shift < 2^31: V is
         }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) f[e] = g[e];
     }
     a = wave_join(a, c);
-    __shared__ float sums[kLpWaves][3];
-    __shared__ unsigned long long keys[TOP ? kLpWaves * kMaxTop : 1];
+    if (TOP && ranked.groups) ranked.flush(V, lane);
+    if (TOP && ranked.n > 64) ranked.cut(lane);
     if (lane == 0) {
         sums[wave][0] = a.m;
         sums[wave][1] = a.l;
         sums[wave][2] = a.s;
+        counts[wave] = ranked.n;
+        floors[wave] = ranked.n >= p.top ? ranked.floor : 1;
     }
-    if (TOP && lane < p.top) keys[wave * p.top + lane] = ranked.key;
     __syncthreads();
-    if (wave != 0) return;
-    a = Sums{sums[0][0], sums[0][1], sums[0][2]};
+    int total = 0;
+    uint32_t floor = 1;
+    if constexpr (TOP) {  // the waves' keys side by side
+        int mine = 0;
 #pragma unroll
-    for (int w = 1; w < kLpWaves; ++w) join(a, Sums{sums[w][0], sums[w][1], sums[w][2]}, c);
-    const unsigned long long key = TOP ? join_lists(keys, kLpWaves, p.top, lane) : 0;
+        for (int w = 0; w < NW; ++w) {
+            if (w == wave) mine = total;
+            total += counts[w];
+            floor = floors[w] > floor ? floors[w] : floor;
+        }
+        floor = __builtin_amdgcn_readfirstlane(floor);
+        if (lane < ranked.n) pool[mine + lane] = ranked.m->keys[lane];
+        __syncthreads();
+    }
+    if (wave != 0) return;
+    a = Sums{kLowest, 0.f, 0.f};
+    if (lane < NW) a = Sums{sums[lane][0], sums[lane][1], sums[lane][2]};
+    a = wave_join(a, c);
+    const unsigned long long key = TOP ? top_of((DN_LDS unsigned long long*)pool, __builtin_amdgcn_readfirstlane(total), p.top, floor, ranked.m, lane) : 0;
     if (p.segments == 1) {
-        finish<T>(p, row, x, a, key, lane, kWave);
+        finish<T>(p, row, x, a, key, given, lane);
     } else {
         if (lane == 0) *reinterpret_cast<f32x4*>(p.part_sums + (int64_t)blockIdx.x * 4) = f32x4{a.m, a.l, a.s, 0.f};
         if (TOP && lane < p.top) p.part_top[(int64_t)blockIdx.x * p.top + lane] = key;
     }
 }
 
-// One wave joins a row's segments (at most 64, one to a lane).
+// Joins a row's segments: one wave.
 template <class T>
 __global__ __launch_bounds__(kWave) void logprobs_join_kernel(LpArgs p) {
-    const int lane = threadIdx.x;
+    __shared__ unsigned long long pool[kMaxSegments * kMaxTop];
+    __shared__ __attribute__((aligned(16))) WaveRanks ranks;
+    const int lane = threadIdx.x, total = p.segments * p.top;
     const int64_t row = blockIdx.x;
+    const T* x = reinterpret_cast<const T*>(p.logits) + row * p.stride;
+    Given given{-1, 0.f};
+    if (p.n) given.load(p, row, x, lane);
+    for (int i = lane; i < total; i += kWave) pool[i] = p.part_top[row * total + i];
     Sums a{kLowest, 0.f, 0.f};
     if (lane < p.segments) {
         const f32x4 v = *reinterpret_cast<const f32x4*>(p.part_sums + (row * p.segments + lane) * 4);
         a = Sums{v[0], v[1], v[2]};
     }
+    lds_in_order();
     a = wave_join(a, p.scale * kLog2eF);
     const unsigned long long key =
-        p.top ? join_lists(p.part_top + row * p.segments * p.top, p.segments, p.top, lane) : 0;
-    finish<T>(p, row, reinterpret_cast<const T*>(p.logits) + row * p.stride, a, key, lane, kWave);
+        p.top ? top_of((DN_LDS unsigned long long*)pool, total, p.top, 1, (DN_LDS WaveRanks*)&ranks, lane) : 0;
+    finish<T>(p, row, x, a, key, given, lane);
+}
+
+template <class T, bool TOP>
+static void launch_logprobs(const LpArgs& p, int threads, hipStream_t s) {
+    const dim3 grid((unsigned)(p.T * p.segments));
+    if (threads == 512)
+        logprobs_kernel<T, TOP, 512><<<grid, 512, 0, s>>>(p);
+    else
+        logprobs_kernel<T, TOP, 256><<<grid, 256, 0, s>>>(p);
+    if (p.segments > 1) logprobs_join_kernel<T><<<dim3((unsigned)p.T), kWave, 0, s>>>(p);
 }
 
 hipError_t launch_token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
                                  const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
-                                 float* top_logprobs, int32_t* top_ids, void* workspace, int64_t segments, hipStream_t s) {
+                                 float* top_logprobs, int32_t* top_ids, void* workspace, hipStream_t s) {
+    const LogprobPlan plan = plan_logprobs(T, V);
     float* sums = reinterpret_cast<float*>(workspace);
-    const LpArgs p{logits, stride, T, V, n, scale, (int)top, (int)segments, targets, logprobs, entropy, top_logprobs, top_ids,
-                   sums, reinterpret_cast<unsigned long long*>(sums + (segments > 1 ? T * segments * 4 : 0))};
-    const dim3 grid((unsigned)(T * segments));
-    if (dtype == 0) {
-        if (top)
-            logprobs_kernel<float, true><<<grid, kLpThreads, 0, s>>>(p);
-        else
-            logprobs_kernel<float, false><<<grid, kLpThreads, 0, s>>>(p);
-        if (segments > 1) logprobs_join_kernel<float><<<dim3((unsigned)T), kWave, 0, s>>>(p);
-    } else {
-        if (top)
-            logprobs_kernel<__bf16, true><<<grid, kLpThreads, 0, s>>>(p);
-        else
-            logprobs_kernel<__bf16, false><<<grid, kLpThreads, 0, s>>>(p);
-        if (segments > 1) logprobs_join_kernel<__bf16><<<dim3((unsigned)T), kWave, 0, s>>>(p);
-    }
+    const LpArgs p{logits, stride, T, V, n, scale, (int)top, (int)plan.segments, targets, logprobs, entropy, top_logprobs,
+                   top_ids, sums, reinterpret_cast<unsigned long long*>(sums + (plan.segments > 1 ? T * plan.segments * 4 : 0))};
+    if (dtype == 0)
+        top ? launch_logprobs<float, true>(p, plan.threads, s) : launch_logprobs<float, false>(p, plan.threads, s);
+    else
+        top ? launch_logprobs<__bf16, true>(p, plan.threads, s) : launch_logprobs<__bf16, false>(p, plan.threads, s);
     return hipGetLastError();
 }
 

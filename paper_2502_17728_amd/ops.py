@@ -11,7 +11,6 @@ from __future__ import annotations
 
 import ctypes
 import dataclasses
-import functools
 import math
 import os
 from typing import Optional
@@ -923,15 +922,15 @@ def attention_shared_prefix_deferred(Q: torch.Tensor, cache: KVCache, prefix_tab
 _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
-def _on_its_device(f):
-    """f, launched on the device of its first tensor where that is not the current one."""
-    @functools.wraps(f)
-    def call(x, *args, **kwargs):
-        if isinstance(x, torch.Tensor) and x.is_cuda and x.get_device() != _current_device():
-            with torch.cuda.device(x.get_device()):
-                return f(x, *args, **kwargs)
-        return f(x, *args, **kwargs)
-    return call
+def _launch(f, dev: int, *args):
+    """f(*args), called on device dev.  Raises if it refuses."""
+    if _current_device() == dev:
+        st = f(*args)
+    else:
+        with torch.cuda.device(dev):
+            st = f(*args)
+    if st:
+        raise DNError(f.__name__, st)
 
 
 def _ptr(t: Optional[torch.Tensor], name: str, shape, dtype, device: int):
@@ -953,74 +952,59 @@ def _rows_of(x: torch.Tensor):
     return _dev(x, "x"), M, K, x.get_device()
 
 
-def _sum_of(x, residual, total, M, K, dev, stream):
-    """Pointers of the residual and of the sum's tensor, which is made where it was not given."""
-    if residual is None:
-        if total is not None:
-            raise ValueError("there is no residual to sum")
-        return None, None, None
-    rp = _ptr(residual, "residual", (M, K), x.dtype, dev)
-    if total is None:
-        total = x.new_empty((M, K)) if stream is None else _empty(x, (M, K), stream)
-        return rp, total.data_ptr(), total
-    return rp, _ptr(total, "total", (M, K), x.dtype, dev), total
+def _made(x, t, name, shape, dtype, dev, stream):
+    """(tensor, pointer) of an output: the one given, or one made for the call."""
+    if t is None:
+        if stream is not None:
+            t = _empty(x, shape, stream, dtype)
+        elif shape == x.shape and x.is_contiguous():  # the quickest of torch's ways
+            t = torch.empty_like(x, dtype=dtype)
+        else:
+            t = x.new_empty(shape, dtype=dtype)
+        return t, t.data_ptr()
+    return t, _ptr(t, name, shape, dtype, dev)
 
 
-@_on_its_device
+def _norm_args(x, residual, gamma, total, stream):
+    """What both norms take: pointer and sizes of x, pointers of the residual, gamma and the sum, the sum."""
+    xp, M, K, dev = _rows_of(x)
+    rp = sp = None
+    if residual is not None:
+        rp = _ptr(residual, "residual", (M, K), x.dtype, dev)
+        total, sp = _made(x, total, "total", (M, K), x.dtype, dev, stream)
+    elif total is not None:
+        raise ValueError("there is no residual to sum")
+    return xp, M, K, dev, rp, _ptr(gamma, "gamma", (K,), x.dtype, dev), sp, total
+
+
 def residual_rmsnorm(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
                      eps: float = 1e-5, total: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                      stream=None):
     """(RMSNorm(x + residual) * gamma, x + residual) of x[M, K] and residual[M, K]; without a residual the
     second is None.  total may be x or residual: the stream updated in place."""
-    xp, M, K, dev = _rows_of(x)
-    rp, sp, total = _sum_of(x, residual, total, M, K, dev, stream)
-    gp = _ptr(gamma, "gamma", (K,), x.dtype, dev)
-    if out is None:
-        out = x.new_empty((M, K)) if stream is None else _empty(x, (M, K), stream)
-        op = out.data_ptr()
-    else:
-        op = _ptr(out, "out", (M, K), x.dtype, dev)
-    st = _lib.residual_rmsnorm(xp, rp, gp, M, K, eps, _dt(x), sp, op, _stream_of(stream, x))
-    if st:
-        raise DNError("residual_rmsnorm", st)
+    xp, M, K, dev, rp, gp, sp, total = _norm_args(x, residual, gamma, total, stream)
+    out, op = _made(x, out, "out", (M, K), x.dtype, dev, stream)
+    _launch(_lib.residual_rmsnorm, dev, xp, rp, gp, M, K, eps, _dt(x), sp, op, _stream_of(stream, x))
     return out, total
 
 
-def _codes_for(x, M, K, codes, scales, dev, stream):
-    if codes is None:
-        codes = _empty(x, (M, K), stream, torch.float8_e4m3fn)
-        cp = codes.data_ptr()
-    else:
-        cp = _ptr(codes, "codes", (M, K), torch.float8_e4m3fn, dev)
-    if scales is None:
-        scales = _empty(x, (M,), stream, torch.float32)
-        return cp, scales.data_ptr(), codes, scales
-    return cp, _ptr(scales, "scales", (M,), torch.float32, dev), codes, scales
-
-
-@_on_its_device
 def residual_rmsnorm_fp8(x: torch.Tensor, residual: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
                          eps: float = 1e-5, total: Optional[torch.Tensor] = None, codes: Optional[torch.Tensor] = None,
                          scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales, x + residual): residual_rmsnorm with its rows as e4m3 codes [M, K] and one scale a row."""
-    xp, M, K, dev = _rows_of(x)
-    rp, sp, total = _sum_of(x, residual, total, M, K, dev, stream)
-    gp = _ptr(gamma, "gamma", (K,), x.dtype, dev)
-    cp, scp, codes, scales = _codes_for(x, M, K, codes, scales, dev, stream)
-    st = _lib.residual_rmsnorm_fp8(xp, rp, gp, M, K, eps, _dt(x), sp, cp, scp, _stream_of(stream, x))
-    if st:
-        raise DNError("residual_rmsnorm_fp8", st)
+    xp, M, K, dev, rp, gp, sp, total = _norm_args(x, residual, gamma, total, stream)
+    codes, cp = _made(x, codes, "codes", (M, K), torch.float8_e4m3fn, dev, stream)
+    scales, scp = _made(x, scales, "scales", (M,), torch.float32, dev, stream)
+    _launch(_lib.residual_rmsnorm_fp8, dev, xp, rp, gp, M, K, eps, _dt(x), sp, cp, scp, _stream_of(stream, x))
     return codes, scales, total
 
 
-@_on_its_device
 def rows_fp8(x: torch.Tensor, codes: Optional[torch.Tensor] = None, scales: Optional[torch.Tensor] = None, stream=None):
     """(codes, scales): the rows of x[M, K] as e4m3 codes and one scale each, x = codes * scales[:, None]."""
     xp, M, K, dev = _rows_of(x)
-    cp, scp, codes, scales = _codes_for(x, M, K, codes, scales, dev, stream)
-    st = _lib.rows_fp8(xp, M, K, _dt(x), cp, scp, _stream_of(stream, x))
-    if st:
-        raise DNError("rows_fp8", st)
+    codes, cp = _made(x, codes, "codes", (M, K), torch.float8_e4m3fn, dev, stream)
+    scales, scp = _made(x, scales, "scales", (M,), torch.float32, dev, stream)
+    _launch(_lib.rows_fp8, dev, xp, M, K, _dt(x), cp, scp, _stream_of(stream, x))
     return codes, scales
 
 
@@ -1050,7 +1034,6 @@ def linear_fp8_packed_bytes(K: int, N: int, gated: bool = False) -> int:
     return int(_lib.linear_fp8_packed_bytes(K, N, int(gated)))
 
 
-@_on_its_device
 def linear_fp8_prepare(W: torch.Tensor, scales: Optional[torch.Tensor] = None, gamma: Optional[torch.Tensor] = None,
                        bias: Optional[torch.Tensor] = None, up: Optional[torch.Tensor] = None,
                        up_scales: Optional[torch.Tensor] = None, up_bias: Optional[torch.Tensor] = None,
@@ -1071,10 +1054,9 @@ def linear_fp8_prepare(W: torch.Tensor, scales: Optional[torch.Tensor] = None, g
         raise DNError("linear_fp8_packed_bytes", 2)
     packed = _empty(W, nbytes, stream, torch.uint8)
     desc = LinearFp8Weights()
-    _check("linear_fp8_prepare", _lib.linear_fp8_prepare(
-        _dev(W, "W"), _dev(scales, "scales"), _dev(gamma, "gamma"), _dev(bias, "bias"), _dev(up, "up"),
-        _dev(up_scales, "up_scales"), _dev(up_bias, "up_bias"), K, N, dt, packed.data_ptr(), nbytes, ctypes.byref(desc),
-        _stream_of(stream, W)))
+    _launch(_lib.linear_fp8_prepare, W.get_device(), _dev(W, "W"), _dev(scales, "scales"), _dev(gamma, "gamma"),
+            _dev(bias, "bias"), _dev(up, "up"), _dev(up_scales, "up_scales"), _dev(up_bias, "up_bias"), K, N, dt,
+            packed.data_ptr(), nbytes, ctypes.byref(desc), _stream_of(stream, W))
     return PreparedFp8(packed, desc)
 
 
@@ -1082,18 +1064,19 @@ def linear_fp8_workspace_bytes(M: int, w: PreparedFp8) -> int:
     return int(_lib.linear_fp8_workspace_bytes(M, w.ref))
 
 
-def _scratch(x: torch.Tensor, workspace: Optional[torch.Tensor], need, stream):
-    """The workspace given, or one made of need() bytes (None for 0)."""
+def _scratch(x: torch.Tensor, workspace: Optional[torch.Tensor], need, sizes, stream):
+    """Pointer and bytes of the workspace given, or of one of need(*sizes) bytes (None for 0), and what holds it."""
     if workspace is None:
-        n = need()
-        return _empty(x, n, stream, torch.uint8) if n else None
-    if workspace.dtype is not torch.uint8 or workspace.get_device() != x.get_device() or not workspace.is_contiguous():
+        n = need(*sizes)
+        if not n:
+            return None, 0, None
+        workspace = _empty(x, n, stream, torch.uint8)
+    elif workspace.dtype is not torch.uint8 or workspace.get_device() != x.get_device() or not workspace.is_contiguous():
         _expect(workspace, "workspace", None, torch.uint8, x.device)
         _dev(workspace, "workspace")
-    return workspace
+    return workspace.data_ptr(), workspace.numel(), workspace
 
 
-@_on_its_device
 def linear_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: PreparedFp8, activation: str = "none",
                residual: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
                out_dtype: Optional[torch.dtype] = None, workspace: Optional[torch.Tensor] = None,
@@ -1118,17 +1101,13 @@ def linear_fp8(x: torch.Tensor, x_scales: torch.Tensor, w: PreparedFp8, activati
     if out_dtype is None:
         like = out if out is not None else residual
         out_dtype = torch.bfloat16 if like is None else like.dtype
+    if out_dtype is not torch.bfloat16 and out_dtype is not torch.float32:
+        raise TypeError(f"unsupported out_dtype {out_dtype}")
     rp = _ptr(residual, "residual", (M, N), out_dtype, dev)
-    if out is None:
-        out = _empty(x, (M, N), stream, out_dtype)
-        op = out.data_ptr()
-    else:
-        op = _ptr(out, "out", (M, N), out_dtype, dev)
-    held = _scratch(x, workspace, lambda: _lib.linear_fp8_workspace_bytes(M, w.ref), stream)
-    st = _lib.linear_fp8(xp, sp, w.ref, M, act, rp, _dt(out), None if held is None else held.data_ptr(),
-                         0 if held is None else held.numel(), op, _stream_of(stream, x))
-    if st:
-        raise DNError("linear_fp8", st)
+    out, op = _made(x, out, "out", (M, N), out_dtype, dev, stream)
+    wp, wn, held = _scratch(x, workspace, _lib.linear_fp8_workspace_bytes, (M, w.ref), stream)
+    _launch(_lib.linear_fp8, dev, xp, sp, w.ref, M, act, rp, DN_BF16 if out_dtype is torch.bfloat16 else DN_F32, wp, wn, op,
+            _stream_of(stream, x))
     return out
 
 
@@ -1137,7 +1116,6 @@ def token_logprobs_workspace_bytes(T: int, V: int, top: int = 0) -> int:
     return int(_lib.token_logprobs_workspace_bytes(T, V, top))
 
 
-@_on_its_device
 def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, scale: float = 1.0,
                    entropy: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
     """{"logprobs", "entropy", "top_logprobs", "top_ids"} of softmax(scale * logits) for logits[T, V] (rows may be
@@ -1151,30 +1129,24 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
     if logits.stride(1) != 1 and V != 1:
         raise ValueError("logits must be contiguous within a row")
     stride = logits.stride(0) if T != 1 else V
-    n, tp, lp, given = 0, None, None, None
+    dev = logits.get_device()
+    n, tp, lp, ep, kp, ip = 0, None, None, None, None, None
+    given = spread = likely = ids = None
     if targets is not None:
         if targets.dim() != 2:
             raise ValueError(f"targets has shape {list(targets.shape)}, expected [T, n]")
         n = targets.shape[1]
         tp = _int32(targets, "targets", (T, n), logits)
         if n:
-            given = _empty(logits, (T, n), stream, torch.float32)
-            lp = given.data_ptr()
+            given, lp = _made(logits, None, "", (T, n), torch.float32, dev, stream)
         else:
             tp = None
-    out = {"logprobs": given, "entropy": None, "top_logprobs": None, "top_ids": None}
-    ep = kp = ip = None
     if entropy:
-        out["entropy"] = _empty(logits, (T,), stream, torch.float32)
-        ep = out["entropy"].data_ptr()
+        spread, ep = _made(logits, None, "", (T,), torch.float32, dev, stream)
     if top > 0:
-        out["top_logprobs"] = _empty(logits, (T, top), stream, torch.float32)
-        out["top_ids"] = _empty(logits, (T, top), stream, torch.int32)
-        kp, ip = out["top_logprobs"].data_ptr(), out["top_ids"].data_ptr()
-    held = _scratch(logits, workspace, lambda: _lib.token_logprobs_workspace_bytes(T, V, top), stream)
-    st = _lib.token_logprobs(logits.data_ptr(), stride, T, V, _dt(logits), scale, tp, n, top, lp, ep, kp, ip,
-                             None if held is None else held.data_ptr(), 0 if held is None else held.numel(),
-                             _stream_of(stream, logits))
-    if st:
-        raise DNError("token_logprobs", st)
-    return out
+        likely, kp = _made(logits, None, "", (T, top), torch.float32, dev, stream)
+        ids, ip = _made(logits, None, "", (T, top), torch.int32, dev, stream)
+    wp, wn, held = _scratch(logits, workspace, _lib.token_logprobs_workspace_bytes, (T, V, top), stream)
+    _launch(_lib.token_logprobs, dev, logits.data_ptr(), stride, T, V, _dt(logits), scale, tp, n, top, lp, ep, kp, ip, wp, wn,
+            _stream_of(stream, logits))
+    return {"logprobs": given, "entropy": spread, "top_logprobs": likely, "top_ids": ids}
