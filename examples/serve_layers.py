@@ -3,10 +3,12 @@
 A prompt that all sequences share is cached once, chunk by chunk; the sequences' own texts follow in one
 ragged call; then every sequence generates, one token a step, the step recorded once as a HIP graph that
 replays while lengths, slots and positions move on the device.  A document that was cached by itself is
-moved behind a sequence without running the layers again: read, turned by the distance, written.
+moved behind a sequence without running the layers again: read, turned by the distance, written.  Texts can be
+scored: the log probability of each of their tokens.  With --products fp8 the layers' products run on e4m3 codes:
+rows are quantised as they are normalized, and each product adds its result to the residual stream itself.
 
     python examples/serve_layers.py                        # 8B-class layers, 32 sequences, an e4m3 cache
-    python examples/serve_layers.py --layers 4 --format bf16
+    python examples/serve_layers.py --layers 4 --format bf16 --products fp8
 
 Weights and tokens are random: what runs is the arithmetic of such a model, not its text.
 """
@@ -45,16 +47,39 @@ class Layer:
         return x + ops.gemm(ops.rms_swiglu_deferred(x, self.mlp), self.down)
 
 
+class Layer8:
+    """The same layer on e4m3 codes: RMSNorm's 1 / rms waits in the rows' scales, gamma is in the weights."""
+
+    def __init__(self, hidden, q_heads, heads, d, ffn, pages, fmt, g):
+        w = lambda K, N: (torch.randn((K, N), generator=g, device="cuda") * K ** -0.5).to(torch.bfloat16)
+        gamma = torch.ones(hidden, dtype=torch.bfloat16, device="cuda")
+        self.qkv = ops.linear_fp8_prepare(w(hidden, (q_heads + 2 * heads) * d), gamma=gamma)
+        self.out = ops.linear_fp8_prepare(w(q_heads * d, hidden))
+        self.mlp = ops.linear_fp8_prepare(w(hidden, ffn), gamma=gamma, up=w(hidden, ffn))
+        self.down = ops.linear_fp8_prepare(w(ffn, hidden))
+        self.cache = ops.kv_cache_create(pages, heads, d, fmt)
+
+    def __call__(self, x, attend, slots, positions, table):
+        codes, scales, _ = ops.residual_rmsnorm_fp8(x)
+        q = ops.kv_cache_append(self.cache, ops.linear_fp8(codes, scales, self.qkv), slots, positions, table)
+        codes, scales = ops.rows_fp8(attend(q, self.cache).view(x.shape[0], -1))
+        x = ops.linear_fp8(codes, scales, self.out, residual=x)
+        codes, scales, _ = ops.residual_rmsnorm_fp8(x)
+        codes, scales = ops.rows_fp8(ops.linear_fp8(codes, scales, self.mlp, activation="silu"))
+        return ops.linear_fp8(codes, scales, self.down, residual=x)
+
+
 class Server:
     def __init__(self, layers=2, hidden=4096, q_heads=32, heads=8, d=128, ffn=14336, vocabulary=8192, sequences=32,
-                 prompt=4096, room=512, fmt="fp8", seed=0):
+                 prompt=4096, room=512, fmt="fp8", seed=0, products="bf16"):
         g = torch.Generator(device="cuda").manual_seed(seed)
         self.sequences, self.prompt = sequences, prompt
         own = -(-room // PAGE)
         self.room = own * PAGE  # tokens of a sequence behind the prompt at most
         self.prefix_pages = -(-prompt // PAGE)
         pages = self.prefix_pages + sequences * own
-        self.layers = [Layer(hidden, q_heads, heads, d, ffn, pages, fmt, g) for _ in range(layers)]
+        kind = {"bf16": Layer, "fp8": Layer8}[products]
+        self.layers = [kind(hidden, q_heads, heads, d, ffn, pages, fmt, g) for _ in range(layers)]
         self.table = ops.rotary_table(ops.rotary_frequencies(d)[0], prompt + self.room)
         self.embed = torch.randn((vocabulary, hidden), generator=g, device="cuda").to(torch.bfloat16)
         self.head = ops.ln_linear_prepare(self.embed.t().contiguous() * hidden ** -0.5,
@@ -96,6 +121,19 @@ class Server:
 
     def read_texts(self, texts):
         """Each sequence's own tokens, all in one ragged call; the tokens that follow."""
+        x, q_start = self._read(texts)
+        return self.next_tokens(x[q_start[1:].long() - 1])
+
+    def score(self, texts):
+        """Reads texts as read_texts does: ln p of each token but the first of each, given all before it (0 in the last
+        row of each text, which nothing follows), and the distributions' entropies."""
+        x, q_start = self._read(texts)
+        follows = torch.cat([torch.cat(texts)[1:], q_start.new_zeros(1)]).int()
+        follows[q_start[1:].long() - 1] = -1
+        got = ops.token_logprobs(ops.rms_linear_deferred(x, self.head), follows[:, None])
+        return got["logprobs"][:, 0], got["entropy"]
+
+    def _read(self, texts):
         if len(texts) != self.sequences or min(map(len, texts)) < 1:
             raise ValueError(f"a text of one token at least is needed for each of {self.sequences} sequences")
         lengths = ints([len(t) for t in texts])
@@ -105,9 +143,8 @@ class Server:
         sequence = torch.repeat_interleave(torch.arange(self.sequences, device="cuda"), lengths.long())
         at = (torch.arange(len(sequence), device="cuda") - q_start[sequence] + self.kv_len[sequence]).int()
         self.kv_len += lengths
-        x = self.run(torch.cat(texts), self.attend_behind_prompt(q_start, self.kv_len), self.slots_of(sequence, at),
-                     (self.prompt + at).int())
-        return self.next_tokens(x[q_start[1:].long() - 1])
+        return self.run(torch.cat(texts), self.attend_behind_prompt(q_start, self.kv_len), self.slots_of(sequence, at),
+                        (self.prompt + at).int()), q_start
 
     def step(self, tokens):
         """One token of every sequence: the lengths move on the device, so the step can be replayed.  A sequence
@@ -153,11 +190,12 @@ def main():
     p.add_argument("--prompt", type=int, default=4096)
     p.add_argument("--steps", type=int, default=64)
     p.add_argument("--format", choices=sorted(ops.KV_FORMATS), default="fp8")
+    p.add_argument("--products", choices=("bf16", "fp8"), default="bf16")
     a = p.parse_args()
     if min(a.layers, a.sequences, a.prompt, a.steps) < 1:
         p.error("--layers, --sequences, --prompt and --steps are at least 1")
     room = 256 + a.steps
-    s = Server(layers=a.layers, sequences=a.sequences, prompt=a.prompt, room=room, fmt=a.format)
+    s = Server(layers=a.layers, sequences=a.sequences, prompt=a.prompt, room=room, fmt=a.format, products=a.products)
     draw = lambda n: torch.randint(0, s.embed.shape[0], (n,), device="cuda")
 
     def timed(what, tokens, f):
@@ -173,6 +211,11 @@ def main():
     timed(f"prompt of {a.prompt} tokens", a.prompt, lambda: s.read_prompt(draw(a.prompt)))
     texts = [draw(20 + 29 * b % 100) for b in range(a.sequences)]
     s.read_texts(texts)
+    s.kv_len.zero_()
+    s.score(texts)
+    s.kv_len.zero_()
+    logprobs, _ = timed("ragged texts scored", sum(map(len, texts)), lambda: s.score(texts))
+    print(f"    {float(logprobs.sum()) / (len(logprobs) - len(texts)):.2f} a token")
     s.kv_len.zero_()
     tokens = timed("ragged texts", sum(map(len, texts)), lambda: s.read_texts(texts))
     n = min(100, a.prompt)  # the prompt's first tokens once more, behind sequence 0: 100 tokens that no layer runs

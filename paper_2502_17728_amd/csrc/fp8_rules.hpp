@@ -60,7 +60,7 @@ constexpr Fp8Tile kFp8Tile[kFp8Tiles] = {{64, 64, 2, 0.235, 0.36},  {64, 128, 1,
                                          {256, 128, 1, 0.80, 0.80}, {256, 256, 1, 1.42, 1.42}};
 constexpr int64_t kMaxSplits = 16;
 
-// tile >= 0: that tile, K in `splits` parts.  tile < 0: the streamed kernel, rf row fragments x nc column blocks.
+// tile >= 0: that tile, K in `splits` parts.  tile < 0: streamed (rf 1) or ring (rf 2) kernel, 16 rf rows x nc column blocks.
 struct Fp8Plan {
     int tile, rf, nc;
     int64_t splits;
@@ -75,15 +75,15 @@ inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32
     const int64_t stages = (K + 127) / 128;
     const double w_us = (double)blocks * 16 * (double)K / 6.2e6, slow = f32 ? 1.8 : 1.0;
     Fp8Plan best{-1, 0, 0, 1, 0};
-    // Streamed: W straight into registers, up to 64 rows.  Per step of 128 codes 0.02 us and 0.072 us per column block
-    // with 16 rows to a workgroup, 0.07 and 0.067 with 32.  16 rows 4096 -> 4096 5.7 us, 64 x 64 tiles 10.7.
+    // Up to 64 rows: W streamed into registers (rf 1) or rings of the waves' own (rf 2).  Per step of 128 codes 0.02 us and
+    // 0.072 us per column block, or 0.045 and 0.068.  16 rows 4096 -> 4096 5.7 us, 32 rows 6.4, 64 rows 7.2, in tiles 10.4.
     for (int rf = 1; rf <= 2 && M <= 64; ++rf) {
         const int64_t rows = (M + 16 * rf - 1) / (16 * rf);
-        static constexpr int kNc[6] = {1, 2, 3, 4, 6, 8};
+        static constexpr int kNc[7] = {1, 2, 3, 4, 6, 7, 8};
         for (int nc : kNc) {
-            if ((gated && nc % 2) || (rf == 2 && nc > 4)) continue;
+            if ((gated && nc % 2) || (rf == 2 && nc == 8)) continue;
             const int64_t wgs = rows * ((blocks + nc - 1) / nc);
-            const double step = rf == 1 ? 0.02 + 0.072 * nc : 0.07 + 0.067 * nc;
+            const double step = rf == 1 ? 0.02 + 0.072 * nc : 0.045 + 0.068 * nc;
             const double us = 2.7 + std::max(w_us, (double)((wgs + 255) / 256) * (double)stages * step * slow);
             if (best.rf == 0 || us < best.us) best = Fp8Plan{-1, rf, nc, 1, us};
         }

@@ -208,34 +208,50 @@ __global__ __launch_bounds__(256) void fp8_join_kernel(Fp8Args p) {
 }
 
 // ------------------------------------------------------------------------------- few rows
-// 16 RF rows x 16 NC packed columns to a workgroup, whose KS waves take every KS-th step of 128 codes of K: W comes
-// straight from HBM into operand registers, 1 KiB to an instruction and read once; x, which every
-// workgroup reads, from L2.  No barrier until the waves' sums meet in LDS.  U steps' loads are issued together.
-template <int RF, int NC, int KS, int U, bool F32>
+// The KS waves' sums of ROWS x 16 NC packed columns, LDR floats to a row and one wave's behind the other's in LDS.
+template <int ROWS, int NC, int KS, int LDR>
+__device__ __forceinline__ void finish_waves(const Fp8Args& p, const float* sums, int64_t m0, int64_t nb0) {
+    const int per_row = p.gated ? NC : NC * 2, rows = (int)min((int64_t)ROWS, p.M - m0);
+    for (int i = threadIdx.x; i < rows * per_row; i += KS * kWave) {
+        const int r = i / per_row;
+        const Column k = column_of(nb0 * 16, i % per_row * 8, p.gated);
+        if (k.out >= p.N) continue;
+        const float* in = sums + r * LDR + (k.packed - nb0 * 16);
+        float g[8] = {}, u[8] = {};
+#pragma unroll
+        for (int w = 0; w < KS; ++w) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) g[e] += in[w * ROWS * LDR + e];
+            if (p.gated)
+#pragma unroll
+                for (int e = 0; e < 8; ++e) u[e] += in[w * ROWS * LDR + 16 + e];
+        }
+        finish8(p, g, u, m0 + r, k.packed, k.out);
+    }
+}
+
+// 16 rows x 16 NC packed columns to a workgroup, whose KS waves take every KS-th step of 128 codes of K: W comes straight
+// from HBM into operand registers, 1 KiB to an instruction and read once; x, which every workgroup reads,
+// from L2.  No barrier until the waves' sums meet in LDS.  U steps' loads are issued together.  Bound by W: one row
+// 4096 -> 12288 9.5 us (5.3 TB/s with the launch), 8192 -> 28672 37 us (6.3 TB/s).
+template <int NC, int KS, int U, bool F32>
 __global__ __launch_bounds__(KS* kWave) void fp8_stream_kernel(Fp8Args p) {
     constexpr int LDR = NC * 16 + 4;
-    __shared__ __attribute__((aligned(16))) float sums[KS * RF * 16 * LDR];
+    __shared__ __attribute__((aligned(16))) float sums[KS * 16 * LDR];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int tiles_m = (int)((p.M + RF * 16 - 1) / (RF * 16));
-    const int t = xcd_contiguous(blockIdx.x, gridDim.x);
-    const int64_t m0 = (int64_t)(t % tiles_m) * RF * 16, nb0 = (int64_t)(t / tiles_m) * NC;
-    const int nst = (int)(p.kchunks / 2);
-
-    const char* xr[RF];
-    const int at = (lane >> 4) * 16;
-#pragma unroll
-    for (int r = 0; r < RF; ++r) xr[r] = p.x + min(m0 + r * 16 + (lane & 15), p.M - 1) * p.K;
+    const int tiles_m = (int)((p.M + 15) / 16), t = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t m0 = (int64_t)(t % tiles_m) * 16, nb0 = (int64_t)(t / tiles_m) * NC;
+    const int nst = (int)(p.kchunks / 2), at = (lane >> 4) * 16;
+    const char* xr = p.x + min(m0 + (lane & 15), p.M - 1) * p.K;
     const char* wc[NC];
 #pragma unroll
     for (int c = 0; c < NC; ++c) wc[c] = p.w + packed_chunk(min(nb0 + c, p.blocks - 1), 0, p.kchunks, lane);
 
-    f32x4 acc[RF][NC];
+    f32x4 acc[NC];
 #pragma unroll
-    for (int r = 0; r < RF; ++r)
-#pragma unroll
-        for (int c = 0; c < NC; ++c) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < NC; ++c) acc[c] = f32x4{0.f, 0.f, 0.f, 0.f};
     for (int s = wave; s < nst; s += KS * U) {
-        u32x4 a[U][RF][2], b[U][NC][2];
+        u32x4 a[U][2], b[U][NC][2];
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u == 0 || s + u * KS < nst) {
@@ -245,46 +261,108 @@ __global__ __launch_bounds__(KS* kWave) void fp8_stream_kernel(Fp8Args p) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h) b[u][c][h] = ld16_stream(wc[c] + (st * 2 + h) * kChunkBytes);
 #pragma unroll
-                for (int r = 0; r < RF; ++r)
-#pragma unroll
-                    for (int h = 0; h < 2; ++h)  // pieces past K: the row's last one, against weights that are zero there
-                        a[u][r][h] = ld16(xr[r] + min(st * 128 + h * 64 + at, p.K - 16));
+                for (int h = 0; h < 2; ++h)  // pieces past K: the row's last one, against weights that are zero there
+                    a[u][h] = ld16(xr + min(st * 128 + h * 64 + at, p.K - 16));
             }
 #pragma unroll
         for (int u = 0; u < U; ++u)
             if (u == 0 || s + u * KS < nst) {
 #pragma unroll
-                for (int r = 0; r < RF; ++r)
-#pragma unroll
-                    for (int c = 0; c < NC; ++c)
-                        acc[r][c] = mfma_codes<F32>(a[u][r][0], a[u][r][1], b[u][c][0], b[u][c][1], acc[r][c]);
+                for (int c = 0; c < NC; ++c) acc[c] = mfma_codes<F32>(a[u][0], a[u][1], b[u][c][0], b[u][c][1], acc[c]);
             }
     }
-    float* mine = sums + wave * RF * 16 * LDR;
+    float* mine = sums + wave * 16 * LDR;
 #pragma unroll
-    for (int r = 0; r < RF; ++r)
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) mine[(4 * (lane >> 4) + i) * LDR + c * 16 + (lane & 15)] = acc[c][i];
+    __syncthreads();
+    finish_waves<16, NC, KS, LDR>(p, sums, m0, nb0);
+}
+
+// The same for 32 rows, whose x loads would be half lines: each wave copies its steps of x, as whole 128-byte lines, and
+// of W into a ring of D slots of its own in LDS and waits for nobody.  Bound by the copies, about 57 bytes a ns
+// and CU for x (from L2) and W together: 32 rows 14336 -> 4096 15.3 us (loads into registers 18.2), 4096 -> 4096 6.4 (7.3).
+template <int NC, int KS, int D, bool F32>
+__global__ __launch_bounds__(KS* kWave) void fp8_ring_kernel(Fp8Args p) {
+    constexpr int ROWS = 32, P = 4 + 2 * NC, SLOT = P * kChunkBytes, LDR = NC * 16 + 4;
+    static_assert(D * SLOT >= ROWS * LDR * 4, "a wave's sums fit its ring");
+    static_assert((D - 1) * P < 64, "copies in flight");
+    __shared__ __attribute__((aligned(1024))) char smem[KS * D * SLOT];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int tiles_m = (int)((p.M + ROWS - 1) / ROWS), t = xcd_contiguous(blockIdx.x, gridDim.x);
+    const int64_t m0 = (int64_t)(t % tiles_m) * ROWS, nb0 = (int64_t)(t / tiles_m) * NC;
+    const int nst = (int)(p.kchunks / 2), n = (nst - wave + KS - 1) / KS;  // this wave's steps
+    const uint64_t a_base = uniform_u64(p.x + m0 * p.K), b_base = uniform_u64(p.w + nb0 * p.kchunks * kChunkBytes);
+    const uint32_t ring = lds_addr32(smem) + wave * D * SLOT, last = (uint32_t)(p.K - 16);
+    char* mine = smem + wave * D * SLOT;
+    uint32_t a_off[4], a_piece[4], b_off[NC];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const int r = j * 8 + (lane >> 3);
+        a_off[j] = (uint32_t)((min(m0 + r, p.M - 1) - m0) * p.K);
+        a_piece[j] = (uint32_t)(((lane & 7) ^ a_swz(r)) * 16);
+    }
+#pragma unroll
+    for (int c = 0; c < NC; ++c) b_off[c] = (uint32_t)packed_chunk(min(nb0 + c, p.blocks - 1) - nb0, 0, p.kchunks, lane);
+    auto issue = [&](int i) {
+        const int s = wave + i * KS;
+        const uint32_t base = ring + (uint32_t)(i % D * SLOT);
 #pragma unroll
         for (int c = 0; c < NC; ++c)
 #pragma unroll
-            for (int i = 0; i < 4; ++i) mine[(r * 16 + 4 * (lane >> 4) + i) * LDR + c * 16 + (lane & 15)] = acc[r][c][i];
-    __syncthreads();
-    const int per_row = p.gated ? NC : NC * 2, rows = (int)min((int64_t)RF * 16, p.M - m0);
-    for (int i = threadIdx.x; i < rows * per_row; i += KS * kWave) {
-        const int r = i / per_row;
-        const Column k = column_of(nb0 * 16, i % per_row * 8, p.gated);
-        if (k.out >= p.N) continue;
-        const float* in = sums + r * LDR + (k.packed - nb0 * 16);
-        float g[8] = {}, v[8] = {};
+            for (int h = 0; h < 2; ++h)
+                g2lds16_stream_sb(b_base + (uint64_t)(2 * s + h) * kChunkBytes, b_off[c], base + (4 + c * 2 + h) * kChunkBytes);
 #pragma unroll
-        for (int w = 0; w < KS; ++w) {
+        for (int j = 0; j < 4; ++j)  // pieces past K: the row's last one, against weights that are zero there
+            g2lds16_async_sb(a_base, a_off[j] + min((uint32_t)s * 128 + a_piece[j], last), base + j * kChunkBytes);
+    };
+    f32x4 acc[2][NC];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) g[e] += in[w * RF * 16 * LDR + e];
-            if (p.gated)
+    for (int r = 0; r < 2; ++r)
 #pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] += in[w * RF * 16 * LDR + 16 + e];
+        for (int c = 0; c < NC; ++c) acc[r][c] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int i = 0; i < D && i < n; ++i) issue(i);
+    for (int i = 0; i < n; ++i) {
+        if (i + D - 1 < n)
+            wait_vmcnt<(D - 1) * P>();  // step i's copies; those of the next D - 1 may be on their way
+        else
+            wait_vmcnt<0>();
+        lds_in_order();
+        char* at = mine + i % D * SLOT;
+        u32x4 a[2][2], b[NC][2];
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int row = r * 16 + (lane & 15);
+                a[r][h] = lds_ld16(lds_ptr(at + row * 128 + (((h * 4 + (lane >> 4)) ^ a_swz(row)) << 4)));
+            }
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) b[c][h] = lds_ld16(lds_ptr(at + (4 + c * 2 + h) * kChunkBytes + lane * 16));
+        lds_in_order();
+        if (i + D < n) {
+            wait_lgkm0();  // step i is in registers: its slot is free
+            issue(i + D);
         }
-        finish8(p, g, v, m0 + r, k.packed, k.out);
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c) acc[r][c] = mfma_codes<F32>(a[r][0], a[r][1], b[c][0], b[c][1], acc[r][c]);
     }
+    __syncthreads();
+    float* sums = reinterpret_cast<float*>(smem);
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                sums[(wave * ROWS + r * 16 + 4 * (lane >> 4) + i) * LDR + c * 16 + (lane & 15)] = acc[r][c][i];
+    __syncthreads();
+    finish_waves<ROWS, NC, KS, LDR>(p, sums, m0, nb0);
 }
 
 // f(0) .. f(N - 1) with constants: loops whose bodies the compiler would not unroll
@@ -645,27 +723,36 @@ static void launch_tile(const Fp8Args& p, int tile, dim3 grid, hipStream_t s) {
         p.out_f32 ? launch_tile_<false, true>(p, tile, grid, s) : launch_tile_<false, false>(p, tile, grid, s);
 }
 
-template <int RF, int NC>
+template <int NC>
 static void launch_stream_(const Fp8Args& p, dim3 grid, hipStream_t s) {
-    // 2 steps' loads at a time while the registers hold them
-    constexpr int U = RF + NC <= 3 ? 2 : 1;
+    constexpr int U = NC <= 2 ? 2 : 1;  // 2 steps' loads at a time while W's bytes in flight are few
     if (p.out_f32)
-        fp8_stream_kernel<RF, NC, 8, U, true><<<grid, 512, 0, s>>>(p);
+        fp8_stream_kernel<NC, 8, U, true><<<grid, 512, 0, s>>>(p);
     else
-        fp8_stream_kernel<RF, NC, 8, U, false><<<grid, 512, 0, s>>>(p);
+        fp8_stream_kernel<NC, 8, U, false><<<grid, 512, 0, s>>>(p);
 }
-static void launch_stream(const Fp8Args& p, int rf, int nc, dim3 grid, hipStream_t s) {
+template <int NC, int KS, int D>
+static void launch_ring_(const Fp8Args& p, dim3 grid, hipStream_t s) {
+    if (p.out_f32)
+        fp8_ring_kernel<NC, KS, D, true><<<grid, KS * kWave, 0, s>>>(p);
+    else
+        fp8_ring_kernel<NC, KS, D, false><<<grid, KS * kWave, 0, s>>>(p);
+}
+static void launch_few_rows(const Fp8Args& p, int rf, int nc, dim3 grid, hipStream_t s) {
     switch (rf * 16 + nc) {
-        case 17: launch_stream_<1, 1>(p, grid, s); break;
-        case 18: launch_stream_<1, 2>(p, grid, s); break;
-        case 19: launch_stream_<1, 3>(p, grid, s); break;
-        case 20: launch_stream_<1, 4>(p, grid, s); break;
-        case 22: launch_stream_<1, 6>(p, grid, s); break;
-        case 24: launch_stream_<1, 8>(p, grid, s); break;
-        case 33: launch_stream_<2, 1>(p, grid, s); break;
-        case 34: launch_stream_<2, 2>(p, grid, s); break;
-        case 35: launch_stream_<2, 3>(p, grid, s); break;
-        default: launch_stream_<2, 4>(p, grid, s);
+        case 17: launch_stream_<1>(p, grid, s); break;
+        case 18: launch_stream_<2>(p, grid, s); break;
+        case 19: launch_stream_<3>(p, grid, s); break;
+        case 20: launch_stream_<4>(p, grid, s); break;
+        case 22: launch_stream_<6>(p, grid, s); break;
+        case 23: launch_stream_<7>(p, grid, s); break;
+        case 24: launch_stream_<8>(p, grid, s); break;
+        case 33: launch_ring_<1, 8, 3>(p, grid, s); break;
+        case 34: launch_ring_<2, 8, 2>(p, grid, s); break;
+        case 35: launch_ring_<3, 4, 3>(p, grid, s); break;
+        case 36: launch_ring_<4, 4, 3>(p, grid, s); break;
+        case 38: launch_ring_<6, 4, 2>(p, grid, s); break;
+        default: launch_ring_<7, 4, 2>(p, grid, s);
     }
 }
 
@@ -686,7 +773,7 @@ hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed,
         launch_tile(p, plan.tile, dim3((unsigned)(tiles * plan.splits)), s);
     } else {
         const int64_t rows = (M + plan.rf * 16 - 1) / (plan.rf * 16);
-        launch_stream(p, plan.rf, plan.nc, dim3((unsigned)(rows * ((l.blocks + plan.nc - 1) / plan.nc))), s);
+        launch_few_rows(p, plan.rf, plan.nc, dim3((unsigned)(rows * ((l.blocks + plan.nc - 1) / plan.nc))), s);
     }
     if (plan.splits > 1) fp8_join_kernel<<<dim3((unsigned)((M * (N / 8) + 255) / 256)), 256, 0, s>>>(p);
     return hipGetLastError();
