@@ -793,7 +793,7 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
     if (!bytes_of(T, stride, (int64_t)esize(dtype), &lb) || !bytes_of(T, std::max<int64_t>(n, 1), 4, &nb))
         return DN_ERR_INVALID_ARG;
     lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
-    const int64_t segments = dn::plan_logprobs(T, V).segments;
+    const int64_t segments = dn::plan_logprobs(T, V, top).segments;
     if (T * segments > kMaxGridX) return DN_ERR_UNSUPPORTED;
     if (!aligned(logits, esize(dtype)) || !aligned(targets, 16) || !aligned(logprobs, 16) || !aligned(entropy, 16) ||
         !aligned(top_logprobs, 16) || !aligned(top_ids, 16) || !aligned(workspace, 256))

@@ -112,21 +112,22 @@ inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
 // ------------------------------------------------------------------------------- log probabilities
 constexpr int64_t kMaxTop = 64, kMaxSegments = 16;
 
-// Threads to a workgroup and workgroups to a row.  Rows that fill the chip take 256 threads each; fewer rows 512, and
-// a workgroup to each 16384 tokens while there is about one to a CU (then a second kernel joins them).  Measured, us, bf16
+// Threads to a workgroup and workgroups to a row.  Rows that fill the chip take 256 threads each if they are ranked, else
+// 512 (4000 x 32008 fp32 without ranks 87 us, 256 threads 91; with 20 alternatives 137 and 108).  Fewer rows take 512, and
+// a workgroup to each 16384 tokens while there is about one to a CU; a second kernel then joins them.  Measured, us, bf16
 // with 20 alternatives: 32 x 131072 17.2 (8 segments; 16: 18.7, 4: 21.0), 1 x 32000 12.4 (2; 1: 13.6), 200 x 32000 16.8
 // (1; 2: 19.0); 1 x 8192 7.7 (256 threads 8.8, 1024 8.1).
 struct LogprobPlan {
     int threads;
     int64_t segments;
 };
-inline LogprobPlan plan_logprobs(int64_t T, int64_t V) {
-    if (T >= 256) return LogprobPlan{256, 1};
+inline LogprobPlan plan_logprobs(int64_t T, int64_t V, int64_t top) {
+    if (T >= 256) return LogprobPlan{top ? 256 : 512, 1};
     return LogprobPlan{512, std::max<int64_t>(1, std::min({256 / T, (V + 8192) / 16384, kMaxSegments}))};
 }
 // A segment leaves its maximum, denominator and entropy sum (16 bytes) and `top` ranked keys of 8 bytes.
 inline size_t logprob_workspace(int64_t T, int64_t V, int64_t top) {
-    const int64_t s = plan_logprobs(T, V).segments;
+    const int64_t s = plan_logprobs(T, V, top).segments;
     return s > 1 ? (size_t)T * s * (16 + 8 * top) : 0;
 }
 

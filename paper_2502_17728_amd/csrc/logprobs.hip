@@ -338,7 +338,7 @@ __device__ __forceinline__ void load8(const T* x, int64_t at, int64_t V, float* 
 template <>
 __device__ __forceinline__ void load8<__bf16>(const __bf16* x, int64_t at, int64_t V, float* f) {
     if (at >= 0 && at + 8 <= V) {
-        const u32x4 w = ld16_stream(x + at);
+        const u32x4 w = ld16(x + at);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f[2 * e] = bf_lo(w[e]);
@@ -352,7 +352,7 @@ __device__ __forceinline__ void load8<__bf16>(const __bf16* x, int64_t at, int64
 template <>
 __device__ __forceinline__ void load8<float>(const float* x, int64_t at, int64_t V, float* f) {
     if (at >= 0 && at + 8 <= V) {
-        const u32x4 a = ld16_stream(x + at), b = ld16_stream(x + at + 4);
+        const u32x4 a = ld16(x + at), b = ld16(x + at + 4);
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f[e] = __uint_as_float(a[e]);
@@ -362,6 +362,16 @@ __device__ __forceinline__ void load8<float>(const float* x, int64_t at, int64_t
 #pragma unroll
         for (int e = 0; e < 8; ++e) f[e] = at + e >= 0 && at + e < V ? x[at + e] : -__builtin_inff();
     }
+}
+
+// The largest of 8 values by three-operand instructions (fmaxf would first quiet each operand); a NaN is no maximum.
+__device__ __forceinline__ float max8(const float* f) {
+    float a, b, c, d;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(f[0]), "v"(f[1]), "v"(f[2]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(f[3]), "v"(f[4]), "v"(f[5]));
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(c) : "v"(a), "v"(f[6]), "v"(f[7]));
+    asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(b), "v"(c));
+    return d;
 }
 
 // A workgroup of NT threads takes a row, or one of its segments; loads run one step of 8 NT tokens ahead.
@@ -389,14 +399,14 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
     int v0 = seg * per + wave * kWave;
     Given given{-1, 0.f};
     if (wave == 0 && p.segments == 1 && p.n) given.load(p, row, x, lane);
-    float f[8], g[8];
     bool first = true;
-    if (v0 < end) load8<T>(x, (int64_t)(v0 + lane) * 8 - shift, v0 + lane < end ? V : 0, f);
-    for (; v0 < end; v0 += NT) {
+    auto load = [&](int from, float* f) {
+        const int v = from + lane;
+        if (from < end) load8<T>(x, (int64_t)v * 8 - shift, v < end ? V : 0, f);  // past the segment: nothing
+    };
+    auto take = [&](const float* f) {
         const int v = v0 + lane;
-        if (v0 + NT < end) load8<T>(x, (int64_t)(v + NT) * 8 - shift, v + NT < end ? V : 0, g);
-        const float most = __builtin_fmaxf(__builtin_fmaxf(__builtin_fmaxf(f[0], f[1]), __builtin_fmaxf(f[2], f[3])),
-                                           __builtin_fmaxf(__builtin_fmaxf(f[4], f[5]), __builtin_fmaxf(f[6], f[7])));
+        const float most = max8(f);
         if (__any(most > a.m)) raise(a, __builtin_fmaxf(a.m, most), c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
@@ -409,8 +419,16 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
             first = false;
             ranked.add(f, most, v < end, v * 8 - shift, V, lane);  // v * 8 - shift < 2^31: V is
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = g[e];
+        v0 += NT;
+    };
+    float f[8], g[8];
+    load(v0, f);
+    while (v0 < end) {
+        load(v0 + NT, g);
+        take(f);
+        if (v0 >= end) break;
+        load(v0 + NT, f);
+        take(g);
     }
     a = wave_join(a, c);
     if (TOP && ranked.groups) ranked.flush(V, lane);
@@ -486,7 +504,7 @@ static void launch_logprobs(const LpArgs& p, int threads, hipStream_t s) {
 hipError_t launch_token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,
                                  const int32_t* targets, int64_t n, int64_t top, float* logprobs, float* entropy,
                                  float* top_logprobs, int32_t* top_ids, void* workspace, hipStream_t s) {
-    const LogprobPlan plan = plan_logprobs(T, V);
+    const LogprobPlan plan = plan_logprobs(T, V, top);
     float* sums = reinterpret_cast<float*>(workspace);
     const LpArgs p{logits, stride, T, V, n, scale, (int)top, (int)plan.segments, targets, logprobs, entropy, top_logprobs,
                    top_ids, sums, reinterpret_cast<unsigned long long*>(sums + (plan.segments > 1 ? T * plan.segments * 4 : 0))};

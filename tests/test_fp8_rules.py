@@ -150,7 +150,7 @@ void plan(int64_t M, int64_t K, int64_t blocks, int gated, int f32, int64_t fit,
 }
 uint64_t space(int64_t M, int64_t K, int64_t blocks, int gated) { return fp8_workspace(M, K, blocks, gated); }
 void rows(int64_t M, int64_t K, int64_t* out) { const RowPlan p = plan_rows(M, K); out[0] = p.threads; out[1] = p.pieces; }
-void lp(int64_t T, int64_t V, int64_t* out) { const LogprobPlan p = plan_logprobs(T, V); out[0] = p.threads; out[1] = p.segments; }
+void lp(int64_t T, int64_t V, int64_t top, int64_t* out) { const LogprobPlan p = plan_logprobs(T, V, top); out[0] = p.threads; out[1] = p.segments; }
 }
 """
 
@@ -200,7 +200,7 @@ def test_row_plans_hold_the_row():
 
 
 def test_logprob_plans():
-    for T, V in itertools.product(SIZES, (1, 8, 1000, 8192, 32000, 50257, 131072, 1 << 20, (1 << 30) - 1)):
-        threads, segments = call("lp", T, V, n=2)
+    for T, V, top in itertools.product(SIZES, (1, 8, 1000, 8192, 32000, 50257, 131072, 1 << 20, (1 << 30) - 1), (0, 1, 64)):
+        threads, segments = call("lp", T, V, top, n=2)
         assert threads in (256, 512) and 1 <= segments <= 16
         assert segments == 1 or (V + 14) // 8 >= segments  # every segment but the last has tokens
