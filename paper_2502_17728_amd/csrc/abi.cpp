@@ -659,7 +659,8 @@ static dn_status rows_call(const void* x, const void* residual, const void* gamm
     size_t xb, yb;
     if (!bytes_of(M, K, (int64_t)esize(dtype), &xb) || !bytes_of(M, K, fp8 ? 1 : (int64_t)esize(dtype), &yb))
         return DN_ERR_INVALID_ARG;
-    if (K % (fp8 ? 16 : 8) || K > (dtype == DN_F32 ? dn::kMaxRowF32 : dn::kMaxRowBf16) || M > kMaxGridX)
+    if (K % (fp8 ? 16 : 8) || K > (dtype == DN_F32 ? dn::kMaxRowF32 : dn::kMaxRowBf16) ||
+        M > (kMaxThreads - 255) / dn::plan_rows(M, K).threads)
         return DN_ERR_UNSUPPORTED;
     if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(gamma, 16) || !aligned(sum, 16) || !aligned(y, 16) ||
         !aligned(scales, 16))
@@ -752,21 +753,24 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
     if (!fp8_rows_valid(M, w)) return DN_ERR_INVALID_ARG;
     const int64_t K = w->K, N = w->N;
     const dn::Fp8Layout l = dn::fp8_layout(K, N, w->gated);
-    if ((M + 15) / 16 * l.blocks > kMaxGridX || (M * (N / 8) + 255) / 256 > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    const size_t part = dn::fp8_partial_bytes(M, l.blocks);
+    const int64_t fit = workspace ? std::max<int64_t>(1, (int64_t)std::min<size_t>(workspace_bytes / part, dn::kMaxSplits)) : 1;
+    const dn::Fp8Plan plan = dn::plan_fp8(M, K, l.blocks, w->gated, out_dtype == DN_F32, fit);
+    if (dn::fp8_workgroups(plan, M, l.blocks) > kMaxThreads / dn::fp8_threads(plan) ||
+        (plan.splits > 1 && M > (kMaxThreads - 255) / (N / 8)))
+        return DN_ERR_UNSUPPORTED;
     if (!aligned(x, 16) || !aligned(x_scales, 16) || !aligned(residual, 16) || !aligned(out, 16) ||
         !aligned(w->packed, 256) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;
-    const size_t part = dn::fp8_partial_bytes(M, l.blocks);
-    const int64_t fit = workspace ? std::max<int64_t>(1, (int64_t)std::min<size_t>(workspace_bytes / part, dn::kMaxSplits)) : 1;
-    const size_t used = fit > 1 ? std::min(workspace_bytes, dn::fp8_workspace(M, K, l.blocks, w->gated)) : 0;
+    const size_t used = plan.splits > 1 ? plan.splits * part : 0;
     const size_t ob = (size_t)M * N * esize(out_dtype);
     const Range in[4] = {{x, (size_t)M * K}, {x_scales, (size_t)M * 4}, {w->packed, l.total}, {residual, ob}};
     const Range out_r{out, ob}, scratch{workspace, used};
     if (any_overlap(out_r, in, 3) || any_overlap(scratch, in, 4) || any_overlap(scratch, &out_r, 1) ||
         (residual != out && any_overlap(out_r, in + 3, 1)))
         return DN_ERR_INVALID_ARG;
-    return from_hip(dn::launch_linear_fp8(x, x_scales, w->packed, M, K, N, w->gated, activation, residual, out_dtype,
-                                          workspace, fit, out, stream));
+    return from_hip(dn::launch_linear_fp8(x, x_scales, w->packed, M, K, N, w->gated, activation, residual, out_dtype, plan,
+                                          workspace, out, stream));
 }
 
 // ------------------------------------------------------------------------------- log probabilities
@@ -793,8 +797,8 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
     if (!bytes_of(T, stride, (int64_t)esize(dtype), &lb) || !bytes_of(T, std::max<int64_t>(n, 1), 4, &nb))
         return DN_ERR_INVALID_ARG;
     lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
-    const int64_t segments = dn::plan_logprobs(T, V, top).segments;
-    if (T * segments > kMaxGridX) return DN_ERR_UNSUPPORTED;
+    const dn::LogprobPlan plan = dn::plan_logprobs(T, V, top);
+    if (T > kMaxThreads / (plan.segments * plan.threads)) return DN_ERR_UNSUPPORTED;
     if (!aligned(logits, esize(dtype)) || !aligned(targets, 16) || !aligned(logprobs, 16) || !aligned(entropy, 16) ||
         !aligned(top_logprobs, 16) || !aligned(top_ids, 16) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;

@@ -9,6 +9,8 @@
 
 namespace dn {
 
+struct Fp8Plan;  // fp8_rules.hpp
+
 // Byte offsets of the pieces of a prepared LN->Linear weight buffer.
 struct PackedLayout {
     int64_t kchunks, nblocks;  // K_pad / kchunk, N_pad / 16
@@ -165,8 +167,8 @@ hipError_t launch_linear_fp8_prepare(const void* W, const float* scales, const v
                                      const void* W_up, const float* up_scales, const float* up_bias, int64_t K, int64_t N,
                                      int dtype, void* packed, hipStream_t s);
 hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed, int64_t M, int64_t K, int64_t N, int gated,
-                             int act, const void* residual, int out_dtype, void* workspace, int64_t splits_that_fit,
-                             void* out, hipStream_t s);
+                             int act, const void* residual, int out_dtype, const Fp8Plan& plan, void* workspace, void* out,
+                             hipStream_t s);
 
 // Log probabilities, entropy and ranks of T rows.
 hipError_t launch_token_logprobs(const void* logits, int64_t stride, int64_t T, int64_t V, int dtype, float scale,

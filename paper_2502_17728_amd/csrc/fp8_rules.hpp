@@ -53,11 +53,14 @@ inline Fp8Layout fp8_layout(int64_t K, int64_t N, int gated) {
 // the join costs a launch and the traffic of the fp32 sums.
 constexpr int kFp8Tiles = 5;
 struct Fp8Tile {
-    int bm, bn, per_cu;
+    int bm, bn, threads, per_cu;
     double stage_us, pair_us;  // one workgroup on a CU, all of per_cu
 };
-constexpr Fp8Tile kFp8Tile[kFp8Tiles] = {{64, 64, 2, 0.235, 0.36},  {64, 128, 1, 0.315, 0.315}, {128, 128, 1, 0.46, 0.46},
-                                         {256, 128, 1, 0.80, 0.80}, {256, 256, 1, 1.42, 1.42}};
+constexpr Fp8Tile kFp8Tile[kFp8Tiles] = {{64, 64, 128, 2, 0.235, 0.36},
+                                         {64, 128, 256, 1, 0.315, 0.315},
+                                         {128, 128, 256, 1, 0.46, 0.46},
+                                         {256, 128, 512, 1, 0.80, 0.80},
+                                         {256, 256, 512, 1, 1.42, 1.42}};
 constexpr int64_t kMaxSplits = 16;
 
 // tile >= 0: that tile, K in `splits` parts.  tile < 0: streamed (rf 1) or ring (rf 2) kernel, 16 rf rows x nc column blocks.
@@ -104,6 +107,16 @@ inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32
     }
     return best;
 }
+// Workgroups of the call, and threads to each.
+inline int64_t fp8_workgroups(const Fp8Plan& p, int64_t M, int64_t blocks) {
+    if (p.tile < 0) return (M + 16 * p.rf - 1) / (16 * p.rf) * ((blocks + p.nc - 1) / p.nc);
+    const Fp8Tile& t = kFp8Tile[p.tile];
+    return (M + t.bm - 1) / t.bm * ((blocks * 16 + t.bn - 1) / t.bn) * p.splits;
+}
+inline int fp8_threads(const Fp8Plan& p) {
+    return p.tile >= 0 ? kFp8Tile[p.tile].threads : p.rf == 2 && p.nc > 2 ? 256 : 512;
+}
+
 inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
     const int64_t splits = std::max(plan_fp8(M, K, blocks, gated, 0, kMaxSplits).splits, plan_fp8(M, K, blocks, gated, 1, kMaxSplits).splits);
     return splits > 1 ? splits * fp8_partial_bytes(M, blocks) : 0;

@@ -706,75 +706,58 @@ hipError_t launch_linear_fp8_prepare(const void* W, const float* scales, const v
 }
 
 template <bool GATED, bool F32>
-static void launch_tile_(const Fp8Args& p, int tile, dim3 grid, hipStream_t s) {
+static void launch_tile(const Fp8Args& p, int tile, dim3 grid, dim3 threads, hipStream_t s) {
     switch (tile) {
-        case 0: fp8_tile_kernel<64, 64, 2, 1, 4, GATED, F32><<<grid, 128, 0, s>>>(p); break;
-        case 1: fp8_tile_kernel<64, 128, 2, 2, 4, GATED, F32><<<grid, 256, 0, s>>>(p); break;
-        case 2: fp8_tile_kernel<128, 128, 2, 2, 4, GATED, F32><<<grid, 256, 0, s>>>(p); break;
-        case 3: fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32><<<grid, 512, 0, s>>>(p); break;
+        case 0: fp8_tile_kernel<64, 64, 2, 1, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
+        case 1: fp8_tile_kernel<64, 128, 2, 2, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
+        case 2: fp8_tile_kernel<128, 128, 2, 2, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
+        case 3: fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32><<<grid, threads, 0, s>>>(p); break;
         default:
-            if constexpr (!F32) fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32><<<grid, 512, 0, s>>>(p);
+            if constexpr (!F32) fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32><<<grid, threads, 0, s>>>(p);
     }
 }
-static void launch_tile(const Fp8Args& p, int tile, dim3 grid, hipStream_t s) {
-    if (p.gated)
-        p.out_f32 ? launch_tile_<true, true>(p, tile, grid, s) : launch_tile_<true, false>(p, tile, grid, s);
-    else
-        p.out_f32 ? launch_tile_<false, true>(p, tile, grid, s) : launch_tile_<false, false>(p, tile, grid, s);
-}
 
-template <int NC>
-static void launch_stream_(const Fp8Args& p, dim3 grid, hipStream_t s) {
-    constexpr int U = NC <= 2 ? 2 : 1;  // 2 steps' loads at a time while W's bytes in flight are few
-    if (p.out_f32)
-        fp8_stream_kernel<NC, 8, U, true><<<grid, 512, 0, s>>>(p);
-    else
-        fp8_stream_kernel<NC, 8, U, false><<<grid, 512, 0, s>>>(p);
-}
-template <int NC, int KS, int D>
-static void launch_ring_(const Fp8Args& p, dim3 grid, hipStream_t s) {
-    if (p.out_f32)
-        fp8_ring_kernel<NC, KS, D, true><<<grid, KS * kWave, 0, s>>>(p);
-    else
-        fp8_ring_kernel<NC, KS, D, false><<<grid, KS * kWave, 0, s>>>(p);
-}
-static void launch_few_rows(const Fp8Args& p, int rf, int nc, dim3 grid, hipStream_t s) {
-    switch (rf * 16 + nc) {
-        case 17: launch_stream_<1>(p, grid, s); break;
-        case 18: launch_stream_<2>(p, grid, s); break;
-        case 19: launch_stream_<3>(p, grid, s); break;
-        case 20: launch_stream_<4>(p, grid, s); break;
-        case 22: launch_stream_<6>(p, grid, s); break;
-        case 23: launch_stream_<7>(p, grid, s); break;
-        case 24: launch_stream_<8>(p, grid, s); break;
-        case 33: launch_ring_<1, 8, 3>(p, grid, s); break;
-        case 34: launch_ring_<2, 8, 2>(p, grid, s); break;
-        case 35: launch_ring_<3, 4, 3>(p, grid, s); break;
-        case 36: launch_ring_<4, 4, 3>(p, grid, s); break;
-        case 38: launch_ring_<6, 4, 2>(p, grid, s); break;
-        default: launch_ring_<7, 4, 2>(p, grid, s);
+template <bool F32>
+static void launch_few_rows(const Fp8Args& p, int rf, int nc, dim3 grid, dim3 threads, hipStream_t s) {
+    if (rf == 1) {
+        switch (nc) {  // 2 steps' loads at a time while W's bytes in flight are few
+            case 1: fp8_stream_kernel<1, 8, 2, F32><<<grid, threads, 0, s>>>(p); break;
+            case 2: fp8_stream_kernel<2, 8, 2, F32><<<grid, threads, 0, s>>>(p); break;
+            case 3: fp8_stream_kernel<3, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
+            case 4: fp8_stream_kernel<4, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
+            case 6: fp8_stream_kernel<6, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
+            case 7: fp8_stream_kernel<7, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
+            default: fp8_stream_kernel<8, 8, 1, F32><<<grid, threads, 0, s>>>(p);
+        }
+    } else {
+        switch (nc) {
+            case 1: fp8_ring_kernel<1, 8, 3, F32><<<grid, threads, 0, s>>>(p); break;
+            case 2: fp8_ring_kernel<2, 8, 2, F32><<<grid, threads, 0, s>>>(p); break;
+            case 3: fp8_ring_kernel<3, 4, 3, F32><<<grid, threads, 0, s>>>(p); break;
+            case 4: fp8_ring_kernel<4, 4, 3, F32><<<grid, threads, 0, s>>>(p); break;
+            case 6: fp8_ring_kernel<6, 4, 2, F32><<<grid, threads, 0, s>>>(p); break;
+            default: fp8_ring_kernel<7, 4, 2, F32><<<grid, threads, 0, s>>>(p);
+        }
     }
 }
 
 hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed, int64_t M, int64_t K, int64_t N, int gated,
-                             int act, const void* residual, int out_dtype, void* workspace, int64_t splits_that_fit,
-                             void* out, hipStream_t s) {
+                             int act, const void* residual, int out_dtype, const Fp8Plan& plan, void* workspace, void* out,
+                             hipStream_t s) {
     const Fp8Layout l = fp8_layout(K, N, gated);
     const char* base = reinterpret_cast<const char*>(packed);
-    const int f32 = out_dtype == 0;
-    const Fp8Plan plan = plan_fp8(M, K, l.blocks, gated, f32, splits_that_fit);
+    const bool f32 = out_dtype == 0;
     const Fp8Args p{reinterpret_cast<const char*>(x), xs, base, reinterpret_cast<const float*>(base + l.scales),
                     reinterpret_cast<const float*>(base + l.bias), residual, out,
                     plan.splits > 1 ? reinterpret_cast<float*>(workspace) : nullptr, M, K, N, l.kchunks, l.blocks, act, gated,
                     f32, (int)plan.splits};
-    if (plan.tile >= 0) {
-        const Fp8Tile& t = kFp8Tile[plan.tile];
-        const int64_t tiles = (M + t.bm - 1) / t.bm * ((l.blocks * 16 + t.bn - 1) / t.bn);
-        launch_tile(p, plan.tile, dim3((unsigned)(tiles * plan.splits)), s);
-    } else {
-        const int64_t rows = (M + plan.rf * 16 - 1) / (plan.rf * 16);
-        launch_few_rows(p, plan.rf, plan.nc, dim3((unsigned)(rows * ((l.blocks + plan.nc - 1) / plan.nc))), s);
-    }
+    const dim3 grid((unsigned)fp8_workgroups(plan, M, l.blocks)), threads((unsigned)fp8_threads(plan));
+    if (plan.tile < 0)
+        f32 ? launch_few_rows<true>(p, plan.rf, plan.nc, grid, threads, s) : launch_few_rows<false>(p, plan.rf, plan.nc, grid, threads, s);
+    else if (gated)
+        f32 ? launch_tile<true, true>(p, plan.tile, grid, threads, s) : launch_tile<true, false>(p, plan.tile, grid, threads, s);
+    else
+        f32 ? launch_tile<false, true>(p, plan.tile, grid, threads, s) : launch_tile<false, false>(p, plan.tile, grid, threads, s);
     if (plan.splits > 1) fp8_join_kernel<<<dim3((unsigned)((M * (N / 8) + 255) / 256)), 256, 0, s>>>(p);
     return hipGetLastError();
 }

@@ -36,7 +36,7 @@ def test_rows_refusals():
         for bad in (dict(x=None), dict(y=None), dict(M=0), dict(K=0), dict(eps=-1.0), dict(eps=NAN), dict(eps=INF), dict(dt=2),
                     dict(res=None), dict(sm=None), dict(M=1 << 62)):
             assert f(**bad) == INVALID, bad
-        for bad in (dict(K=60), dict(K=65544 if f is norm else 65552), dict(K=32784, dt=0), dict(M=1 << 31)):
+        for bad in (dict(K=60), dict(K=65544 if f is norm else 65552), dict(K=32784, dt=0), dict(M=1 << 31)):  # (too many threads)
             assert f(**bad) == UNSUPPORTED, bad
         for name in ("x", "res", "gamma", "sm", "y"):
             assert f(**{name: P[9] + 8}) == MISALIGNED, name
@@ -131,6 +131,21 @@ def test_logprobs_refusals():
     assert f(0, 10, 0) == f(1, 0, 0) == f(1, 10, 11) == f(1, 100, 65) == f(4096, 8192, 5) == f(1, 8192, 5) == 0
 
 
+def test_launches_past_the_devices_limit_are_refused():
+    """2^32 threads and more in one launch, where the device would refuse it; one row less is past validation."""
+    far = [0x7F0000000000 + (i << 46) for i in range(10)]
+    # 256 threads to a row of 4096, 64 to one of 512
+    for K, most in ((4096, (1 << 24) - 1), (512, (1 << 26) - 4)):
+        assert lib.rows_fp8(far[0], most + 1 + 4 * (K == 512), K, 1, far[1], far[2], None) == UNSUPPORTED
+        assert lib.rows_fp8(far[0] + 2, most, K, 1, far[1], far[2], None) == MISALIGNED
+    w = weights(K=16, N=8)
+    # 256 x 256 or 256 x 128 tiles of 512 threads, one column of them
+    f = lambda M, x=far[0]: lib.linear_fp8(x, far[1], ctypes.byref(w), M, 0, None, 1, None, 0, far[2], None)
+    assert f(1 << 32) == UNSUPPORTED
+    f = lambda T, x=far[0]: lib.token_logprobs(x, 8, T, 8, 1, 1.0, None, 0, 0, None, far[1], None, None, None, 0, None)
+    assert f(1 << 23) == UNSUPPORTED and f((1 << 23) - 1, far[0] + 1) == MISALIGNED
+
+
 def test_binding_refuses_cpu_tensors():
     x = torch.zeros((2, 64), dtype=torch.bfloat16)
     for f in (lambda: ops.residual_rmsnorm(x), lambda: ops.residual_rmsnorm_fp8(x), lambda: ops.rows_fp8(x),
@@ -147,6 +162,7 @@ extern "C" {
 void plan(int64_t M, int64_t K, int64_t blocks, int gated, int f32, int64_t fit, int64_t* out) {
     const Fp8Plan p = plan_fp8(M, K, blocks, gated, f32, fit);
     out[0] = p.tile; out[1] = p.rf; out[2] = p.nc; out[3] = p.splits;
+    out[4] = fp8_workgroups(p, M, blocks); out[5] = fp8_threads(p);
 }
 uint64_t space(int64_t M, int64_t K, int64_t blocks, int gated) { return fp8_workspace(M, K, blocks, gated); }
 void rows(int64_t M, int64_t K, int64_t* out) { const RowPlan p = plan_rows(M, K); out[0] = p.threads; out[1] = p.pieces; }
@@ -182,15 +198,18 @@ def test_product_plans_are_ones_that_exist(gated, f32):
         blocks = (N + 15) // 16 * (1 + gated)
         space = rules().space(ctypes.c_int64(M), ctypes.c_int64(K), ctypes.c_int64(blocks), gated)
         for fit in (1, 2, 3, 5, 16):
-            tile, rf, nc, splits = call("plan", M, K, blocks, gated, f32, fit, n=4)
+            tile, rf, nc, splits, wgs, threads = call("plan", M, K, blocks, gated, f32, fit, n=6)
             if tile < 0:
                 assert M <= 64 and splits == 1 and (rf, nc) in [(1, c) for c in (1, 2, 3, 4, 6, 7, 8)] + [(2, c) for c in (1, 2, 3, 4, 6, 7)]
                 assert not gated or nc % 2 == 0
+                assert wgs == -(-M // (16 * rf)) * -(-blocks // nc) and threads == (256 if rf == 2 and nc > 2 else 512)
             else:
                 assert 0 <= tile <= (3 if f32 else 4) and M > 16
                 # every split has a stage, and its sums fit what the caller was asked for
                 assert 1 <= splits <= min(fit, 16) and splits <= (K + 127) // 128
                 assert splits == 1 or splits * M * blocks * 64 <= space
+                bm, bn, t = [(64, 64, 128), (64, 128, 256), (128, 128, 256), (256, 128, 512), (256, 256, 512)][tile]
+                assert threads == t and wgs == -(-M // bm) * -(-blocks * 16 // bn) * splits
 
 
 def test_row_plans_hold_the_row():
