@@ -42,8 +42,8 @@ inline Fp8Layout fp8_layout(int64_t K, int64_t N, int gated) {
 // Which kernel takes a call, by estimated time: rounds of workgroups (256 CUs, `per_cu` of them on each), each a
 // fixed 1.5 us (first copies, epilogue) and its stages of 128 codes at `stage_us`; never less than W from HBM at 6.2 TB/s.
 // Stage times were fitted to calls of one round, us: 64 x 64 tiles 0.235 (two on a CU 0.36 the pair), 64 x 128 0.315,
-// 128 x 128 0.46, 256 x 128 0.80, 256 x 256 1.42.  Measured, us, best first:
-//   64 rows 4096 -> 12288    64 x 64 11.4, 64 x 128 12.9, streamed 14.9, 128 x 128 17
+// 128 x 128 0.46, 256 x 128 0.84, 256 x 256 1.42.  Measured, us, best first:
+//   64 rows 4096 -> 12288    64 x 64 11.4, 64 x 128 12.9, 128 x 128 17
 //   128 rows 4096 -> 12288   64 x 128 13.2, 64 x 64 14.3, 128 x 128 16.9
 //   256 rows 4096 -> 12288   128 x 128 18.2, 64 x 128 24.3
 //   512 rows 4096 -> 12288   256 x 128 28.8, 128 x 128 35.5, 256 x 256 42.4
@@ -59,7 +59,7 @@ struct Fp8Tile {
 constexpr Fp8Tile kFp8Tile[kFp8Tiles] = {{64, 64, 128, 2, 0.235, 0.36},
                                          {64, 128, 256, 1, 0.315, 0.315},
                                          {128, 128, 256, 1, 0.46, 0.46},
-                                         {256, 128, 512, 1, 0.80, 0.80},
+                                         {256, 128, 512, 1, 0.84, 0.84},
                                          {256, 256, 512, 1, 1.42, 1.42}};
 constexpr int64_t kMaxSplits = 16;
 
@@ -87,7 +87,7 @@ inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32
             if ((gated && nc % 2) || (rf == 2 && nc == 8)) continue;
             const int64_t wgs = rows * ((blocks + nc - 1) / nc);
             const double step = rf == 1 ? 0.02 + 0.072 * nc : 0.045 + 0.068 * nc;
-            const double us = 2.7 + std::max(w_us, (double)((wgs + 255) / 256) * (double)stages * step * slow);
+            const double us = 2.7 + std::max(w_us, (double)((wgs + 255) / 256) * (double)stages * step * (f32 ? 1.15 : 1.0));
             if (best.rf == 0 || us < best.us) best = Fp8Plan{-1, rf, nc, 1, us};
         }
     }
@@ -101,7 +101,7 @@ inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32
             const double stage = (wgs <= 256 ? t.stage_us : t.pair_us) * slow;
             const int64_t each = (stages + splits - 1) / splits;
             double us = 3.0 + std::max(w_us, (double)((wgs + per_round - 1) / per_round) * (1.5 + (double)each * stage));
-            if (splits > 1) us += 2.5 + (double)splits * (double)fp8_partial_bytes(M, blocks) * 2.0 / 6e6;
+            if (splits > 1) us += 3.5 + (double)splits * (double)fp8_partial_bytes(M, blocks) * 2.0 / 6e6;
             if (best.us == 0 || us < best.us) best = Fp8Plan{i, 0, 0, splits, us};
         }
     }
