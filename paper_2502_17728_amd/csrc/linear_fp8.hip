@@ -139,14 +139,24 @@ struct Residual8 {
         }
     }
 };
+// STREAM: with the non-temporal hint.  The large tiles' outputs then reach HBM beside the products that follow, instead of
+// being written back when these need the cache: 4096 x 4096 -> 12288 174 -> 169 us.
+template <bool STREAM = false>
+__device__ __forceinline__ void store16(void* to, const u32x4& v) {
+    if constexpr (STREAM)
+        __builtin_nontemporal_store(v, reinterpret_cast<u32x4*>(to));
+    else
+        *reinterpret_cast<u32x4*>(to) = v;
+}
+template <bool STREAM = false>
 __device__ __forceinline__ void store8(const Fp8Args& p, int64_t at, const float* v) {
     if (p.out_f32) {
         float* o = reinterpret_cast<float*>(p.out) + at;
-        *reinterpret_cast<f32x4*>(o) = f32x4{v[0], v[1], v[2], v[3]};
-        *reinterpret_cast<f32x4*>(o + 4) = f32x4{v[4], v[5], v[6], v[7]};
+        store16<STREAM>(o, u32x4{__float_as_uint(v[0]), __float_as_uint(v[1]), __float_as_uint(v[2]), __float_as_uint(v[3])});
+        store16<STREAM>(o + 4, u32x4{__float_as_uint(v[4]), __float_as_uint(v[5]), __float_as_uint(v[6]), __float_as_uint(v[7])});
     } else {
-        *reinterpret_cast<u32x4*>(reinterpret_cast<__bf16*>(p.out) + at) =
-            u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]), pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])};
+        store16<STREAM>(reinterpret_cast<__bf16*>(p.out) + at, u32x4{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]),
+                                                                     pack_bf16(v[4], v[5]), pack_bf16(v[6], v[7])});
     }
 }
 
@@ -592,7 +602,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void fp8_tile_kernel(Fp8Args p) {
                     for (int e = 0; e < 8; ++e) v[e] *= ku.z(e < 4 ? u0[e & 3] : u1[e & 3], sx, e);
                 }
                 if (p.residual) res[it].add(p, v);
-                if (row < p.M && n < p.N) store8(p, row * p.N + n, v);
+                if (row < p.M && n < p.N) store8<(BM >= 256)>(p, row * p.N + n, v);
             }
             lds_in_order();
         });
