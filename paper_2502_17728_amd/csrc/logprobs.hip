@@ -486,8 +486,12 @@ __global__ __launch_bounds__(kWave) void logprobs_join_kernel(LpArgs p) {
     }
     lds_in_order();
     a = wave_join(a, p.scale * kLog2eF);
-    const unsigned long long key =
-        p.top ? top_of((DN_LDS unsigned long long*)pool, total, p.top, 1, (DN_LDS WaveRanks*)&ranks, lane) : 0;
+    unsigned long long key = 0;
+    if (p.top) {
+        // a segment's last key has `top` keys at or above it (0 where a segment has fewer)
+        const uint32_t last = lane < p.segments ? (uint32_t)(pool[lane * p.top + p.top - 1] >> 32) : 0, most = wave_max(last);
+        key = top_of((DN_LDS unsigned long long*)pool, total, p.top, most > 1 ? most : 1, (DN_LDS WaveRanks*)&ranks, lane);
+    }
     finish<T>(p, row, x, a, key, given, lane);
 }
 

@@ -1137,15 +1137,18 @@ def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None,
             raise ValueError(f"targets has shape {list(targets.shape)}, expected [T, n]")
         n = targets.shape[1]
         tp = _int32(targets, "targets", (T, n), logits)
-        if n:
-            given, lp = _made(logits, None, "", (T, n), torch.float32, dev, stream)
-        else:
+        if n == 0:
             tp = None
+    new = logits.new_empty if stream is None else lambda shape, dtype: _empty(logits, shape, stream, dtype)
+    if n:
+        given = new((T, n), dtype=torch.float32)
+        lp = given.data_ptr()
     if entropy:
-        spread, ep = _made(logits, None, "", (T,), torch.float32, dev, stream)
+        spread = new((T,), dtype=torch.float32)
+        ep = spread.data_ptr()
     if top > 0:
-        likely, kp = _made(logits, None, "", (T, top), torch.float32, dev, stream)
-        ids, ip = _made(logits, None, "", (T, top), torch.int32, dev, stream)
+        likely, ids = new((T, top), dtype=torch.float32), new((T, top), dtype=torch.int32)
+        kp, ip = likely.data_ptr(), ids.data_ptr()
     wp, wn, held = _scratch(logits, workspace, _lib.token_logprobs_workspace_bytes, (T, V, top), stream)
     _launch(_lib.token_logprobs, dev, logits.data_ptr(), stride, T, V, _dt(logits), scale, tp, n, top, lp, ep, kp, ip, wp, wn,
             _stream_of(stream, logits))
