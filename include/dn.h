@@ -494,15 +494,16 @@ DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_strid
  * Rows as OCP e4m3 codes with one fp32 scale per row, x = code * scale:
  * scale = max(max |x| / 448, 2^-120), the code x / scale rounded to nearest even.
  * A row that holds a NaN or an infinity is held as codes 0 and a NaN scale, so
- * every product with it is NaN.
+ * every product with it is NaN.  Scales of rows are aligned to 4 bytes: a part of a
+ * batch may be given.
  *
  * residual_rmsnorm: sum = x + residual and y = RMSNorm(sum) * gamma (Eq. (6), eps
  * as for rms_linear_deferred), all [M][K] of `dtype` (DN_F32 or DN_BF16).  The
  * norm is taken of the fp32 sum, before its rounding; sum and y are rounded once
  * each.  residual may be NULL (sum is then NULL too: y = RMSNorm(x) * gamma), gamma
  * NULL is all ones (as where a product's weights already hold it).  sum may be x or
- * residual itself (the stream updated in place); y and every other pair of ranges
- * must not overlap.
+ * residual itself (the stream updated in place); otherwise no output may overlap an
+ * input or another output.
  *
  * residual_rmsnorm_fp8: the same with y as codes[M][K] and scales[M].  1 / rms is a
  * positive factor of the whole row, so it scales the row's scale and leaves its codes
@@ -601,7 +602,7 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
  * of -inf (forbidden tokens) have p = 0 and rank last.  A row whose logits are all -inf, or
  * that holds +inf or a NaN, gives NaN (targets < 0 excepted); NaN logits have no rank, and
  * a rank that no token has is id -1.  top <= min(V, 64), V < 2^30, scale finite and > 0.
- * logits is aligned to its element, every other array to 16 bytes.
+ * logits is aligned to its element, every other array to 4 bytes.
  * workspace: caller-owned, 256-byte aligned, token_logprobs_workspace_bytes bytes (NULL
  * where that is 0), scratch of one call at a time: long rows are read by several
  * workgroups each, whose sums and ranks a second kernel joins in a fixed order.

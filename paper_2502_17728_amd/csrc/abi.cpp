@@ -663,7 +663,7 @@ static dn_status rows_call(const void* x, const void* residual, const void* gamm
         M > (kMaxThreads - 255) / dn::plan_rows(M, K).threads)
         return DN_ERR_UNSUPPORTED;
     if (!aligned(x, 16) || !aligned(residual, 16) || !aligned(gamma, 16) || !aligned(sum, 16) || !aligned(y, 16) ||
-        !aligned(scales, 16))
+        !aligned(scales, 4))
         return DN_ERR_MISALIGNED;
     const Range in[3] = {{x, xb}, {residual, xb}, {gamma, (size_t)K * esize(dtype)}};
     const Range out_y{y, yb}, out_s{scales, (size_t)M * 4}, out_sum{sum, xb};
@@ -759,7 +759,7 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
     if (dn::fp8_workgroups(plan, M, l.blocks) > kMaxThreads / dn::fp8_threads(plan) ||
         (plan.splits > 1 && M > (kMaxThreads - 255) / (N / 8)))
         return DN_ERR_UNSUPPORTED;
-    if (!aligned(x, 16) || !aligned(x_scales, 16) || !aligned(residual, 16) || !aligned(out, 16) ||
+    if (!aligned(x, 16) || !aligned(x_scales, 4) || !aligned(residual, 16) || !aligned(out, 16) ||
         !aligned(w->packed, 256) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;
     const size_t used = plan.splits > 1 ? plan.splits * part : 0;
@@ -799,8 +799,8 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
     lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
     const dn::LogprobPlan plan = dn::plan_logprobs(T, V, top);
     if (T > kMaxThreads / (plan.segments * plan.threads)) return DN_ERR_UNSUPPORTED;
-    if (!aligned(logits, esize(dtype)) || !aligned(targets, 16) || !aligned(logprobs, 16) || !aligned(entropy, 16) ||
-        !aligned(top_logprobs, 16) || !aligned(top_ids, 16) || !aligned(workspace, 256))
+    if (!aligned(logits, esize(dtype)) || !aligned(targets, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) ||
+        !aligned(top_logprobs, 4) || !aligned(top_ids, 4) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;
     const size_t need = dn::logprob_workspace(T, V, top);
     if (need && (!workspace || workspace_bytes < need)) return DN_ERR_INVALID_ARG;

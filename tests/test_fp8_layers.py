@@ -123,6 +123,27 @@ def test_on_streams_of_their_own():
     assert same(got, want[0])
 
 
+def test_a_part_of_a_batch():
+    """Rows from any one on, with what belongs to them; the rows around are left as they were."""
+    L = Layer(70)
+    s = L()
+    for a, b in ((1, 4), (3, 70), (5, 6)):
+        codes, scales = torch.zeros_like(s["codes"]), torch.full_like(s["scales"], -1.0)
+        ops.residual_rmsnorm_fp8(L.x[a:b], L.d[a:b], L.gamma, codes=codes[a:b], scales=scales[a:b])
+        R.assert_codes(codes[a:b], s["codes"][a:b].double())
+        assert torch.equal(scales[a:b], s["scales"][a:b]) and (scales[:a] == -1).all() and (scales[b:] == -1).all()
+        assert (codes[:a].view(torch.uint8) == 0).all() and (codes[b:].view(torch.uint8) == 0).all()
+        ref, e = R.linear(s["codes"][a:b], s["scales"][a:b], L.w, L.ws, None, "silu", L.u, L.us, None, f32=False)
+        h = torch.full_like(s["h"], 7.0)
+        ops.linear_fp8(s["codes"][a:b], s["scales"][a:b], L.W, "silu", out=h[a:b])
+        R.assert_within(h[a:b], ref, e + (ref.abs() + e) * 2.0 ** -8)
+        assert (h[:a] == 7).all() and (h[b:] == 7).all()
+        targets = torch.cat([L.targets, L.targets[:, :1]], 1)  # rows of 12 bytes
+        got, ref = ops.token_logprobs(s["logits"][a:b], targets[a:b], 3), R.logprobs(s["logits"][a:b], targets[a:b], 3)
+        assert torch.equal(got["top_ids"].long(), ref["top_ids"])
+        R.assert_within(got["logprobs"], ref["logprobs"], ref["logprobs"].abs() * 4 * 2.0 ** -24 + 2e-5)
+
+
 def test_long_offsets():
     """Rows whose last bytes lie past 4 GiB."""
     K = 16384

@@ -44,7 +44,7 @@ def test_rows_refusals():
             assert f(**{name: P[4] + 16}) == INVALID, name
         assert f(sm=P[0] + 16) == INVALID and f(sm=P[1] - 16) == INVALID and f(sm=P[2]) == INVALID
     assert norm8(s=None) == INVALID and norm8(s=P[0]) == INVALID and norm8(s=P[3]) == INVALID and norm8(s=P[4]) == INVALID
-    assert norm8(s=P[9] + 4) == MISALIGNED and norm8(K=72) == UNSUPPORTED
+    assert norm8(s=P[9] + 2) == MISALIGNED and norm8(K=72) == UNSUPPORTED
     for bad in (dict(x=None), dict(y=None), dict(s=None), dict(M=0), dict(dt=3), dict(y=P[0]), dict(s=P[0])):
         assert rows(**bad) == INVALID, bad
     assert rows(K=24) == UNSUPPORTED and rows(x=P[0] + 2) == MISALIGNED
@@ -89,7 +89,7 @@ def test_linear_refusals():
         assert linear(**bad) == INVALID, bad
     for bad in (dict(w=weights(K=72)), dict(w=weights(N=12)), dict(M=1 << 40)):
         assert linear(**bad) == UNSUPPORTED, bad
-    for bad in (dict(x=P[0] + 8), dict(s=P[1] + 4), dict(res=P[2] + 8), dict(out=P[4] + 2), dict(ws=P[3] + 16),
+    for bad in (dict(x=P[0] + 8), dict(s=P[1] + 2), dict(res=P[2] + 8), dict(out=P[4] + 2), dict(ws=P[3] + 16),
                 dict(w=weights(packed=P[7] + 16))):
         assert linear(**bad) == MISALIGNED, bad
     # a workspace that is used must not lie over anything
@@ -119,8 +119,8 @@ def test_logprobs_refusals():
                 dict(t=None, lp=None, n=0, e=None, tl=None, ti=None, top=0), dict(lp=P[0]), dict(e=P[0]), dict(tl=P[3]), dict(ti=P[4]),
                 dict(lp=P[1]), dict(T=1 << 60)):
         assert logprobs(**bad) == INVALID, bad
-    for bad in (dict(x=P[0] + 1), dict(x=P[0] + 2, dt=0), dict(t=P[1] + 4), dict(lp=P[2] + 8), dict(e=P[3] + 4), dict(tl=P[4] + 4),
-                dict(ti=P[5] + 4)):
+    for bad in (dict(x=P[0] + 1), dict(x=P[0] + 2, dt=0), dict(t=P[1] + 2), dict(lp=P[2] + 1), dict(e=P[3] + 2), dict(tl=P[4] + 3),
+                dict(ti=P[5] + 2)):
         assert logprobs(**bad) == MISALIGNED, bad
     big = dict(T=1, V=131072, stride=131072)
     need = lib.token_logprobs_workspace_bytes(1, 131072, 5)
