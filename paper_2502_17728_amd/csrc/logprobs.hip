@@ -332,37 +332,40 @@ __device__ __forceinline__ void finish(const LpArgs& p, int64_t row, const T* x,
     }
 }
 
-// 8 values from x[at] on, -inf outside [0, V); x + at is aligned to 16 bytes.
+// 8 values as they lie in memory: a load that is not widened at once is not waited for at once.
+#define DN_GLOBAL __attribute__((address_space(1)))
+__device__ __forceinline__ u32x4 global_ld16(const DN_GLOBAL char* p) { return *reinterpret_cast<const DN_GLOBAL u32x4*>(p); }
 template <class T>
-__device__ __forceinline__ void load8(const T* x, int64_t at, int64_t V, float* f);
+struct Piece;
 template <>
-__device__ __forceinline__ void load8<__bf16>(const __bf16* x, int64_t at, int64_t V, float* f) {
-    if (at >= 0 && at + 8 <= V) {
-        const u32x4 w = ld16(x + at);
+struct Piece<__bf16> {
+    u32x4 w;
+    __device__ __forceinline__ void load(const DN_GLOBAL char* p) { w = global_ld16(p); }
+    __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f[2 * e] = bf_lo(w[e]);
             f[2 * e + 1] = bf_hi(w[e]);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = at + e >= 0 && at + e < V ? (float)x[at + e] : -__builtin_inff();
     }
-}
+};
 template <>
-__device__ __forceinline__ void load8<float>(const float* x, int64_t at, int64_t V, float* f) {
-    if (at >= 0 && at + 8 <= V) {
-        const u32x4 a = ld16(x + at), b = ld16(x + at + 4);
+struct Piece<float> {
+    u32x4 a, b;
+    __device__ __forceinline__ void load(const DN_GLOBAL char* p) {
+        a = global_ld16(p);
+        b = global_ld16(p + 16);
+    }
+    __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
             f[e] = __uint_as_float(a[e]);
             f[4 + e] = __uint_as_float(b[e]);
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) f[e] = at + e >= 0 && at + e < V ? x[at + e] : -__builtin_inff();
     }
-}
+};
+// What a row without a whole piece loads, in vain.
+__device__ const u32x4 kNoPiece[2] = {};
 
 // The largest of 8 values by three-operand instructions (fmaxf would first quiet each operand); a NaN is no maximum.
 __device__ __forceinline__ float max8(const float* f) {
@@ -374,7 +377,7 @@ __device__ __forceinline__ float max8(const float* f) {
     return d;
 }
 
-// A workgroup of NT threads takes a row, or one of its segments; loads run one step of 8 NT tokens ahead.
+// A workgroup of NT threads takes a row, or one of its segments; loads run two steps of 8 NT tokens ahead.
 template <class T, bool TOP, int NT>
 __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
     constexpr int NW = NT / kWave;
@@ -393,6 +396,11 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
     const int shift = (int)((reinterpret_cast<uintptr_t>(x) & 15) / sizeof(T));
     const int pieces = (int)((p.V + shift + 7) / 8), per = (pieces + p.segments - 1) / p.segments;
     const int end = min(pieces, (seg + 1) * per);
+    // pieces that lie in the row whole; the others' values are read one by one
+    const int whole0 = shift ? 1 : 0, whole1 = (V + shift) / 8 - 1;
+    const bool any_whole = whole1 >= whole0;
+    const DN_GLOBAL char* base = (const DN_GLOBAL char*)(any_whole ? (const void*)(x - shift) : (const void*)kNoPiece);
+    const int from0 = any_whole ? whole0 : 0, from1 = any_whole ? whole1 : 0, whole_end = min(end - 1, whole1);
 
     Sums a{kLowest, 0.f, 0.f};
     Ranked ranked{(DN_LDS WaveRanks*)&ranks[TOP ? wave : 0], 0, 0, p.top, 0, 0};
@@ -400,12 +408,26 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
     Given given{-1, 0.f};
     if (wave == 0 && p.segments == 1 && p.n) given.load(p, row, x, lane);
     bool first = true;
-    auto load = [&](int from, float* f) {
-        const int v = from + lane;
-        if (from < end) load8<T>(x, (int64_t)v * 8 - shift, v < end ? V : 0, f);  // past the segment: nothing
+    Piece<T> q[2];
+    // without conditions, so that the loads in flight can be counted: past the row's last whole piece this one again
+    auto load = [&](int from, Piece<T>& to) {
+        const uint32_t v = (uint32_t)max(min(from + lane, from1), from0);
+        to.load(base + (size_t)(v * (uint32_t)(8 * sizeof(T))));  // below 2^32: V is below 2^30
     };
-    auto take = [&](const float* f) {
+    auto take = [&](Piece<T>& piece) {
         const int v = v0 + lane;
+        float f[8];
+        piece.get(f);
+        load(v0 + 2 * NT, piece);
+        if (v0 < whole0 || v0 + kWave - 1 > whole_end) {
+            if (v < whole0 || v > whole_end) {
+#pragma unroll
+                for (int e = 0; e < 8; ++e) {
+                    const int at = v * 8 - shift + e;
+                    f[e] = v < end && at >= 0 && at < V ? to_f32<T>(x[at]) : -__builtin_inff();
+                }
+            }
+        }
         const float most = max8(f);
         if (__any(most > a.m)) raise(a, __builtin_fmaxf(a.m, most), c);
 #pragma unroll
@@ -421,14 +443,13 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
         }
         v0 += NT;
     };
-    float f[8], g[8];
-    load(v0, f);
+    load(v0, q[0]);
+    __builtin_amdgcn_sched_barrier(0);  // in this order: the first is waited for alone
+    load(v0 + NT, q[1]);
+    __builtin_amdgcn_sched_barrier(0);
     while (v0 < end) {
-        load(v0 + NT, g);
-        take(f);
-        if (v0 >= end) break;
-        load(v0 + NT, f);
-        take(g);
+        take(q[0]);
+        take(q[1]);  // possibly past the end, where it changes nothing
     }
     a = wave_join(a, c);
     if (TOP && ranked.groups) ranked.flush(V, lane);
