@@ -143,17 +143,25 @@ struct WaveRanks {
 };
 
 // A wave's likeliest tokens so far: n keys, none below `floor`, and groups of 8 tokens that have not been looked at.
-// A further token counts if the order of its logit is `bar` or more.
+// A further token counts if the order of its logit is `bar` or more, which is to say the logit `least` or more.
 struct Ranked {
     DN_LDS WaveRanks* m;
     int n, groups, top;
     uint32_t floor, bar;
+    float least;
 
-    // From the lanes' maxima of the first tokens (order 0 where a lane has none): at least `top` tokens are not below
+    __device__ __forceinline__ void set_bar(uint32_t b) {
+        bar = b;
+        // orders up to that of -inf belong to NaNs of either sign: every number counts
+        least = b <= 0x007fffffu ? -__builtin_inff() : value_of((unsigned long long)b << 32);
+    }
+
+    // From the lanes' maxima of the first tokens (NaN where a lane has none): at least `top` tokens are not below
     // what `top` of these reach, and the rest need not be kept.
-    __device__ __forceinline__ void start(float most, bool there) {
-        const uint32_t o = there && most == most ? order_of(most) : 0;
-        bar = floor = search(wave_min(o), wave_max(o), 16, top, top + 1, [&](uint32_t t) { return __popcll(__ballot(o >= t)); });
+    __device__ __forceinline__ void start(float most) {
+        const uint32_t o = most == most ? order_of(most) : 0;
+        floor = search(wave_min(o), wave_max(o), 16, top, top + 1, [&](uint32_t t) { return __popcll(__ballot(o >= t)); });
+        set_bar(floor);
     }
 
     // Sorts the keys and cuts them to `top`, by counting the larger ones.
@@ -183,7 +191,8 @@ struct Ranked {
         lds_in_order();
         if (n >= top) {
             n = top;
-            bar = floor = (uint32_t)__builtin_amdgcn_readfirstlane((int)(k[top - 1] >> 32));
+            floor = (uint32_t)__builtin_amdgcn_readfirstlane((int)(k[top - 1] >> 32));
+            set_bar(floor);
         }
     }
 
@@ -200,7 +209,7 @@ struct Ranked {
         if (kb) m->keys[__popcll(ma) + lanes_below(mb)] = b;
         n = __popcll(ma) + __popcll(mb);
         lds_in_order();
-        bar = floor;
+        set_bar(floor);
         if (n > 64) rank(lane);  // many equals
     }
 
@@ -226,13 +235,13 @@ struct Ranked {
         groups = 0;
         if (n >= top) {
             cut(lane);
-            if (floor != 0xffffffffu) bar = floor + 1;
+            if (floor != 0xffffffffu) set_bar(floor + 1);
         }
     }
 
-    // f[0 .. 7] are tokens at, at + 1, .., `most` the largest of them; `there`: the lane has some.
-    __device__ __forceinline__ void add(const float* f, float most, bool there, int at, int V, int lane) {
-        const bool keep = there && order_of(most) >= bar;
+    // f[0 .. 7] are tokens at, at + 1, .., `most` the largest of them (NaN: there is none).
+    __device__ __forceinline__ void add(const float* f, float most, int at, int V, int lane) {
+        const bool keep = most >= least;
         const unsigned long long mask = __ballot(keep);
         if (!mask) return;
         if (keep) {
@@ -282,7 +291,7 @@ __device__ __forceinline__ unsigned long long top_of_(const DN_LDS unsigned long
             return n;
         });
     }
-    Ranked r{m, 0, 0, top, 0, 0};
+    Ranked r{m, 0, 0, top, 0, 0, 0.f};
     lds_in_order();
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
@@ -403,7 +412,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
     const int from0 = any_whole ? whole0 : 0, from1 = any_whole ? whole1 : 0, whole_end = min(end - 1, whole1);
 
     Sums a{kLowest, 0.f, 0.f};
-    Ranked ranked{(DN_LDS WaveRanks*)&ranks[TOP ? wave : 0], 0, 0, p.top, 0, 0};
+    Ranked ranked{(DN_LDS WaveRanks*)&ranks[TOP ? wave : 0], 0, 0, p.top, 0, 0, 0.f};
     int v0 = seg * per + wave * kWave;
     Given given{-1, 0.f};
     if (wave == 0 && p.segments == 1 && p.n) given.load(p, row, x, lane);
@@ -419,6 +428,7 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
         float f[8];
         piece.get(f);
         load(v0 + 2 * NT, piece);
+        bool there = true;
         if (v0 < whole0 || v0 + kWave - 1 > whole_end) {
             if (v < whole0 || v > whole_end) {
 #pragma unroll
@@ -427,9 +437,10 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
                     f[e] = v < end && at >= 0 && at < V ? to_f32<T>(x[at]) : -__builtin_inff();
                 }
             }
+            there = v < end;
         }
-        const float most = max8(f);
-        if (__any(most > a.m)) raise(a, __builtin_fmaxf(a.m, most), c);
+        float most = max8(f);
+        if (__any(most > a.m)) raise(a, wave_maxf(__builtin_fmaxf(a.m, most)), c);  // seldom: one maximum for the wave
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float d = exponent(f[e], a.m, c), w = __builtin_amdgcn_exp2f(d);
@@ -437,9 +448,10 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
             a.s = __builtin_fmaf(w, __builtin_fmaxf(d, kLeastExponent), a.s);
         }
         if constexpr (TOP) {
-            if (first) ranked.start(most, v < end);
+            if (!there) most = __builtin_nanf("");
+            if (first) ranked.start(most);
             first = false;
-            ranked.add(f, most, v < end, v * 8 - shift, V, lane);  // v * 8 - shift < 2^31: V is
+            ranked.add(f, most, v * 8 - shift, V, lane);  // v * 8 - shift < 2^31: V is
         }
         v0 += NT;
     };
