@@ -125,17 +125,21 @@ inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
 // ------------------------------------------------------------------------------- log probabilities
 constexpr int64_t kMaxTop = 64, kMaxSegments = 16;
 
-// Threads to a workgroup and workgroups to a row.  Rows that fill the chip take 256 threads each if they are ranked, else
-// 512 (4000 x 32008 fp32 without ranks 87 us, 256 threads 91; with 20 alternatives 137 and 108).  Fewer rows take 512, and
-// a workgroup to each 16384 tokens while there is about one to a CU; a second kernel then joins them.  Measured, us, bf16
-// with 20 alternatives: 32 x 131072 17.2 (8 segments; 16: 18.7, 4: 21.0), 1 x 32000 12.4 (2; 1: 13.6), 200 x 32000 16.8
-// (1; 2: 19.0); 1 x 8192 7.7 (256 threads 8.8, 1024 8.1).
+// Threads to a workgroup and workgroups to a row.  Each wave ranks what it reads by itself, so ranked rows take as few
+// waves as fill the chip, and rows without ranks few only if they are short.  Measured, us, with 512, 256 and 128 threads,
+// bf16 with 20 alternatives: 300 x 131072 34.6, 37.2, 57.4; 1000 x 100003 48.8, 46.0, 49.1; 4000 x 32008 87.7, 65.8, 58.6;
+// 16000 x 8192 179, 113, 86; without: 16000 x 8192 58, 47, 44; fp32 4000 x 32008 87.8, 91.4, 96.4.
+// Fewer than 256 rows get a workgroup to each 16384 tokens while there is about one to a CU; a second kernel then joins
+// them: 32 x 131072 17.2 (8 segments; 16: 18.7, 4: 21.0), 1 x 32000 12.4 (2; 1: 13.6), 200 x 32000 16.8 (1; 2: 19.0).
 struct LogprobPlan {
     int threads;
     int64_t segments;
 };
 inline LogprobPlan plan_logprobs(int64_t T, int64_t V, int64_t top) {
-    if (T >= 256) return LogprobPlan{top ? 256 : 512, 1};
+    if (T >= 256) {
+        if (T < 512) return LogprobPlan{512, 1};
+        return top ? LogprobPlan{T < 2000 ? 256 : 128, 1} : LogprobPlan{V < 16384 ? 128 : 512, 1};
+    }
     return LogprobPlan{512, std::max<int64_t>(1, std::min({256 / T, (V + 8192) / 16384, kMaxSegments}))};
 }
 // A segment leaves its maximum, denominator and entropy sum (16 bytes) and `top` ranked keys of 8 bytes.

@@ -533,8 +533,10 @@ static void launch_logprobs(const LpArgs& p, int threads, hipStream_t s) {
     const dim3 grid((unsigned)(p.T * p.segments));
     if (threads == 512)
         logprobs_kernel<T, TOP, 512><<<grid, 512, 0, s>>>(p);
-    else
+    else if (threads == 256)
         logprobs_kernel<T, TOP, 256><<<grid, 256, 0, s>>>(p);
+    else
+        logprobs_kernel<T, TOP, 128><<<grid, 128, 0, s>>>(p);
     if (p.segments > 1) logprobs_join_kernel<T><<<dim3((unsigned)p.T), kWave, 0, s>>>(p);
 }
 

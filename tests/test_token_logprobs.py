@@ -31,10 +31,10 @@ def check(ops, logits, targets, top, scale=1.0, **kw):
     ref = R.logprobs(logits, targets, top, scale)
     # ln p = d - ln l, d = scale (x - m).  d is 2 roundings off; an exponent to base 2 takes a third and is then
     # off by 3 2^-24 of itself, at most 40 where its power counts in a sum (2^-40 V is past fp32 else): l and ln l
-    # are off by 3 * 40 * 2^-24 * ln 2, the powers' and logarithm's own 2 steps, and a chain of sums: 64 values and rescalings
-    # of a lane's share per 16384, 6 + 2 + 6 joins.
+    # are off by 3 * 40 * 2^-24 * ln 2, the powers' and logarithm's own 2 steps, and a chain of sums: a lane's
+    # share of at most V / 128 values (128 threads to a row) and rescalings, 6 + 2 + 6 joins.
     V = logits.shape[1]
-    l = (3 * 40 * 0.7 + 4 + 2 * (V / 512 + 40)) * 2.0 ** -24
+    l = (3 * 40 * 0.7 + 4 + (V / 128 + 80)) * 2.0 ** -24
     for name in ("logprobs", "top_logprobs"):
         if ref[name] is None:
             assert got[name] is None
@@ -66,6 +66,14 @@ def test_rows_that_start_at_any_element(ops, dtype, offset):
     for V, row in ((37, 41), (4099, 4101), (9001, 9003)):
         logits, targets = make(5, V, dtype, offset, row, offset)
         check(ops, logits, targets, 7)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("T,V", [(600, 3000), (600, 20003), (2100, 11), (2100, 1023), (2003, 5001)])
+def test_many_rows(ops, T, V, dtype):
+    for top in (0, 1, 20, 64):
+        logits, targets = make(T, V, dtype, T + V + top)
+        check(ops, logits, targets, min(top, V))
 
 
 def test_what_lies_around_the_rows_is_not_read(ops):
