@@ -126,9 +126,10 @@ inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
 constexpr int64_t kMaxTop = 64, kMaxSegments = 16;
 
 // Threads to a workgroup and workgroups to a row.  Each wave ranks what it reads by itself, so ranked rows take as few
-// waves as fill the chip, and rows without ranks few only if they are short.  Measured, us, with 512, 256 and 128 threads,
-// bf16 with 20 alternatives: 300 x 131072 34.6, 37.2, 57.4; 1000 x 100003 48.8, 46.0, 49.1; 4000 x 32008 87.7, 65.8, 58.6;
-// 16000 x 8192 179, 113, 86; without: 16000 x 8192 58, 47, 44; fp32 4000 x 32008 87.8, 91.4, 96.4.
+// waves as fill the chip, and rows without ranks few only if they are short.  Measured, us, with 512, 256, 128 and 64 threads,
+// bf16 with 20 alternatives: 300 x 131072 34.6, 37.2, 57.4, -; 1000 x 100003 48.8, 46.0, 49.1, -; 2000 x 8192 -, 20.8, 17.9, 18.4;
+// 4000 x 32008 87.7, 66.1, 57.8, 53.5; 8000 x 32008 171, 128, 108, 114; 16000 x 8192 179, 115, 86, 67; without: 16000 x 8192
+// 58, 49, 44, 44; 16000 x 1000 -, 28, 20, 12; fp32 4000 x 32008 87.8, 91.2, 96.9, 94.0.
 // Fewer than 256 rows get a workgroup to each 16384 tokens while there is about one to a CU; a second kernel then joins
 // them: 32 x 131072 17.2 (8 segments; 16: 18.7, 4: 21.0), 1 x 32000 12.4 (2; 1: 13.6), 200 x 32000 16.8 (1; 2: 19.0).
 struct LogprobPlan {
@@ -137,8 +138,10 @@ struct LogprobPlan {
 };
 inline LogprobPlan plan_logprobs(int64_t T, int64_t V, int64_t top) {
     if (T >= 256) {
+        const bool shorter = V < 16384;
         if (T < 512) return LogprobPlan{512, 1};
-        return top ? LogprobPlan{T < 2000 ? 256 : 128, 1} : LogprobPlan{V < 16384 ? 128 : 512, 1};
+        if (!top) return LogprobPlan{!shorter ? 512 : T >= 2000 && V < 8192 ? 64 : 128, 1};
+        return LogprobPlan{T < 2000 ? 256 : shorter && T >= 4000 ? 64 : 128, 1};
     }
     return LogprobPlan{512, std::max<int64_t>(1, std::min({256 / T, (V + 8192) / 16384, kMaxSegments}))};
 }

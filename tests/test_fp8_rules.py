@@ -143,7 +143,7 @@ def test_launches_past_the_devices_limit_are_refused():
     f = lambda M, x=far[0]: lib.linear_fp8(x, far[1], ctypes.byref(w), M, 0, None, 1, None, 0, far[2], None)
     assert f(1 << 32) == UNSUPPORTED
     f = lambda T, x=far[0]: lib.token_logprobs(x, 8, T, 8, 1, 1.0, None, 0, 0, None, far[1], None, None, None, 0, None)
-    assert f(1 << 25) == UNSUPPORTED and f((1 << 25) - 1, far[0] + 1) == MISALIGNED
+    assert f(1 << 26) == UNSUPPORTED and f((1 << 26) - 1, far[0] + 1) == MISALIGNED
 
 
 def test_binding_refuses_cpu_tensors():
@@ -221,5 +221,5 @@ def test_row_plans_hold_the_row():
 def test_logprob_plans():
     for T, V, top in itertools.product(SIZES, (1, 8, 1000, 8192, 32000, 50257, 131072, 1 << 20, (1 << 30) - 1), (0, 1, 64)):
         threads, segments = call("lp", T, V, top, n=2)
-        assert threads in (128, 256, 512) and 1 <= segments <= 16
+        assert threads in (64, 128, 256, 512) and 1 <= segments <= 16
         assert segments == 1 or (V + 14) // 8 >= segments  # every segment but the last has tokens

@@ -32,9 +32,9 @@ def check(ops, logits, targets, top, scale=1.0, **kw):
     # ln p = d - ln l, d = scale (x - m).  d is 2 roundings off; an exponent to base 2 takes a third and is then
     # off by 3 2^-24 of itself, at most 40 where its power counts in a sum (2^-40 V is past fp32 else): l and ln l
     # are off by 3 * 40 * 2^-24 * ln 2, the powers' and logarithm's own 2 steps, and a chain of sums: a lane's
-    # share of at most V / 128 values (128 threads to a row) and rescalings, 6 + 2 + 6 joins.
+    # share of at most V / 64 values (64 threads to a row) and rescalings, 6 + 2 + 6 joins.
     V = logits.shape[1]
-    l = (3 * 40 * 0.7 + 4 + (V / 128 + 80)) * 2.0 ** -24
+    l = (3 * 40 * 0.7 + 4 + (V / 64 + 80)) * 2.0 ** -24
     for name in ("logprobs", "top_logprobs"):
         if ref[name] is None:
             assert got[name] is None
@@ -69,7 +69,8 @@ def test_rows_that_start_at_any_element(ops, dtype, offset):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
-@pytest.mark.parametrize("T,V", [(600, 3000), (600, 20003), (2100, 11), (2100, 1023), (2003, 5001)])
+@pytest.mark.parametrize("T,V", [(600, 3000), (600, 20003), (2100, 11), (2100, 1023), (2003, 5001), (2001, 8200), (4003, 257),
+                                 (4003, 4500)])
 def test_many_rows(ops, T, V, dtype):
     for top in (0, 1, 20, 64):
         logits, targets = make(T, V, dtype, T + V + top)
