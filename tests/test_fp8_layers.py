@@ -167,6 +167,23 @@ def test_long_offsets():
     assert torch.equal(a["top_ids"][-1], b["top_ids"][0]) and a["top_ids"][0].tolist() == [0, 1, 2, 3, 4]
 
 
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_the_longest_row(dtype):
+    V = 2 ** 30 - 1
+    logits = torch.zeros((1, V), dtype=dtype, device="cuda")
+    ids = [V - 1, 2 ** 29 + 7, 3]
+    for i, at in enumerate(ids):
+        logits[0, at] = 50.0 - 5 * i
+    got = ops.token_logprobs(logits, torch.tensor([ids], dtype=torch.int32, device="cuda"), 5)
+    assert got["top_ids"][0].tolist() == ids + [0, 1]
+    # the zeros' share is 2^30 e^-50, 2e-13 of the sum
+    d = torch.tensor([0.0, -5.0, -10.0], dtype=torch.float64, device="cuda")
+    want = d - d.exp().sum().log()
+    bound = 16 * 2.0 ** -24 * (1 + want.abs())
+    R.assert_within(got["logprobs"][0], want, bound)
+    R.assert_within(got["top_logprobs"][0, :3], want, bound)
+
+
 PATH = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "examples", "serve_layers.py")
 spec = importlib.util.spec_from_file_location("serve_layers", PATH)
 serve = importlib.util.module_from_spec(spec)
