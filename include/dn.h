@@ -492,7 +492,8 @@ DN_API dn_status attention_shared_prefix_deferred(const void* Q, int64_t q_strid
 
 /*
  * Rows as OCP e4m3 codes with one fp32 scale per row, x = code * scale:
- * scale = max(max |x| / 448, 2^-120), the code x / scale rounded to nearest even.
+ * scale = max(max |x| / 448, 2^-120), the code x / scale (the fp32 quotient) rounded to
+ * nearest even.
  * A row that holds a NaN or an infinity is held as codes 0 and a NaN scale, so
  * every product with it is NaN.  Scales of rows are aligned to 4 bytes: a part of a
  * batch may be given.

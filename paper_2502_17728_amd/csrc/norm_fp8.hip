@@ -14,7 +14,7 @@
 namespace dn {
 
 constexpr float kF8Max = 448.f;
-constexpr float kLeastScale = 7.52316385e-37f;  // 2^-120: its reciprocal is finite
+constexpr float kLeastScale = 7.52316385e-37f;  // 2^-120
 
 // What a row becomes.
 enum class RowOut { kNorm, kNormFp8, kFp8 };
@@ -29,6 +29,16 @@ struct RowArgs {
     int64_t M, K;
     float eps;
 };
+
+// a / s as a code's rounding sees it, s >= kExactFrom: inv = 1 / s to the nearest, and the remainder of a inv is exact and puts it
+// right.  Next to a tie t of two codes (5 bits) a inv is one of the fp32 neighbours of a / s, so the remainder is s / 2
+// steps of them at most, the error of its product with inv below 2^-25 steps, and no quotient of two 24-bit numbers is as near as that
+// to the middle of two neighbours.  8192 x 8192 bf16 84.1 us, with the division 85.6; rows alone 4096 x 14336 26.2 and 31.5.
+constexpr float kExactFrom = 2.01948392e-28f;  // 2^-92: the remainder's last bit is 2^-149 at least
+__device__ __forceinline__ float quotient(float a, float s, float inv) {
+    const float q = a * inv;
+    return __builtin_fmaf(__builtin_fmaf(-q, s, a), inv, q);
+}
 
 // 8 consecutive values of a row as they lie in memory
 template <class T>
@@ -169,15 +179,21 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs p) 
         const float inv = 1.f / s;
         if (t == 0) p.scales[row] = bad ? __builtin_nanf("") : s * r;
         char* codes = reinterpret_cast<char*>(p.y) + row * p.K;
+        auto put = [&](auto quotient_of) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            if (t + j * TPR >= pieces) continue;
+            for (int j = 0; j < NV; ++j) {
+                if (t + j * TPR >= pieces) continue;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) a[j][e] *= inv;
-            uint2 w = {pack_e4m3(a[j][0], a[j][1], a[j][2], a[j][3]), pack_e4m3(a[j][4], a[j][5], a[j][6], a[j][7])};
-            if (bad) w = uint2{0u, 0u};
-            *reinterpret_cast<uint2*>(codes + (t + j * TPR) * 8) = w;
-        }
+                for (int e = 0; e < 8; ++e) a[j][e] = quotient_of(a[j][e]);
+                uint2 w = {pack_e4m3(a[j][0], a[j][1], a[j][2], a[j][3]), pack_e4m3(a[j][4], a[j][5], a[j][6], a[j][7])};
+                if (bad) w = uint2{0u, 0u};
+                *reinterpret_cast<uint2*>(codes + (t + j * TPR) * 8) = w;
+            }
+        };
+        if (s >= kExactFrom)
+            put([&](float v) { return quotient(v, s, inv); });
+        else
+            put([&](float v) { return v / s; });
     }
 }
 
