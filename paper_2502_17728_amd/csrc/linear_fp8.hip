@@ -64,20 +64,35 @@ __device__ __forceinline__ f32x4 mfma_codes(const u32x4& a0, const u32x4& a1, co
 // z / (1 + e^-t)
 __device__ __forceinline__ float gate(float z, float t) { return z / (1.f + __builtin_amdgcn_exp2f(-t * kLog2eF)); }
 
-// z Phi(z) by Abramowitz and Stegun 7.1.26: erfc(x) = (a1 t + .. + a5 t^5) e^-x^2, t = 1 / (1 + p x), x >= 0, off
-// by 1.5e-7 at most.  With the tail q = erfc(|z| / sqrt 2) / 2 it is max(z, 0) - |z| q: nothing cancels at negative z.
-// (|z| stands still at 30, where q is 0, so that an infinity is not multiplied by 0.)  Less than half of erff's
-// instructions: the GELU of 8192 x 28672 outputs cost 216 us of 1740 with it.
+// z Phi(z) = max(z, 0) - |z| q with the tail q = erfc(|z| / sqrt 2) / 2: nothing cancels at negative z, so the result is as
+// good there as q is relative to itself.  q = t P(t) e^(-z^2 / 2), t = 1 / (1 + p |z|); P is fitted here, by exchange of the largest
+// relative errors (Remez), for |z| to 13.5, where q leaves fp32: degree 7 to 1.3e-7 where the output is fp32 (WIDE), degree 4
+// to 3.5e-5, a hundredth of the rounding, where it is bf16.  The power adds up to 1.5 z^2 2^-24 of itself.  (|z| stands still at
+// 30, where q is 0, so that an infinity is not multiplied by 0.)  Less than half of erff's instructions: the GELU of
+// 8192 x 28672 outputs cost 216 us of 1740 with it.
+template <bool WIDE>
 __device__ __forceinline__ float gelu(float z) {
-    const float a = __builtin_fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3275911f * 0.70710678118654752f, a, 1.f));
-    float q = __builtin_fmaf(0.5f * 1.061405429f, t, 0.5f * -1.453152027f);
-    q = __builtin_fmaf(q, t, 0.5f * 1.421413741f);
-    q = __builtin_fmaf(q, t, 0.5f * -0.284496736f);
-    q = __builtin_fmaf(q, t, 0.5f * 0.254829592f);
+    const float a = __builtin_fabsf(z), t = __builtin_amdgcn_rcpf(__builtin_fmaf(WIDE ? 0.30f : 0.38f, a, 1.f));
+    float q;
+    if constexpr (WIDE) {
+        q = __builtin_fmaf(0.0359317251f, t, -0.158275962f);
+        q = __builtin_fmaf(q, t, 0.208206534f);
+        q = __builtin_fmaf(q, t, -0.0553937852f);
+        q = __builtin_fmaf(q, t, 0.129469171f);
+        q = __builtin_fmaf(q, t, 0.0996375009f);
+        q = __builtin_fmaf(q, t, 0.120798357f);
+        q = __builtin_fmaf(q, t, 0.119626388f);
+    } else {
+        q = __builtin_fmaf(-0.0899283141f, t, 0.188876390f);
+        q = __builtin_fmaf(q, t, 0.0919798091f);
+        q = __builtin_fmaf(q, t, 0.157829449f);
+        q = __builtin_fmaf(q, t, 0.151225135f);
+    }
     q *= t * __builtin_amdgcn_exp2f(-0.5f * kLog2eF * z * z);
     return __builtin_fmaf(-__builtin_fminf(a, 30.f), q, __builtin_fmaxf(z, 0.f));
 }
 
+template <bool WIDE>
 __device__ __forceinline__ void activate8(float* v, int act) {
     switch (act) {  // uniform: outside the loops over values
         case 0: break;
@@ -91,7 +106,7 @@ __device__ __forceinline__ void activate8(float* v, int act) {
             break;
         case 3:
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = gelu(v[e]);
+            for (int e = 0; e < 8; ++e) v[e] = gelu<WIDE>(v[e]);
             break;
         default:  // (1 + tanh a) / 2 = 1 / (1 + e^-2a), 2a = sqrt(8 / pi) (z + 0.044715 z^3)
 #pragma unroll
@@ -171,7 +186,7 @@ __device__ __forceinline__ void finish8(const Fp8Args& p, const float* g, const 
     float v[8];
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[e] = k.z(g[e], sx, e);
-    activate8(v, p.act);
+    p.out_f32 ? activate8<true>(v, p.act) : activate8<false>(v, p.act);
     if (p.gated) {
         k.load(p.ws + c + 16, p.bias + c + 16);
 #pragma unroll
@@ -595,7 +610,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void fp8_tile_kernel(Fp8Args p) {
                 float v[8];
 #pragma unroll
                 for (int e = 0; e < 8; ++e) v[e] = k.z(e < 4 ? a0[e & 3] : a1[e & 3], sx, e);
-                activate8(v, p.act);
+                activate8<F32>(v, p.act);
                 if (GATED) {
                     const f32x4 u0 = *reinterpret_cast<const f32x4*>(at + 16), u1 = *reinterpret_cast<const f32x4*>(at + 20);
 #pragma unroll
