@@ -158,7 +158,7 @@ struct Ranked {
         least = b <= 0x007fffffu ? -__builtin_inff() : value_of((unsigned long long)b << 32);
     }
 
-    // From the lanes' maxima of the first tokens (NaN where a lane has none): at least `top` tokens are not below
+    // From the lanes' maxima of the first tokens (NaN where a lane has none, or NaNs among them): at least `top` tokens are not below
     // what `top` of these reach, and the rest need not be kept.
     __device__ __forceinline__ void start(float most) {
         const uint32_t o = most == most ? order_of(most) : 0;
@@ -247,9 +247,11 @@ struct Ranked {
         }
     }
 
-    // f[0 .. 7] are tokens at, at + 1, .., `most` the largest of them (NaN: there is none).
+    // f[0 .. 7] are tokens at, at + 1, .. (from V on they are none), `most` the largest of them, or NaN if one of them is: then the
+    // group is put aside whatever its numbers are.  (Rows of nothing but NaNs, 1000 x 100003, take 118 us instead of 44 with
+    // a look for their groups' numbers here, and all other rows 46.0 instead of 47.4.)
     __device__ __forceinline__ void add(const float* f, float most, int at, int V, int lane) {
-        const bool keep = most >= least;
+        const bool keep = !(most < least);
         const unsigned long long mask = __ballot(keep);
         if (!mask) return;
         if (keep) {
@@ -384,13 +386,14 @@ struct Piece<float> {
 // What a row without a whole piece loads, in vain.
 __device__ const u32x4 kNoPiece[2] = {};
 
-// The largest of 8 values by three-operand instructions (fmaxf would first quiet each operand); a NaN is no maximum.
+// The largest of 8 values by three-operand instructions (the two-operand ones take twice as many), NaN if one of them is: the
+// other kind of maximum, v_max3, drops what stands beside a signalling NaN.
 __device__ __forceinline__ float max8(const float* f) {
     float a, b, c, d;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(f[0]), "v"(f[1]), "v"(f[2]));
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(f[3]), "v"(f[4]), "v"(f[5]));
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(c) : "v"(a), "v"(f[6]), "v"(f[7]));
-    asm("v_max_f32 %0, %1, %2" : "=v"(d) : "v"(b), "v"(c));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(a) : "v"(f[0]), "v"(f[1]), "v"(f[2]));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(b) : "v"(f[3]), "v"(f[4]), "v"(f[5]));
+    asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(c) : "v"(a), "v"(f[6]), "v"(f[7]));
+    asm("v_maximum3_f32 %0, %1, %2, %2" : "=v"(d) : "v"(b), "v"(c));
     return d;
 }
 
@@ -448,7 +451,8 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
             there = v < end;
         }
         float most = max8(f);
-        if (__any(most > a.m)) raise(a, wave_maxf(__builtin_fmaxf(a.m, most)), c);  // seldom: one maximum for the wave
+        // seldom: one maximum for the wave.  (A NaN raises nothing: the row's sums are NaN by then.)
+        if (__any(most > a.m)) raise(a, wave_maxf(__builtin_fmaxf(a.m, most)), c);
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const float d = exponent(f[e], a.m, c), w = __builtin_amdgcn_exp2f(d);
@@ -456,10 +460,9 @@ __global__ __launch_bounds__(NT) void logprobs_kernel(LpArgs p) {
             a.s = __builtin_fmaf(w, __builtin_fmaxf(d, kLeastExponent), a.s);
         }
         if constexpr (TOP) {
-            if (!there) most = __builtin_nanf("");
-            if (first) ranked.start(most);
+            if (first) ranked.start(there ? most : __builtin_nanf(""));
             first = false;
-            ranked.add(f, most, v * 8 - shift, V, lane);  // v * 8 - shift < 2^31: V is
+            ranked.add(f, most, there ? v * 8 - shift : V, V, lane);  // v * 8 - shift < 2^31: V is
         }
         v0 += NT;
     };
