@@ -604,8 +604,8 @@ DN_API dn_status linear_fp8(const void* x, const float* x_scales, const linear_f
  * of -inf (forbidden tokens) have p = 0 and rank last.  A row whose logits are all -inf, or
  * that holds +inf or a NaN, gives NaN (targets < 0 excepted); NaN logits, of either kind,
  * have no rank and leave the others theirs; a rank that no token has is id -1.
- * top <= min(V, 64), V < 2^30, scale finite and > 0.  logits is aligned to its element,
- * every other array to 4 bytes.
+ * top <= min(V, 64), V < 2^30, scale finite and at least 2^-96.  logits is aligned to its
+ * element, every other array to 4 bytes.
  * workspace: caller-owned, 256-byte aligned, token_logprobs_workspace_bytes bytes (NULL
  * where that is 0), scratch of one call at a time: long rows are read by several
  * workgroups each, whose sums and ranks a second kernel joins in a fixed order.

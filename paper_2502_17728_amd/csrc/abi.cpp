@@ -798,7 +798,8 @@ DN_API dn_status token_logprobs(const void* logits, int64_t stride, int64_t T, i
         return DN_ERR_INVALID_ARG;
     lb -= (size_t)(stride - V) * esize(dtype);  // the last row ends with its last token
     const dn::LogprobPlan plan = dn::plan_logprobs(T, V, top);
-    if (T > kMaxThreads / (plan.segments * plan.threads)) return DN_ERR_UNSUPPORTED;
+    // below 2^-96 logits that lie further apart than fp32 reaches would still count beside each other
+    if (T > kMaxThreads / (plan.segments * plan.threads) || scale < 0x1p-96f) return DN_ERR_UNSUPPORTED;
     if (!aligned(logits, esize(dtype)) || !aligned(targets, 4) || !aligned(logprobs, 4) || !aligned(entropy, 4) ||
         !aligned(top_logprobs, 4) || !aligned(top_ids, 4) || !aligned(workspace, 256))
         return DN_ERR_MISALIGNED;

@@ -24,7 +24,9 @@
 namespace dn {
 
 constexpr float kLowest = -3.402823466e38f;
-constexpr float kLeastExponent = -200.f;  // 2^-200 is 0 in fp32; keeps 0 * -inf out of the sums
+// 2^-200 is 0 in fp32; keeps 0 * -inf out of the sums.  (x - m may pass fp32's range: with a scale of 2^-96 or more, which calls have,
+// such a token's power is below e^(-2^32).)
+constexpr float kLeastExponent = -200.f;
 constexpr float kLn2 = 0.6931471805599453f;
 constexpr int kBuffer = 128;                 // keys of a wave's list
 constexpr int kMostKept = 72;                // of which a cut leaves at most: `top` (at most 64) and 8 more
@@ -322,6 +324,9 @@ __device__ __forceinline__ unsigned long long top_of(const DN_LDS unsigned long 
 }
 
 // ------------------------------------------------------------------------------- results
+// scale (x - m), also where x - m alone has no room in fp32 (halves are exact)
+__device__ __forceinline__ float distance(float x, float m, float scale) { return (0.5f * x - 0.5f * m) * scale * 2.f; }
+
 // A lane's first given token and its logit, read before the pass over the row.
 struct Given {
     int32_t t;
@@ -332,7 +337,7 @@ struct Given {
         x = t >= 0 && t < p.V ? to_f32<T>(logits[t]) : 0.f;
     }
     __device__ __forceinline__ float logprob(const LpArgs& p, const Sums& a, float log_l) const {
-        return t < 0 ? 0.f : t < p.V ? (x - a.m) * p.scale - log_l : __builtin_nanf("");
+        return t < 0 ? 0.f : t < p.V ? distance(x, a.m, p.scale) - log_l : __builtin_nanf("");
     }
 };
 
@@ -346,7 +351,7 @@ __device__ __forceinline__ void finish(const LpArgs& p, int64_t row, const T* x,
     }
     if (p.entropy && lane == 0) p.entropy[row] = log_l - kLn2 * (a.s / a.l);
     if (lane < p.top) {
-        p.top_logprobs[row * p.top + lane] = key ? (value_of(key) - a.m) * p.scale - log_l : __builtin_nanf("");
+        p.top_logprobs[row * p.top + lane] = key ? distance(value_of(key), a.m, p.scale) - log_l : __builtin_nanf("");
         p.top_ids[row * p.top + lane] = key ? (int32_t)id_of(key) : -1;
     }
 }

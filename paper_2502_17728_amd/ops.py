@@ -1118,7 +1118,7 @@ def token_logprobs_workspace_bytes(T: int, V: int, top: int = 0) -> int:
 
 def token_logprobs(logits: torch.Tensor, targets: Optional[torch.Tensor] = None, top: int = 0, scale: float = 1.0,
                    entropy: bool = True, workspace: Optional[torch.Tensor] = None, stream=None):
-    """{"logprobs", "entropy", "top_logprobs", "top_ids"} of softmax(scale * logits) for logits[T, V] (rows may be
+    """{"logprobs", "entropy", "top_logprobs", "top_ids"} of softmax(scale * logits), scale >= 2^-96, for logits[T, V] (rows may be
     strided, V and the stride odd): ln p of targets[T, n] (int32; 0 for a negative one), the entropy [T], and the
     `top` likeliest tokens (the lowest id first among equals) with their ln p.  What was not asked for is None."""
     if logits.dim() != 2:

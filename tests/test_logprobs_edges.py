@@ -1,4 +1,5 @@
-"""Token log probabilities at the edges of their numbers: ranks beside NaNs of either kind (GPU)."""
+"""Token log probabilities at the edges of their numbers: ranks beside NaNs of either kind, logits whose difference has
+no room in fp32."""
 import math
 
 import pytest
@@ -60,3 +61,32 @@ def test_rows_of_little_but_nans(V, dtype, kind):
     got = ops.token_logprobs(logits, None, 3)
     assert torch.equal(got["top_ids"].long(), ranked(logits, 3))
     assert torch.isnan(got["entropy"]).all() and torch.isnan(got["top_logprobs"]).all()
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("V", [6, 40000])
+def test_logits_further_apart_than_their_type_reaches(V, dtype):
+    """x - m passes fp32's range where scale (x - m) does not."""
+    from paper_2502_17728_amd import ops
+    most = torch.finfo(dtype).max
+    logits = torch.zeros((2, V), dtype=dtype, device="cuda")
+    logits[:, 3], logits[0, 4], logits[1, V - 1] = most, -most, -0.75 * most
+    targets = torch.tensor([[3, 4], [V - 1, 0]], dtype=torch.int32, device="cuda")
+    for scale in (0.5, 0.25, 2.0 ** -40, 2.0 ** -96):
+        got, ref = ops.token_logprobs(logits, targets, 6, scale), R.logprobs(logits, targets, 6, scale)
+        # the difference, its product with the scale, ln l's sum and the result's rounding
+        for name in ("logprobs", "top_logprobs"):
+            fits = ref[name].abs() <= torch.finfo(F32).max
+            assert fits.all()
+            R.assert_within(got[name][fits], ref[name][fits], ref[name][fits].abs() * 4 * 2.0 ** -24)
+    top = torch.sort(logits[:, :6].double() if V == 6 else logits.double(), dim=1, descending=True, stable=True)[1][:, :6]
+    assert torch.equal(got["top_ids"].long(), top)
+
+
+def test_scales_that_bring_such_logits_together_are_refused():
+    # below 2^-96 a difference past fp32's range would count in the sums
+    from paper_2502_17728_amd import ops
+    far = [0x7F0000000000 + (i << 36) for i in range(2)]  # not touched: the entropy's address is misaligned, which is seen later
+    call = lambda s: ops._lib.token_logprobs(far[0], 100, 4, 100, 0, s, None, 0, 0, None, far[1] + 1, None, None, None, 0, None)
+    assert call(2.0 ** -97) == 2 and call(1e-40) == 2 and call(2.0 ** -96) == 3 and call(1.0) == 3
