@@ -751,7 +751,9 @@ static void launch_few_rows(const Fp8Args& p, int rf, int nc, dim3 grid, dim3 th
             case 3: fp8_stream_kernel<3, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
             case 4: fp8_stream_kernel<4, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
             case 6: fp8_stream_kernel<6, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
-            case 7: fp8_stream_kernel<7, 8, 1, F32><<<grid, threads, 0, s>>>(p); break;
+            case 7:
+                if constexpr (!F32) fp8_stream_kernel<7, 8, 1, F32><<<grid, threads, 0, s>>>(p);
+                break;
             default: fp8_stream_kernel<8, 8, 1, F32><<<grid, threads, 0, s>>>(p);
         }
     } else {

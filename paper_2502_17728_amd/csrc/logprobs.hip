@@ -550,7 +550,9 @@ static void launch_logprobs(const LpArgs& p, int threads, hipStream_t s) {
     switch (threads) {
         case 64: logprobs_kernel<T, TOP, 64><<<grid, 64, 0, s>>>(p); break;
         case 128: logprobs_kernel<T, TOP, 128><<<grid, 128, 0, s>>>(p); break;
-        case 256: logprobs_kernel<T, TOP, 256><<<grid, 256, 0, s>>>(p); break;
+        case 256:  // ranked rows alone
+            if constexpr (TOP) logprobs_kernel<T, TOP, 256><<<grid, 256, 0, s>>>(p);
+            break;
         default: logprobs_kernel<T, TOP, 512><<<grid, 512, 0, s>>>(p);
     }
     if (p.segments > 1) logprobs_join_kernel<T><<<dim3((unsigned)p.T), kWave, 0, s>>>(p);

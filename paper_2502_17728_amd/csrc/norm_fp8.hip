@@ -197,16 +197,20 @@ __global__ __launch_bounds__(TPR < 256 ? 256 : TPR) void rows_kernel(RowArgs p) 
     }
 }
 
+// Only the kernels that plan_rows can choose: up to 2 pieces to each of 64 threads, 4 to each of 256 and, as long as rows
+// can be, 4 (fp32) or 8 to each of 1024.
 template <class T, int TPR, RowOut OUT>
 static hipError_t launch_pieces(const RowArgs& p, int nv, hipStream_t s) {
-    constexpr int NT = TPR < 256 ? 256 : TPR;
+    constexpr int NT = TPR < 256 ? 256 : TPR, MOST = TPR == 64 ? 2 : TPR == 256 || sizeof(T) == 4 ? 4 : 8;
     const dim3 grid((unsigned)((p.M + NT / TPR - 1) / (NT / TPR)));
-    switch (nv) {
-        case 1: rows_kernel<T, TPR, 1, OUT><<<grid, NT, 0, s>>>(p); break;
-        case 2: rows_kernel<T, TPR, 2, OUT><<<grid, NT, 0, s>>>(p); break;
-        case 4: rows_kernel<T, TPR, 4, OUT><<<grid, NT, 0, s>>>(p); break;
-        default: rows_kernel<T, TPR, 8, OUT><<<grid, NT, 0, s>>>(p); break;
-    }
+    if (nv == 1)
+        rows_kernel<T, TPR, 1, OUT><<<grid, NT, 0, s>>>(p);
+    else if (nv == 2)
+        rows_kernel<T, TPR, 2, OUT><<<grid, NT, 0, s>>>(p);
+    else if (MOST == 4 || nv == 4)
+        rows_kernel<T, TPR, MOST < 4 ? MOST : 4, OUT><<<grid, NT, 0, s>>>(p);
+    else
+        rows_kernel<T, TPR, MOST, OUT><<<grid, NT, 0, s>>>(p);
     return hipGetLastError();
 }
 

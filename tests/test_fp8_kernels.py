@@ -92,3 +92,25 @@ def test_shallow(K, gated, dtype):
     from paper_2502_17728_amd import ops
     for M, N in SHALLOW[gated]:
         _run(ops, M, K, N, bool(gated), dtype)
+
+
+def test_rows_take_no_more_pieces_than_their_kernels_have():
+    most = {64: 2, 256: 4, 1024: 8}
+    seen = set()
+    for M in (1, 2, 255, 256, 257, 5000):
+        for K in range(8, 65537, 8):
+            threads, pieces = call("rows", M, K, n=2)
+            assert pieces <= most[threads] and (pieces <= 4 or K > 32768), (M, K)
+            seen.add((threads, pieces))
+    assert seen == {(t, p) for t in most for p in (1, 2, 4, 8) if p <= most[t]}
+
+
+def test_no_plan_for_fp32_outputs_streams_seven_blocks():
+    for M, K, blocks, gated in itertools.product((1, 5, 16, 17, 33, 64), (16, 784, 4096, 14336), range(1, 6000, 3), (0, 1)):
+        assert call("plan", M, K, blocks, gated, 1, 16, n=6)[:3] != [-1, 1, 7]
+
+
+def test_rows_without_ranks_take_64_128_or_512_threads():
+    seen = {call("lp", T, V, 0, n=2)[0] for T in (1, 5, 255, 256, 500, 511, 512, 1000, 1999, 2000, 4000, 5000, 100000)
+            for V in (1, 100, 1000, 8191, 8192, 16383, 16384, 32000, 131072, 1 << 25)}
+    assert seen == {64, 128, 512}
