@@ -118,6 +118,15 @@ inline int fp8_threads(const Fp8Plan& p) {
     return p.tile >= 0 ? kFp8Tile[p.tile].threads : p.rf == 2 && p.nc > 2 ? 256 : 512;
 }
 
+// Whether the outputs are stored with the non-temporal hint: those of the 256-row tiles, where rows are whole 64-byte pieces.  They
+// then reach HBM beside the products that follow, instead of being written back when these need the cache; broken pieces would go
+// there one part at a time.  us with the hint and without: 4096 x 4096 -> 12288 162, 164, -> 2 x 14336 379, 387 (with the
+// quantisation of its rows behind it 409, 418), 501 rows of it 52, 53 (58, 58); 6244 x 1088 -> 11712 104, 112, -> 11744 107, 113, -> 11728
+// 136, 115, -> 11704 148, 117; in fp32 -> 11712 203, 205, -> 11704 217, 208.
+inline bool fp8_streams_out(const Fp8Plan& p, int64_t N, int f32, uintptr_t out) {
+    return p.tile >= 0 && kFp8Tile[p.tile].bm >= 256 && N * (f32 ? 4 : 2) % 64 == 0 && out % 64 == 0;
+}
+
 inline size_t fp8_workspace(int64_t M, int64_t K, int64_t blocks, int gated) {
     const int64_t splits = std::max(plan_fp8(M, K, blocks, gated, 0, kMaxSplits).splits, plan_fp8(M, K, blocks, gated, 1, kMaxSplits).splits);
     return splits > 1 ? splits * fp8_partial_bytes(M, blocks) : 0;

@@ -154,8 +154,7 @@ struct Residual8 {
         }
     }
 };
-// STREAM: with the non-temporal hint.  The large tiles' outputs then reach HBM beside the products that follow, instead of
-// being written back when these need the cache: 4096 x 4096 -> 12288 174 -> 169 us.
+// STREAM: with the non-temporal hint (fp8_streams_out).
 template <bool STREAM = false>
 __device__ __forceinline__ void store16(void* to, const u32x4& v) {
     if constexpr (STREAM)
@@ -431,7 +430,7 @@ __device__ __forceinline__ f32x16 mfma_32(const Piece2& x, const Piece2& w, f32x
     }
 }
 
-template <int BM, int BN, int WM, int WN, int NST, bool GATED, bool F32>
+template <int BM, int BN, int WM, int WN, int NST, bool GATED, bool F32, bool STREAM = false>
 __global__ __launch_bounds__(WM* WN* kWave) void fp8_tile_kernel(Fp8Args p) {
     constexpr int NW = WM * WN, WTM = BM / WM, WTN = BN / WN, FM = WTM / 32, FN = WTN / 32;
     constexpr int A_BYTES = BM * 128, STAGE = (BM + BN) * 128;
@@ -617,7 +616,7 @@ __global__ __launch_bounds__(WM* WN* kWave) void fp8_tile_kernel(Fp8Args p) {
                     for (int e = 0; e < 8; ++e) v[e] *= ku.z(e < 4 ? u0[e & 3] : u1[e & 3], sx, e);
                 }
                 if (p.residual) res[it].add(p, v);
-                if (row < p.M && n < p.N) store8<(BM >= 256)>(p, row * p.N + n, v);
+                if (row < p.M && n < p.N) store8<STREAM>(p, row * p.N + n, v);
             }
             lds_in_order();
         });
@@ -731,14 +730,19 @@ hipError_t launch_linear_fp8_prepare(const void* W, const float* scales, const v
 }
 
 template <bool GATED, bool F32>
-static void launch_tile(const Fp8Args& p, int tile, dim3 grid, dim3 threads, hipStream_t s) {
+static void launch_tile(const Fp8Args& p, int tile, bool stream, dim3 grid, dim3 threads, hipStream_t s) {
     switch (tile) {
         case 0: fp8_tile_kernel<64, 64, 2, 1, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
         case 1: fp8_tile_kernel<64, 128, 2, 2, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
         case 2: fp8_tile_kernel<128, 128, 2, 2, 4, GATED, F32><<<grid, threads, 0, s>>>(p); break;
-        case 3: fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32><<<grid, threads, 0, s>>>(p); break;
+        case 3:
+            stream ? fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32, true><<<grid, threads, 0, s>>>(p)
+                   : fp8_tile_kernel<256, 128, 4, 2, 3, GATED, F32><<<grid, threads, 0, s>>>(p);
+            break;
         default:
-            if constexpr (!F32) fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32><<<grid, threads, 0, s>>>(p);
+            if constexpr (!F32)
+                stream ? fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32, true><<<grid, threads, 0, s>>>(p)
+                       : fp8_tile_kernel<256, 256, 4, 2, 2, GATED, F32><<<grid, threads, 0, s>>>(p);
     }
 }
 
@@ -773,7 +777,7 @@ hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed,
                              hipStream_t s) {
     const Fp8Layout l = fp8_layout(K, N, gated);
     const char* base = reinterpret_cast<const char*>(packed);
-    const bool f32 = out_dtype == 0;
+    const bool f32 = out_dtype == 0, stream = fp8_streams_out(plan, N, f32, reinterpret_cast<uintptr_t>(out));
     const Fp8Args p{reinterpret_cast<const char*>(x), xs, base, reinterpret_cast<const float*>(base + l.scales),
                     reinterpret_cast<const float*>(base + l.bias), residual, out,
                     plan.splits > 1 ? reinterpret_cast<float*>(workspace) : nullptr, M, K, N, l.kchunks, l.blocks, act, gated,
@@ -782,9 +786,9 @@ hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed,
     if (plan.tile < 0)
         f32 ? launch_few_rows<true>(p, plan.rf, plan.nc, grid, threads, s) : launch_few_rows<false>(p, plan.rf, plan.nc, grid, threads, s);
     else if (gated)
-        f32 ? launch_tile<true, true>(p, plan.tile, grid, threads, s) : launch_tile<true, false>(p, plan.tile, grid, threads, s);
+        f32 ? launch_tile<true, true>(p, plan.tile, stream, grid, threads, s) : launch_tile<true, false>(p, plan.tile, stream, grid, threads, s);
     else
-        f32 ? launch_tile<false, true>(p, plan.tile, grid, threads, s) : launch_tile<false, false>(p, plan.tile, grid, threads, s);
+        f32 ? launch_tile<false, true>(p, plan.tile, stream, grid, threads, s) : launch_tile<false, false>(p, plan.tile, stream, grid, threads, s);
     if (plan.splits > 1) fp8_join_kernel<<<dim3((unsigned)((M * (N / 8) + 255) / 256)), 256, 0, s>>>(p);
     return hipGetLastError();
 }
