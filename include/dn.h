@@ -564,9 +564,11 @@ DN_API dn_status linear_fp8_prepare(const void* W, const float* scales, const vo
  * the codes are widened to bf16 (exactly) and their products summed in fp32; with DN_BF16
  * the 8-bit matrix instructions sum them, twice as fast, which keep the products of 16
  * neighbours along K to 2^-13 of their largest: 1.5e-5 of a result of normal data in the
- * 2-norm, a hundredth of the output's rounding.  GELU is off by at most (24 + 1.5 z^2) 2^-24 of
- * itself with an fp32 output, for z down to -12.5, and by 3.6e-5 more with a bf16 one.  residual[M][N] (out_dtype) may
- * be NULL, and may be out itself.
+ * 2-norm, a hundredth of the output's rounding; sums of products of one sign come out 2.6e-6
+ * of themselves low.  A row's scale multiplies its sums before the columns' scales do: the
+ * products of both have to fit fp32.  GELU is off by at most (24 + 1.5 z^2) 2^-24 of itself
+ * with an fp32 output, for z down to -12.5, and by 3.6e-5 more with a bf16 one.
+ * residual[M][N] (out_dtype) may be NULL, and may be out itself.
  * workspace: caller-owned, 256-byte aligned, linear_fp8_workspace_bytes(M, w) bytes
  * (NULL where that is 0), scratch of one call at a time: calls of few tiles split K over
  * several workgroups, whose fp32 partial sums a second kernel joins in a fixed order.
@@ -576,7 +578,7 @@ typedef enum {
     DN_ACT_NONE = 0,
     DN_ACT_RELU = 1,
     DN_ACT_SILU = 2,      /* z / (1 + e^-z)                                             */
-    DN_ACT_GELU = 3,      /* z (1 + erf(z / sqrt 2)) / 2                                */
+    DN_ACT_GELU = 3,      /* z (1 + erf(z / sqrt 2)) / 2; 0 at -inf                     */
     DN_ACT_GELU_TANH = 4  /* z (1 + tanh(sqrt(2 / pi) (z + 0.044715 z^3))) / 2          */
 } dn_activation;
 

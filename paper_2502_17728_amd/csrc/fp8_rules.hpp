@@ -49,8 +49,8 @@ inline Fp8Layout fp8_layout(int64_t K, int64_t N, int gated) {
 //   512 rows 4096 -> 12288   256 x 128 28.8, 128 x 128 35.5, 256 x 256 42.4
 //   1024 rows 4096 -> 12288  256 x 256 48.9, 256 x 128 56.6, 128 x 128 59.8
 //   2048 rows 14336 -> 4096  256 x 128 101, 128 x 128 124, 256 x 256 (128 tiles) 128
-// K is split where that fills the chip: 32 rows 14336 -> 4096 15.7 us with 4 splits of 64 x 128, 43 without;
-// the join costs a launch and the traffic of the fp32 sums.
+// K is split where that fills the chip: 100 rows 14336 -> 4096 16.9 us with 8 splits, 17.1 with 4, 19.0 with 2, 26.9 without; the join
+// costs a launch and the traffic of the fp32 sums.
 constexpr int kFp8Tiles = 5;
 struct Fp8Tile {
     int bm, bn, threads, per_cu;
@@ -80,6 +80,7 @@ inline Fp8Plan plan_fp8(int64_t M, int64_t K, int64_t blocks, int gated, int f32
     Fp8Plan best{-1, 0, 0, 1, 0};
     // Up to 64 rows: W streamed into registers (rf 1) or rings of the waves' own (rf 2).  Per step of 128 codes 0.02 us and
     // 0.072 us per column block, or 0.045 and 0.068.  16 rows 4096 -> 4096 5.7 us, 32 rows 6.4, 64 rows 7.2, in tiles 10.4.
+    // (5 blocks, which would suit widths of about 20480, are not built.)
     for (int rf = 1; rf <= 2 && M <= 64; ++rf) {
         const int64_t rows = (M + 16 * rf - 1) / (16 * rf);
         static constexpr int kNc[7] = {1, 2, 3, 4, 6, 7, 8};
@@ -137,9 +138,11 @@ constexpr int64_t kMaxTop = 64, kMaxSegments = 16;
 
 // Threads to a workgroup and workgroups to a row.  Each wave ranks what it reads by itself, so ranked rows take as few
 // waves as fill the chip, and rows without ranks few only if they are short.  Measured, us, with 512, 256, 128 and 64 threads,
-// bf16 with 20 alternatives: 300 x 131072 34.6, 37.2, 57.4, -; 1000 x 100003 48.8, 46.0, 49.1, -; 2000 x 8192 -, 20.8, 17.9, 18.4;
-// 4000 x 32008 87.7, 66.1, 57.8, 53.5; 8000 x 32008 171, 128, 108, 114; 16000 x 8192 179, 115, 86, 67; without: 16000 x 8192
-// 58, 49, 44, 44; 16000 x 1000 -, 28, 20, 12; fp32 4000 x 32008 87.8, 91.2, 96.9, 94.0.
+// bf16 with 20 alternatives: 300 x 131072 34.6, 37.2, 57.4, -; 1000 x 100003 50.3, 45.9, 49.7, 67.3; 2000 x 8192 28.3, 21.2, 18.0, 18.3;
+// 4000 x 32008 90.8, 67.2, 59.1, 53.7; 8000 x 32008 177, 130, 110, 115; 16000 x 8192 195, 120, 88, 68; without alternatives:
+// 16000 x 8192 58, 49, 44, 44; 16000 x 1000 -, 28, 20, 12; fp32 4000 x 32008 87.8, 91.2, 96.9, 94.0.
+// The rule was fitted to these and asks neither for the type nor for `top`, which costs up to a fifth elsewhere: fp32 with 20
+// 4000 x 32008 116, 100, 108, 100, 16000 x 8192 204, 136, 111, 104; bf16 4000 x 32008 with 64 193, 117, 93, 76, with 5 70, 54, 52, 48.
 // Fewer than 256 rows get a workgroup to each 16384 tokens while there is about one to a CU; a second kernel then joins
 // them: 32 x 131072 17.2 (8 segments; 16: 18.7, 4: 21.0), 1 x 32000 12.4 (2; 1: 13.6), 200 x 32000 16.8 (1; 2: 19.0).
 struct LogprobPlan {

@@ -36,8 +36,8 @@ struct Fp8Args {
 
 // Sums.  The 8-bit matrix instructions (this one and its half-rate relatives alike) add products in groups
 // of 16 along k aligned to the group's largest, with 13 bits below it, and the groups in fp32 (probed with
-// products that cancel): 1.5e-5 of a result of normal data in the 2-norm, without bias, for any K.
-// A bf16 output's rounding is 100 times that.  An fp32 output's is not: there the codes are widened to bf16, which
+// products that cancel): 1.5e-5 of a result of normal data in the 2-norm, for any K; sums of products of one sign
+// come out 2.6e-6 of themselves low.  A bf16 output's rounding is 100 times that.  An fp32 output's is not: there the codes are widened to bf16, which
 // holds them exactly, and the bf16 instructions keep their products and sums to 2^-24, at half the rate.
 __device__ __forceinline__ bf16x8_t widen8(uint32_t lo, uint32_t hi) {
     const auto a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.f, true);
@@ -305,8 +305,8 @@ __global__ __launch_bounds__(KS* kWave) void fp8_stream_kernel(Fp8Args p) {
 }
 
 // The same for 32 rows, whose x loads would be half lines: each wave copies its steps of x, as whole 128-byte lines, and
-// of W into a ring of D slots of its own in LDS and waits for nobody.  Bound by the copies, about 57 bytes a ns
-// and CU for x (from L2) and W together: 32 rows 14336 -> 4096 15.3 us (loads into registers 18.2), 4096 -> 4096 6.4 (7.3).
+// of W into a ring of D slots of its own in LDS and waits for nobody.  Bound by the copies of x (from L2) and W together, about 55
+// bytes a ns and CU: 32 rows 14336 -> 4096 (180 MB of L2 reads by the counters) 15.3 us (loads into registers 18.2), 4096 -> 4096 6.4 (7.3).
 template <int NC, int KS, int D, bool F32>
 __global__ __launch_bounds__(KS* kWave) void fp8_ring_kernel(Fp8Args p) {
     constexpr int ROWS = 32, P = 4 + 2 * NC, SLOT = P * kChunkBytes, LDR = NC * 16 + 4;
@@ -786,9 +786,11 @@ hipError_t launch_linear_fp8(const void* x, const float* xs, const void* packed,
     if (plan.tile < 0)
         f32 ? launch_few_rows<true>(p, plan.rf, plan.nc, grid, threads, s) : launch_few_rows<false>(p, plan.rf, plan.nc, grid, threads, s);
     else if (gated)
-        f32 ? launch_tile<true, true>(p, plan.tile, stream, grid, threads, s) : launch_tile<true, false>(p, plan.tile, stream, grid, threads, s);
+        f32 ? launch_tile<true, true>(p, plan.tile, stream, grid, threads, s)
+            : launch_tile<true, false>(p, plan.tile, stream, grid, threads, s);
     else
-        f32 ? launch_tile<false, true>(p, plan.tile, stream, grid, threads, s) : launch_tile<false, false>(p, plan.tile, stream, grid, threads, s);
+        f32 ? launch_tile<false, true>(p, plan.tile, stream, grid, threads, s)
+            : launch_tile<false, false>(p, plan.tile, stream, grid, threads, s);
     if (plan.splits > 1) fp8_join_kernel<<<dim3((unsigned)((M * (N / 8) + 255) / 256)), 256, 0, s>>>(p);
     return hipGetLastError();
 }

@@ -16,7 +16,8 @@
 // keys are then cut together, and only what is left, about `top` keys, is put in order.
 //
 // Bound by HBM where fp32 is read (4000 x 32001 88 us, 5.8 TB/s), by the VALU in bf16 (1000 x 100003 34 us without ranks,
-// 46 with 20; HBM 29), by launches and the serial ranking for short inputs (1 x 8192 6.4 us, 32 x 131072 12.7 and a join).
+// 46 with 20, 47.5 on other logits each time; HBM 29), by launches and the serial ranking for short inputs (1 x 8192 6.4 us,
+// 32 x 131072 12.7 and a join).
 #include "dn_device.hpp"
 #include "dn_launch.hpp"
 #include "fp8_rules.hpp"
